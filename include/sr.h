@@ -281,6 +281,111 @@ int sr_grpo_loss_static(const double *logprob, const float *rewards, int n_group
                         float *advantages, double *loss, void *stream);
 
 /*
+ * The update half of a GRPO step, from the logits that the policy being trained gives to the tokens of the kept
+ * trajectories (Appendix C.2: one causal forward, log softmax at action-token positions; Section 2.1: the loss over them)
+ * to gradients that an optimizer can take.  No context needed; the caller brings every buffer.
+ *
+ * Rows.  Row t of `logits` is the distribution of token targets[t].  The rows of a sequence lie together, the sequences
+ * one behind another: sequence i owns rows [seq_start[i], seq_start[i + 1]), some possibly none.  A row counts unless its
+ * mask entry is 0 or it lies outside [seq_start[0], seq_start[n_seq]) (padding).  Rows that do not count are not read; they
+ * receive log-probability 0 and a gradient of exactly 0.  An entry of -infinity is a token that cannot occur; a row whose
+ * entries are all -infinity, or that holds NaN or +infinity, has log-probability NaN, and so has a counting row whose target
+ * lies outside the vocabulary.  seq_start must not decrease; other values give unspecified results, but no access outside
+ * the buffers.
+ *
+ * Arithmetic: the logits are widened to single precision; maximum, sum of exponentials, loss and slopes are single
+ * precision, sums over tokens double, added in a fixed order (the results are the same bit for bit from call to call); the
+ * gradient is rounded once, to the type of the logits.
+ */
+typedef enum { SR_F32 = 0, SR_BF16 = 1, SR_F16 = 2 } sr_dtype;
+
+typedef struct {
+    const void *logits;        /* device [n_rows][ld_logits], of type dtype, any alignment that the type allows */
+    void *grad;                /* device [n_rows][ld_grad], same type: d(loss * grad_scale) / d(logits); may be `logits` itself
+                                  (with the same row stride), must not overlap it otherwise; NULL: the loss alone */
+    int64_t ld_logits, ld_grad;/* elements from one row to the next, >= vocab */
+    const int32_t *targets;    /* device [n_rows] */
+    const uint8_t *mask;       /* device [n_rows], 0 = the row does not count; NULL: all count */
+    const int32_t *seq_start;  /* device [n_seq + 1] */
+    float *token_logprob;      /* device [n_rows], written; may be NULL */
+    int32_t dtype;             /* sr_dtype of logits and grad */
+    int32_t n_rows, vocab, n_seq;
+    float grad_scale;          /* multiplies the gradient only (loss scaling for 16-bit gradients) */
+    int32_t reserved;
+} sr_token_rows;
+
+/* Bytes of device memory, 16-byte aligned, that the two losses need as workspace.  Nothing in it outlives the call, and
+ * calls that may overlap (different streams) need one each. */
+#define SR_TOKEN_LOSS_WORKSPACE(n_rows, n_seq) (65536 + (size_t)64 * (size_t)(n_rows) + (size_t)32 * (size_t)(n_seq))
+
+/*
+ * Clipped policy loss with a KL term.  With l the log-probability of a counting row's token, A the advantage of its
+ * sequence (Eq. 1; sr_grpo_loss writes them), r = exp(l - old_logprob) and, where ref_logprob is given, d = ref_logprob - l:
+ *     surrogate = min(r A, clip(r, 1 - clip_low, 1 + clip_high) A)        kl = exp(d) - d - 1
+ *     loss = mean(kl_coef * kl - surrogate)
+ * (kl is the estimate, never negative, of KL(policy | reference) from the sampled token.)  The mean is one of
+ *     SR_MEAN_TOKENS     over all counting rows
+ *     SR_MEAN_SEQUENCES  over the rows of a sequence, then over the sequences that have any
+ *     SR_MEAN_SUMS       of the sums over a sequence's rows, over the sequences that have any: with r = 1 and kl_coef = 0 the
+ *                        gradient of the loss of Section 2.1
+ * and 0 where nothing counts.  The gradient of a row is slope * (onehot(target) - softmax), slope = weight *
+ * (kl_coef * (1 - exp(d)) - r A [r A <= clip(r) A]).
+ * stats: device float [4]: loss, mean surrogate, mean kl (0 without ref_logprob), mean of [r A > clip(r) A] (the fraction of
+ * tokens that the clip takes out of the gradient).
+ * old_logprob, ref_logprob: device float [n_rows], as sr_score_chunk writes them; ref_logprob may be NULL if kl_coef == 0.
+ * advantages: device float [n_seq].
+ * SR_E_ARG: null pointers, a bad dtype, shape, stride or option, a workspace that is too small or not 16-byte aligned.
+ * n_rows may be 0.
+ */
+typedef enum { SR_MEAN_TOKENS = 0, SR_MEAN_SEQUENCES = 1, SR_MEAN_SUMS = 2 } sr_reduce;
+typedef struct {
+    float clip_low, clip_high; /* 0 <= clip_low <= 1, clip_high >= 0 */
+    float kl_coef;
+    int32_t reduce;            /* sr_reduce */
+} sr_policy_options;
+int sr_policy_loss(const sr_token_rows *rows, const float *old_logprob, const float *ref_logprob, const float *advantages,
+                   const sr_policy_options *opt, float *stats, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Preference loss over pairs of sequences: sequence 2 i is the one preferred to sequence 2 i + 1 (two members of a group with
+ * different rewards, for example).  With the log ratio L of a sequence = sum over its counting rows of (l - ref_logprob) and
+ * the margin m_i = beta (L_{2i} - L_{2i+1}):
+ *     loss = mean over pairs of  -(1 - label_smoothing) log sigmoid(m) - label_smoothing log sigmoid(-m)
+ * A sequence without counting rows has L = 0.  The gradient of a row of sequence 2 i is s_i (onehot(target) - softmax), of
+ * sequence 2 i + 1 the same with -s_i, s_i = beta / pairs * (label_smoothing sigmoid(m_i) - (1 - label_smoothing) sigmoid(-m_i)).
+ * stats: device float [4]: loss, fraction of pairs with m > 0, mean of beta L over the preferred and over the other sequences.
+ * log_ratio: device float [n_seq] receiving L, or NULL.  ref_logprob: device float [n_rows], or NULL (taken as 0).
+ * SR_E_ARG as above, and n_seq odd, beta not finite, label_smoothing outside [0, 1].
+ */
+int sr_preference_loss(const sr_token_rows *rows, const float *ref_logprob, float beta, float label_smoothing, float *log_ratio,
+                       float *stats, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The global 2-norm of a list of gradient tensors, and the list scaled down to a largest norm.
+ *     norm = |scale| * sqrt(sum over all tensors and elements of g^2)        c = max_norm / norm if norm > max_norm, else 1
+ *     out = scale * c * g
+ * norm: device float [1].  Squares are added in double, in a fixed order, so that neither 1e30 nor 1e-30 is lost and
+ * the norm is the same bit for bit from call to call.  A norm that is infinite or NaN is written as it is, and c is 1: what
+ * was not finite stays where it was, for the caller who looks at the norm.
+ * host_tensors: HOST array, read during the call only; the data are device memory, contiguous, any alignment that the type
+ * allows.  `out` may be `data` itself or NULL (in place; then nothing is written where scale * c is 1) and must not overlap any
+ * tensor otherwise; its type is that of the data, or SR_F32.  sr_grad_norm reads `data` only.
+ * workspace: SR_GRAD_NORM_WORKSPACE bytes of device memory, 16-byte aligned.
+ * SR_E_ARG: null pointers, n < 0, a bad type, scale or max_norm not finite, max_norm < 0.  The list and its tensors may be empty.
+ */
+typedef struct {
+    void *data;
+    void *out;
+    int64_t n;                 /* elements */
+    int32_t dtype, out_dtype;  /* sr_dtype; out_dtype is ignored where out is NULL */
+} sr_tensor;
+#define SR_GRAD_NORM_WORKSPACE 65536
+int sr_grad_norm(const sr_tensor *host_tensors, int n_tensors, float scale, float *norm, void *workspace, size_t workspace_bytes,
+                 void *stream);
+int sr_clip_grad_norm(const sr_tensor *host_tensors, int n_tensors, float scale, float max_norm, float *norm, void *workspace,
+                      size_t workspace_bytes, void *stream);
+
+/*
  * The in-group divergence signals of Appendix B at step K, and the gates of Eq. 2 and of
  * Appendix E (Eq. 3), for groups whose members may have finished early (no context needed).
  *

@@ -21,7 +21,12 @@ EXPORTS = ("sr_init", "sr_destroy", "sr_load_weights", "sr_prefill_chunk", "sr_d
            "sr_get_live_map", "sr_stats", "sr_strerror", "sr_profile", "sr_profile_read", "sr_signals_batch",
            "sr_score_chunk", "sr_get_logprob", "sr_grpo_loss", "sr_finish_sequences", "sr_grpo_loss_static",
            "sr_probe_hbm", "sr_probe_mfma_bf16", "sr_probe_mfma_under_loads", "sr_gate_batch_antidiag",
-           "sr_probe_decode_attention")
+           "sr_probe_decode_attention", "sr_policy_loss", "sr_preference_loss", "sr_grad_norm", "sr_clip_grad_norm")
+
+# element types of the update step (sr_dtype) by the name that torch gives them, and ways to take the mean (sr_reduce)
+DTYPES = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}
+REDUCE = {"tokens": 0, "sequences": 1, "sums": 2}
+GRAD_NORM_WORKSPACE = 65536
 
 KERNEL_CLASSES = ("norm", "gemm_qkv", "qkv_post", "attn_decode", "attn_prefill", "attn_merge",
                   "gemm_o", "gemm_gate_up", "gemm_down", "gemm_lm_head", "argmax")
@@ -55,6 +60,24 @@ class LayerWeights(ctypes.Structure):
 class Weights(ctypes.Structure):
     _fields_ = [("embed", ctypes.c_void_p), ("lm_head", ctypes.c_void_p), ("final_norm", ctypes.c_void_p),
                 ("layers", ctypes.POINTER(LayerWeights))]
+
+
+class TokenRows(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("ld_logits", ctypes.c_int64), ("ld_grad", ctypes.c_int64),
+                ("targets", ctypes.c_void_p), ("mask", ctypes.c_void_p), ("seq_start", ctypes.c_void_p),
+                ("token_logprob", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("n_rows", ctypes.c_int32),
+                ("vocab", ctypes.c_int32), ("n_seq", ctypes.c_int32), ("grad_scale", ctypes.c_float),
+                ("reserved", ctypes.c_int32)]
+
+
+class PolicyOptions(ctypes.Structure):
+    _fields_ = [("clip_low", ctypes.c_float), ("clip_high", ctypes.c_float), ("kl_coef", ctypes.c_float),
+                ("reduce", ctypes.c_int32)]
+
+
+class Tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("out_dtype", ctypes.c_int32)]
 
 
 class KernelTime(ctypes.Structure):
@@ -102,6 +125,12 @@ def lib():
         L.sr_probe_mfma_bf16.argtypes = [vp, ctypes.c_size_t, ci, vp, ctypes.POINTER(ctypes.c_double)]
         L.sr_probe_mfma_under_loads.argtypes = [vp, ctypes.c_size_t, vp, ctypes.c_size_t, ci, ci, ci, ci, vp,
                                                 ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double)]
+        L.sr_policy_loss.argtypes = [ctypes.POINTER(TokenRows), vp, vp, vp, ctypes.POINTER(PolicyOptions), vp, vp,
+                                     ctypes.c_size_t, vp]
+        L.sr_preference_loss.argtypes = [ctypes.POINTER(TokenRows), vp, ctypes.c_float, ctypes.c_float, vp, vp, vp,
+                                         ctypes.c_size_t, vp]
+        L.sr_grad_norm.argtypes = [vp, ci, ctypes.c_float, vp, vp, ctypes.c_size_t, vp]
+        L.sr_clip_grad_norm.argtypes = [vp, ci, ctypes.c_float, ctypes.c_float, vp, vp, ctypes.c_size_t, vp]
         L.sr_finish_sequences.argtypes = [vp, vp, ctypes.POINTER(ci), vp]
         L.sr_set_actions.argtypes = [vp, ci, vp, vp]
         L.sr_get_actions.argtypes = [vp, vp, vp]
@@ -188,6 +217,111 @@ def sr_grpo_loss_static(logprob, rewards, G: int, eps: float, advantages, loss, 
     n_groups = logprob.numel() // G
     _check(lib().sr_grpo_loss_static(_ptr(logprob), _ptr(rewards), n_groups, G, eps, _ptr(advantages), _ptr(loss),
                                      _stream(stream)), "sr_grpo_loss_static")
+
+
+def token_loss_workspace(n_rows: int, n_seq: int) -> int:
+    """Bytes of workspace for sr_policy_loss and sr_preference_loss (SR_TOKEN_LOSS_WORKSPACE)."""
+    return 65536 + 64 * n_rows + 32 * n_seq
+
+
+def _of_type(t, name: str, n: int, what: str):
+    """Address of a contiguous tensor of n elements of that type, or None."""
+    if t is None:
+        return None
+    if str(t.dtype) != name or t.numel() != n or not t.is_contiguous():
+        raise SrError(SR_E_ARG, f"{what}: contiguous {name} tensor of {n} elements expected, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _token_rows(where, logits, targets, seq_start, mask, grad, token_logprob, grad_scale):
+    if logits.dim() != 2 or str(logits.dtype) not in DTYPES or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise SrError(SR_E_ARG, f"{where}: logits: [rows, vocab] of float32, bfloat16 or float16 with adjacent columns expected")
+    n, vocab = logits.shape
+    ld_grad = 0
+    if grad is not None:
+        if grad.shape != logits.shape or grad.dtype != logits.dtype or (vocab > 1 and grad.stride(1) != 1):
+            raise SrError(SR_E_ARG, f"{where}: grad: shape and type of the logits, with adjacent columns, expected")
+        ld_grad = grad.stride(0) if n > 1 else vocab
+        grad = grad.data_ptr()
+    n_seq = seq_start.numel() - 1
+    return TokenRows(logits.data_ptr(), grad, logits.stride(0) if n > 1 else vocab, ld_grad,
+                     _of_type(targets, "torch.int32", n, "targets"), _of_type(mask, "torch.uint8", n, "mask"),
+                     _of_type(seq_start, "torch.int32", n_seq + 1, "seq_start"),
+                     _of_type(token_logprob, "torch.float32", n, "token_logprob"), DTYPES[str(logits.dtype)], n, vocab, n_seq,
+                     grad_scale, 0)
+
+
+def sr_policy_loss(logits, targets, seq_start, old_logprob, advantages, stats, workspace, *, mask=None, ref_logprob=None,
+                   grad=None, token_logprob=None, clip_low=0.2, clip_high=0.2, kl_coef=0.0, reduce="tokens", grad_scale=1.0,
+                   stream=None):
+    """Clipped policy loss with a KL term over the rows of `logits` (float32, bfloat16 or float16 [rows, vocab]; rows may be
+    padded), and its gradient in `grad` (same shape and type; may be `logits` itself; None: the loss alone).
+
+    targets int32 [rows]; seq_start int32 [sequences + 1]; old_logprob, ref_logprob, token_logprob float32 [rows];
+    advantages float32 [sequences]; mask uint8 [rows]; stats float32 [4] receives loss, surrogate, KL, clipped fraction;
+    workspace: device bytes, token_loss_workspace(rows, sequences) of them; reduce: "tokens", "sequences" or "sums"."""
+    rows = _token_rows("sr_policy_loss", logits, targets, seq_start, mask, grad, token_logprob, grad_scale)
+    opt = PolicyOptions(clip_low, clip_high, kl_coef, REDUCE[reduce])
+    _check(lib().sr_policy_loss(ctypes.byref(rows), _of_type(old_logprob, "torch.float32", rows.n_rows, "old_logprob"),
+                                _of_type(ref_logprob, "torch.float32", rows.n_rows, "ref_logprob"),
+                                _of_type(advantages, "torch.float32", rows.n_seq, "advantages"), ctypes.byref(opt),
+                                _of_type(stats, "torch.float32", 4, "stats"), workspace.data_ptr(),
+                                workspace.numel() * workspace.element_size(), _stream(stream)), "sr_policy_loss")
+
+
+def sr_preference_loss(logits, targets, seq_start, stats, workspace, *, mask=None, ref_logprob=None, grad=None,
+                       token_logprob=None, log_ratio=None, beta=0.1, label_smoothing=0.0, grad_scale=1.0, stream=None):
+    """Preference loss over pairs of sequences (2 i preferred to 2 i + 1), and its gradient in `grad`; arguments as for
+    sr_policy_loss.  stats float32 [4] receives loss, fraction of pairs in the right order, mean reward of the preferred
+    and of the other sequences; log_ratio float32 [sequences]."""
+    rows = _token_rows("sr_preference_loss", logits, targets, seq_start, mask, grad, token_logprob, grad_scale)
+    _check(lib().sr_preference_loss(ctypes.byref(rows), _of_type(ref_logprob, "torch.float32", rows.n_rows, "ref_logprob"), beta,
+                                    label_smoothing, _of_type(log_ratio, "torch.float32", rows.n_seq, "log_ratio"),
+                                    _of_type(stats, "torch.float32", 4, "stats"), workspace.data_ptr(),
+                                    workspace.numel() * workspace.element_size(), _stream(stream)), "sr_preference_loss")
+
+
+class TensorList:
+    """The tensors of a norm, as the C boundary takes them; keeps them alive.  To be built again when one of them is replaced."""
+
+    def __init__(self, tensors, out=None):
+        self.tensors, self.out = list(tensors), None if out is None else list(out)
+        if self.out is not None and len(self.out) != len(self.tensors):
+            raise SrError(SR_E_ARG, "tensor_list: one output per tensor expected")
+        self.array = (Tensor * len(self.tensors))()
+        for i, t in enumerate(self.tensors):
+            o = self.out[i] if self.out is not None else None
+            for x in (t, o):
+                if x is not None and (str(x.dtype) not in DTYPES or not x.is_contiguous() or x.numel() != t.numel()):
+                    raise SrError(SR_E_ARG, f"tensor_list: contiguous float32, bfloat16 or float16 tensors expected ({i})")
+            self.array[i] = Tensor(t.data_ptr(), None if o is None else o.data_ptr(), t.numel(), DTYPES[str(t.dtype)],
+                                   DTYPES[str((t if o is None else o).dtype)])
+
+
+def tensor_list(tensors, out=None) -> TensorList:
+    """tensors: contiguous float32, bfloat16 or float16 device tensors; out: where the scaled tensors go (same type, or
+    float32), None = in place."""
+    return TensorList(tensors, out)
+
+
+def _norm_args(tensors, norm, workspace):
+    if not isinstance(tensors, TensorList):
+        tensors = TensorList(tensors)
+    return (tensors.array, len(tensors.array)), (_of_type(norm, "torch.float32", 1, "norm"), workspace.data_ptr(),
+                                                 workspace.numel() * workspace.element_size())
+
+
+def sr_grad_norm(tensors, norm, workspace, *, scale=1.0, stream=None):
+    """norm (device float32 [1]) = |scale| * the 2-norm over all tensors (a tensor_list, or a list of tensors);
+    workspace: GRAD_NORM_WORKSPACE device bytes."""
+    head, tail = _norm_args(tensors, norm, workspace)
+    _check(lib().sr_grad_norm(*head, scale, *tail, _stream(stream)), "sr_grad_norm")
+
+
+def sr_clip_grad_norm(tensors, max_norm: float, norm, workspace, *, scale=1.0, stream=None):
+    """sr_grad_norm, and the tensors times scale * min(1, max_norm / norm), in place or to the list's outputs."""
+    head, tail = _norm_args(tensors, norm, workspace)
+    _check(lib().sr_clip_grad_norm(*head, scale, max_norm, *tail, _stream(stream)), "sr_clip_grad_norm")
 
 
 def sr_probe_hbm(src, dst, mode: int, iters: int = 10, stream=None) -> float:

@@ -1,0 +1,110 @@
+// 16 bytes at a time of float, bf16 or f16 data that may begin at any address its type allows, widened to single precision;
+// and the sum over a workgroup.  Shared by the kernels of the update step.
+#pragma once
+#include <float.h>
+
+#include "sr_internal.h"
+
+namespace sr {
+
+typedef _Float16 f16_t;
+
+// The hardware reads and writes vectors at any address; the alignment says so to the compiler, which then splits nothing.
+typedef uint32_t raw16 __attribute__((ext_vector_type(4), aligned(16)));
+typedef uint32_t raw16_any __attribute__((ext_vector_type(4), aligned(2)));
+
+template <typename T> struct Elem;
+template <> struct Elem<float> {
+    static constexpr int kPerVec = 4;
+    static __device__ __forceinline__ void widen(const raw16 &r, float *x) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(r[i]);
+    }
+    static __device__ __forceinline__ raw16 narrow(const float *x) {
+        raw16 r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = __float_as_uint(x[i]);
+        return r;
+    }
+};
+template <> struct Elem<__bf16> {
+    static constexpr int kPerVec = 8;
+    static __device__ __forceinline__ void widen(const raw16 &r, float *x) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(r[i] << 16);
+            x[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ raw16 narrow(const float *x) {
+        raw16 r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+        return r;
+    }
+};
+template <> struct Elem<f16_t> {
+    static constexpr int kPerVec = 8;
+    typedef f16_t pair __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ void widen(const raw16 &r, float *x) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const pair p = __builtin_bit_cast(pair, (uint32_t)r[i]);
+            x[2 * i] = (float)p[0];
+            x[2 * i + 1] = (float)p[1];
+        }
+    }
+    static __device__ __forceinline__ raw16 narrow(const float *x) {
+        raw16 r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const pair p = {(f16_t)x[2 * i], (f16_t)x[2 * i + 1]};
+            r[i] = __builtin_bit_cast(uint32_t, p);
+        }
+        return r;
+    }
+};
+
+template <typename T> __device__ __forceinline__ raw16 load_vec(const T *p) { return *(const raw16_any *)p; }
+template <typename T> __device__ __forceinline__ void store_vec(T *p, raw16 v) { *(raw16_any *)p = v; }
+
+// Elements [at, at + kPerVec) of a run of n, `fill` behind its end
+template <typename T>
+__device__ __forceinline__ void load_widened(const T *p, int64_t at, int64_t n, float fill, float *x) {
+    constexpr int N = Elem<T>::kPerVec;
+    if (at + N <= n) {
+        Elem<T>::widen(load_vec(p + at), x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = at + i < n ? (float)p[at + i] : fill;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store_narrowed(T *p, int64_t at, int64_t n, const float *x) {
+    constexpr int N = Elem<T>::kPerVec;
+    if (at + N <= n) {
+        store_vec(p + at, Elem<T>::narrow(x));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (at + i < n) p[at + i] = (T)x[i];
+    }
+}
+
+// Sum over the workgroup, in an order that depends on the thread number alone; valid in thread 0.  s: WAVES doubles of LDS,
+// free to be overwritten.
+template <int WAVES>
+__device__ __forceinline__ double block_sum(double x, double *s) {
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off, 64);
+    if (WAVES == 1) return x;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = 0.0;
+    if (threadIdx.x == 0)
+        for (int w = 0; w < WAVES; ++w) x += s[w];
+    return x;
+}
+
+}  // namespace sr

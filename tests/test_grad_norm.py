@@ -1,0 +1,192 @@
+"""sr_grad_norm and sr_clip_grad_norm against a plain evaluation in 64 bits.
+
+Tolerances.  Squares are formed and added in 64 bits (at most 2^31 terms: relative 1e-7 at the very worst, 1e-12 as a rule), so the
+norm carries one rounding to single precision; the factor another, the product a third and, for 16-bit outputs, a fourth to
+the output's type: 4 * 2^-24 relative, plus half a unit in the last place of the output's type."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_05802_amd as sr
+
+U = 2.0 ** -24
+ROUND = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+SMALLEST = {torch.float32: 1.5e-45, torch.bfloat16: 1e-40, torch.float16: 2.0 ** -24}
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+def work():
+    return torch.full((1,), 7.0, device="cuda"), torch.full((sr.GRAD_NORM_WORKSPACE,), 255, dtype=torch.uint8, device="cuda")
+
+
+def tensors_of(sizes, dtypes, seed, std=0.01, shift=0):
+    """Tensors that begin `shift` elements behind an aligned address."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    out = []
+    for i, n in enumerate(sizes):
+        d = dtypes[i % len(dtypes)]
+        buf = torch.empty(n + shift, dtype=d, device="cuda")
+        buf.copy_(torch.randn(n + shift, generator=g, device="cuda") * std)
+        out.append(buf[shift:])
+    return out
+
+
+def norm_of(ts, scale=1.0):
+    return abs(scale) * math.sqrt(sum(float((t.double() ** 2).sum()) for t in ts))
+
+
+def check(ts, max_norm, scale=1.0, out_dtype=None, in_place=False):
+    want = norm_of(ts, scale)
+    c = scale * (max_norm / want if want > max_norm else 1.0)
+    expect = [t.double() * c for t in ts]
+    norm, ws = work()
+    sr.sr_grad_norm(ts, norm, ws, scale=scale)
+    assert norm.item() == pytest.approx(want, rel=4 * U)
+    norm.fill_(7.0)
+    outs = None if in_place else [torch.full_like(t, 5.0, dtype=out_dtype or t.dtype) for t in ts]
+    sr.sr_clip_grad_norm(sr.tensor_list(ts, outs), max_norm, norm, ws, scale=scale)
+    assert norm.item() == pytest.approx(want, rel=4 * U)
+    for got, e in zip(ts if in_place else outs, expect):
+        tol = e.abs() * (4 * U + ROUND[got.dtype]) + SMALLEST[got.dtype]
+        assert bool(((got.double() - e).abs() <= tol).all())
+    return norm, outs
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,out", [(F32, F32), (BF16, BF16), (BF16, F32), (F16, F16), (F16, F32)])
+@pytest.mark.parametrize("sizes", [[1], [7], [8], [0, 3, 0], [8191, 8192, 8193], [1 << 20], [5, 100003, 1, 64, 262147], list(range(1, 400))])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_sizes_types_and_alignment(dtype, out, sizes, shift):
+    ts = tensors_of(sizes, [dtype], 1, shift=shift)
+    norm = norm_of(ts)
+    for limit in (0.5 * norm, 2 * norm):
+        check(ts, limit, out_dtype=out)
+    if out == dtype:
+        check(ts, 2 * norm, in_place=True)
+        check(ts, 0.5 * norm, in_place=True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale", [0.125, -2.0, 1.0, 0.0])
+def test_mixed_types_scales_and_limits(scale):
+    ts = tensors_of([1000, 33, 20001, 4096], [F32, BF16, F16], 2)
+    for limit in (0.0, 1e-3, 1e9):
+        check(ts, limit, scale=scale, out_dtype=F32)
+    check(ts, 1e-3, scale=scale, in_place=True)
+
+
+@pytest.mark.gpu
+def test_magnitudes_whose_squares_leave_single_precision():
+    for std in (1e-30, 1e30):
+        check(tensors_of([5000, 77], [F32, BF16], 3, std=std), 1.0, out_dtype=F32)
+
+
+@pytest.mark.gpu
+def test_a_limit_that_is_met_changes_no_bit():
+    ts = tensors_of([1000, 5], [BF16, F32], 4)
+    before = [t.clone() for t in ts]
+    norm, ws = work()
+    sr.sr_clip_grad_norm(ts, norm_of(ts) * 1.001, norm, ws)
+    assert all(torch.equal(a, b) for a, b in zip(ts, before))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_a_norm_that_is_not_finite_is_reported_and_nothing_is_scaled(bad):
+    ts = tensors_of([10000, 50], [F32], 5)
+    ts[0][7777] = bad
+    before = [t.clone() for t in ts]
+    norm, ws = work()
+    sr.sr_clip_grad_norm(ts, 0.1, norm, ws)
+    assert math.isnan(norm.item()) if math.isnan(bad) else norm.item() == math.inf
+    assert all(torch.equal(a.view(torch.int32), b.view(torch.int32)) for a, b in zip(ts, before))
+    outs = [torch.empty_like(t) for t in ts]
+    sr.sr_clip_grad_norm(sr.tensor_list(ts, outs), 0.1, norm, ws, scale=2.0)
+    assert torch.equal(outs[1], 2 * ts[1])
+
+
+@pytest.mark.gpu
+def test_more_tensors_than_any_launch_takes():
+    """Several thousand small tensors among large ones: the sums of many launches share the workspace."""
+    sizes = [3 + i % 5 for i in range(1500)] + ([20_000_001] + [9] * 130) * 7
+    ts = tensors_of(sizes, [F32], 6)
+    check(ts, 0.3)
+
+
+@pytest.mark.gpu
+def test_nothing_at_all():
+    norm, ws = work()
+    sr.sr_clip_grad_norm([], 1.0, norm, ws)
+    assert norm.item() == 0.0
+    norm.fill_(7.0)
+    sr.sr_grad_norm([torch.empty(0, device="cuda")], norm, ws)
+    assert norm.item() == 0.0
+    check([torch.zeros(100, device="cuda")], 0.0)
+
+
+@pytest.mark.gpu
+def test_one_tensor_of_more_than_2_to_the_31_elements():
+    n = (1 << 31) + 12345
+    t = torch.zeros(n, dtype=BF16, device="cuda")
+    t[5], t[n - 1], t[1 << 31] = 3.0, 4.0, 12.0
+    norm, ws = work()
+    sr.sr_clip_grad_norm([t], 1.0, norm, ws)
+    assert norm.item() == 13.0
+    want = torch.tensor([3 / 13, 4 / 13, 12 / 13], dtype=F32).to(BF16)
+    assert [t[5].item(), t[n - 1].item(), t[1 << 31].item()] == want.tolist() and t[1000].item() == 0.0
+
+
+@pytest.mark.gpu
+def test_repetitions_streams_and_graphs():
+    ts = tensors_of([100000, 33, 9_000_001], [F32, BF16], 8)
+    outs = [torch.empty_like(t) for t in ts]
+    listed = sr.tensor_list(ts, outs)
+    norm, ws = work()
+    sr.sr_clip_grad_norm(listed, 0.5, norm, ws)
+    want, first = norm.clone(), [o.clone() for o in outs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        sr.sr_clip_grad_norm(listed, 0.5, norm, ws)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(norm, want) and all(torch.equal(a, b) for a, b in zip(outs, first))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sr.sr_clip_grad_norm(listed, 0.5, norm, ws)
+    for k in range(3):
+        if k == 2:
+            ts[0].mul_(3.0)
+            sr.sr_clip_grad_norm(listed, 0.5, norm, ws)
+            want, first = norm.clone(), [o.clone() for o in outs]
+        norm.fill_(7.0)
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(norm, want) and all(torch.equal(a, b) for a, b in zip(outs, first))
+
+
+def test_refusals():
+    L, fake = sr.lib(), ctypes.c_void_p(4096)                      # never dereferenced: validation fails first
+    one = lambda data=4096, out=None, n=5, dtype=0, out_dtype=0: (sr.Tensor * 1)(sr.Tensor(data, out, n, dtype, out_dtype))
+    clip = lambda a=one(), n=1, scale=1.0, limit=1.0, norm=fake, ws=fake, size=sr.GRAD_NORM_WORKSPACE: L.sr_clip_grad_norm(
+        a, n, scale, limit, norm, ws, size, None)
+    for r in (clip(a=None), clip(n=-1), clip(scale=math.nan), clip(limit=math.inf), clip(limit=-1.0), clip(norm=None), clip(ws=None),
+              clip(ws=ctypes.c_void_p(4100)), clip(size=sr.GRAD_NORM_WORKSPACE - 1), clip(a=one(data=None)), clip(a=one(data=4098)),
+              clip(a=one(n=-1)), clip(a=one(n=1 << 50)), clip(a=one(dtype=3)), clip(a=one(dtype=1, out=8192, out_dtype=2)),
+              clip(a=one(out=8192, out_dtype=1)), clip(a=one(dtype=1, out=8193, out_dtype=1)), clip(a=one(dtype=1, out=4096, out_dtype=0))):
+        assert r == sr.SR_E_ARG
+    assert L.sr_grad_norm(one(data=None), 1, 1.0, fake, fake, sr.GRAD_NORM_WORKSPACE, None) == sr.SR_E_ARG
+    with pytest.raises(sr.SrError):
+        sr.tensor_list([torch.zeros(3, dtype=torch.float64)])
+    with pytest.raises(sr.SrError):
+        sr.tensor_list([torch.zeros(4, 4).t()])
+    with pytest.raises(sr.SrError):
+        sr.tensor_list([torch.zeros(3)], [torch.zeros(4)])
+    with pytest.raises(sr.SrError):
+        sr.tensor_list([torch.zeros(3)], [])
