@@ -16,6 +16,7 @@ typedef uint32_t raw16_any __attribute__((ext_vector_type(4), aligned(2)));
 template <typename T> struct Elem;
 template <> struct Elem<float> {
     static constexpr int kPerVec = 4;
+    static constexpr uint32_t kMinusInf = 0xff800000u;       // as many as fit 32 bits
     static __device__ __forceinline__ void widen(const raw16 &r, float *x) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(r[i]);
@@ -29,6 +30,7 @@ template <> struct Elem<float> {
 };
 template <> struct Elem<__bf16> {
     static constexpr int kPerVec = 8;
+    static constexpr uint32_t kMinusInf = 0xff80ff80u;
     static __device__ __forceinline__ void widen(const raw16 &r, float *x) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -45,6 +47,7 @@ template <> struct Elem<__bf16> {
 };
 template <> struct Elem<f16_t> {
     static constexpr int kPerVec = 8;
+    static constexpr uint32_t kMinusInf = 0xfc00fc00u;
     typedef f16_t pair __attribute__((ext_vector_type(2)));
     static __device__ __forceinline__ void widen(const raw16 &r, float *x) {
 #pragma unroll
@@ -67,6 +70,9 @@ template <> struct Elem<f16_t> {
 
 template <typename T> __device__ __forceinline__ raw16 load_vec(const T *p) { return *(const raw16_any *)p; }
 template <typename T> __device__ __forceinline__ void store_vec(T *p, raw16 v) { *(raw16_any *)p = v; }
+// the same with the non-temporal hint, for data that the call does not touch again
+template <typename T> __device__ __forceinline__ raw16 load_vec_once(const T *p) { return __builtin_nontemporal_load((const raw16_any *)p); }
+template <typename T> __device__ __forceinline__ void store_vec_once(T *p, raw16 v) { __builtin_nontemporal_store(v, (raw16_any *)p); }
 
 // Elements [at, at + kPerVec) of a run of n, `fill` behind its end
 template <typename T>

@@ -16,25 +16,68 @@
 #include <cmath>
 
 #include "row_vectors.h"
+#include "token_plan.h"
 
 namespace sr {
 namespace {
 
-constexpr float kLog2e = 1.44269504088896341f;
-constexpr int kRowThreads = 256;
 constexpr int kTermThreads = 256;
+constexpr int kSumThreads = 1024;
+constexpr int kParts = 1024;           // parts of rows that the workspace holds
 
-// exp(x) for x <= 0 by the exponential instruction (results below 2^-126 are 0)
+// exp(x) for x <= 0 by the exponential instruction; results below 2^-126 are 0.  The product with log2(e) in single precision is
+// off by 1.3e-8 |x| relative, in one direction: nothing in a probability, but in a sum of exponentials the same for every row, so
+// that a log ratio of 150 tokens was off by 2e-5.  The second form adds what the constant lacks.
+constexpr float kLog2e = 1.44269504088896341f, kLog2eRest = (float)(1.44269504088896341 - (double)1.44269504088896341f);
 __device__ __forceinline__ float exp_neg(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+__device__ __forceinline__ float exp_neg_exact(float x) { return __builtin_amdgcn_exp2f(fmaf(x, kLog2eRest, x * kLog2e)); }
+static_assert(kLog2eRest > 0.f, "-infinity has to stay -infinity");
 
-// running maximum and sum of exponentials relative to it; nothing seen: (-FLT_MAX, 0)
+// Running maximum and sum of exponentials relative to it; nothing seen: (-FLT_MAX, 0).  Products and sums that the compiler might
+// fuse in one kernel and not in another are written as they are meant: a row comes out the same whichever kernel takes it.
 struct RowSum {
     float m, s;
 };
 __device__ __forceinline__ void merge(RowSum &a, float m2, float s2) {
     const float mn = fmaxf(a.m, m2);
-    a.s = a.s * exp_neg(a.m - mn) + s2 * exp_neg(m2 - mn);
+    a.s = fmaf(a.s, exp_neg_exact(a.m - mn), s2 * exp_neg_exact(m2 - mn));
     a.m = mn;
+}
+__device__ __forceinline__ RowSum one_element(float x) {
+    const float m = fmaxf(x, -FLT_MAX);
+    return RowSum{m, exp_neg_exact(x - m)};
+}
+template <int LANES>
+__device__ __forceinline__ void merge_lanes(RowSum &r) {
+#pragma unroll
+    for (int off = LANES / 2; off >= 1; off >>= 1) merge(r, __shfl_xor(r.m, off, 64), __shfl_xor(r.s, off, 64));
+}
+// over the wavefronts of a workgroup, in every lane; s: LDS that nobody reads any more
+template <int WAVES>
+__device__ __forceinline__ RowSum merge_waves(RowSum r, RowSum *s) {
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = r;
+    __syncthreads();
+    r = s[threadIdx.x & (WAVES - 1)];
+    merge_lanes<WAVES>(r);
+    return r;
+}
+// The elements of COUNT vectors, sixteen at a time
+template <typename T, int COUNT>
+__device__ __forceinline__ void add_vectors(RowSum &r, const raw16 *raw) {
+    constexpr int N = Elem<T>::kPerVec, GROUP = 16 / N;
+    static_assert(COUNT % GROUP == 0, "whole groups");
+#pragma unroll
+    for (int k = 0; k < COUNT; k += GROUP) {
+        float v[16], mn = r.m, sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < GROUP; ++j) Elem<T>::widen(raw[k + j], v + j * N);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mn = fmaxf(mn, v[i]);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum += exp_neg_exact(v[i] - mn);
+        r.s = fmaf(r.s, exp_neg_exact(r.m - mn), sum);
+        r.m = mn;
+    }
 }
 
 struct RowArgs {
@@ -45,12 +88,15 @@ struct RowArgs {
     const uint8_t *mask;
     const int32_t *seq_start;
     float *token_logprob;
-    int n_rows, vocab, n_seq, splits, split_elems;
+    int n_rows, vocab, n_seq;
+    int splits, split_elems;           // parts of a row, whole vectors each
     float grad_scale;
     // workspace
     float2 *part;        // [n_rows][splits] (m, s)
+    float2 *whole;       // [n_rows] (m, s)
+    float2 *info;        // [n_rows] policy: weight (0: does not count), advantage
     float *slope;        // [n_rows], grad_scale included
-    float4 *terms;       // [n_rows] policy: surrogate, kl, clipped, weight; pairs ([n_seq / 2]): loss, m > 0, rewards
+    float4 *terms;       // [n_rows] policy: surrogate, kl, clipped, weight; [n_seq / 2] pairs: loss, m > 0, rewards
     int32_t *count;      // [n_seq] counting rows
 };
 
@@ -58,14 +104,14 @@ struct RowArgs {
 constexpr float kNoRow = -1.f;
 
 // the sequence of a row, or -1: the last one that begins at or before it
-__device__ __forceinline__ int sequence_of(const RowArgs &a, int row) {
-    int lo = -1, hi = a.n_seq;
+__device__ __forceinline__ int sequence_of(const int32_t *seq_start, int n_seq, int row) {
+    int lo = -1, hi = n_seq;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (a.seq_start[mid] <= row) lo = mid;
+        if (seq_start[mid] <= row) lo = mid;
         else hi = mid;
     }
-    return lo >= 0 && row < a.seq_start[lo + 1] ? lo : -1;
+    return lo >= 0 && row < seq_start[lo + 1] ? lo : -1;
 }
 __device__ __forceinline__ bool row_counts(const RowArgs &a, int row) {
     return (!a.mask || a.mask[row]) && row >= a.seq_start[0] && row < a.seq_start[a.n_seq];
@@ -76,77 +122,105 @@ __device__ __forceinline__ float logit_of(const RowArgs &a, int row, int v) {
     return v >= 0 && v < a.vocab ? (float)((const T *)a.logits)[row * a.ld_logits + v] : NAN;
 }
 
-// One workgroup per (row, part)
-template <typename T>
-__global__ __launch_bounds__(kRowThreads) void row_stats_kernel(RowArgs a) {
-    constexpr int N = Elem<T>::kPerVec;
-    __shared__ RowSum s_part[kRowThreads / 64];
-    const int row = blockIdx.x / a.splits, part = blockIdx.x % a.splits;
-    float2 *out = a.part + blockIdx.x;
+// ---------------------------------------------------------------------------------------------
+// streaming: (m, s) in one kernel, the gradient in another
+// ---------------------------------------------------------------------------------------------
+// The threads and wavefronts of a workgroup for rows of WAVES wavefronts: four rows of one each
+constexpr int row_block(int waves) { return waves == 1 ? 256 : 64 * waves; }
+
+// WAVES wavefronts per (row, part).  Four vectors in flight per thread.
+template <typename T, int WAVES>
+__global__ __launch_bounds__(row_block(WAVES)) void row_stats_kernel(RowArgs a) {
+    constexpr int N = Elem<T>::kPerVec, LANES = 64 * WAVES, DEPTH = 4;
+    __shared__ RowSum s_part[WAVES];
+    const int unit = WAVES == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+    const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+    if (unit >= a.n_rows * a.splits) return;                 // wavefronts without a barrier to come, if any
+    const int row = unit / a.splits, part = unit - row * a.splits;
+    float2 *out = a.part + unit;
     if (!row_counts(a, row)) {
-        if (threadIdx.x == 0) *out = make_float2(0.f, kNoRow);
+        if (t == 0) *out = make_float2(0.f, kNoRow);
         return;
     }
     const T *x = (const T *)a.logits + row * a.ld_logits;
-    const int from = part * a.split_elems, to = min(from + a.split_elems, a.vocab);
+    const int from = part * a.split_elems, to = min(from + a.split_elems, a.vocab), full = from + (to - from) / N * N;
     RowSum r = {-FLT_MAX, 0.f};
-    for (int e = from + (int)threadIdx.x * N; e < to; e += kRowThreads * N) {
-        float v[N];
-        load_widened(x, e, to, -INFINITY, v);
-        float mn = r.m;
+    if (full + t < to) r = one_element((float)x[full + t]);
+    raw16 raw[DEPTH];
+    int e = from + t * N;
+    for (; e + (DEPTH - 1) * LANES * N < full; e += DEPTH * LANES * N) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) mn = fmaxf(mn, v[i]);
-        r.s *= exp_neg(r.m - mn);
-#pragma unroll
-        for (int i = 0; i < N; ++i) r.s += exp_neg(v[i] - mn);
-        r.m = mn;
+        for (int j = 0; j < DEPTH; ++j) raw[j] = load_vec(x + e + j * LANES * N);
+        add_vectors<T, DEPTH>(r, raw);
     }
+    if (e < full) {
 #pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) merge(r, __shfl_xor(r.m, off, 64), __shfl_xor(r.s, off, 64));
-    if ((threadIdx.x & 63) == 0) s_part[threadIdx.x >> 6] = r;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < kRowThreads / 64; ++w) merge(r, s_part[w].m, s_part[w].s);
-        *out = make_float2(r.m, r.s);
+        for (int j = 0; j < DEPTH; ++j)
+            raw[j] = e + j * LANES * N < full ? load_vec(x + e + j * LANES * N) : raw16(Elem<T>::kMinusInf);
+        add_vectors<T, DEPTH>(r, raw);
     }
+    merge_lanes<64>(r);
+    if (WAVES > 1) r = merge_waves<WAVES>(r, s_part);
+    if (t == 0) *out = make_float2(r.m, r.s);
 }
 
 // (m, s) of a row from its parts, in their order
 __device__ __forceinline__ RowSum whole_row(const RowArgs &a, int row) {
     const float2 *p = a.part + (size_t)row * a.splits;
     RowSum r = {p[0].x, p[0].y};
+    if (r.s == kNoRow) return r;
     for (int k = 1; k < a.splits; ++k) merge(r, p[k].x, p[k].y);
     return r;
 }
 
-// One workgroup per (row, part), the parts of row_stats_kernel.  In place: a thread reads what it then writes.
+// The gradient of the elements of a vector; the row's token is its element number `hot`, if that is one
 template <typename T>
-__global__ __launch_bounds__(kRowThreads) void logit_grad_kernel(RowArgs a) {
+__device__ __forceinline__ raw16 gradient(const raw16 &raw, int hot, float m, float factor, float slope) {
     constexpr int N = Elem<T>::kPerVec;
-    const int row = blockIdx.x / a.splits, part = blockIdx.x % a.splits;
+    float v[N];
+    Elem<T>::widen(raw, v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = factor * exp_neg(v[i] - m);
+    if ((unsigned)hot < N)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (hot == i) v[i] += slope;
+    return Elem<T>::narrow(v);
+}
+
+// The parts of row_stats_kernel.  In place: a thread reads what it then writes.
+template <typename T, int WAVES>
+__global__ __launch_bounds__(row_block(WAVES)) void logit_grad_kernel(RowArgs a) {
+    constexpr int N = Elem<T>::kPerVec, LANES = 64 * WAVES, DEPTH = 4;
+    const int unit = WAVES == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+    const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+    if (unit >= a.n_rows * a.splits) return;
+    const int row = unit / a.splits, part = unit - row * a.splits;
     const T *x = (const T *)a.logits + row * a.ld_logits;
     T *g = (T *)a.grad + row * a.ld_grad;
-    const int from = part * a.split_elems, to = min(from + a.split_elems, a.vocab);
-    const bool counts = a.part[(size_t)row * a.splits].y != kNoRow;
-    if (!counts) {
-        const float zero[N] = {};
-        for (int e = from + (int)threadIdx.x * N; e < to; e += kRowThreads * N) store_narrowed(g, e, to, zero);
+    const int from = part * a.split_elems, to = min(from + a.split_elems, a.vocab), full = from + (to - from) / N * N;
+    const float2 whole = a.whole[row];
+    if (whole.y == kNoRow) {
+        for (int e = from + t * N; e < full; e += LANES * N) store_vec_once(g + e, raw16(0));
+        if (full + t < to) g[full + t] = (T)0.f;
         return;
     }
-    const RowSum r = whole_row(a, row);
-    const float slope = a.slope[row], f = -slope / r.s;
+    const float m = whole.x, slope = a.slope[row], factor = -slope / whole.y;
     const int target = a.targets[row];
-    for (int e = from + (int)threadIdx.x * N; e < to; e += kRowThreads * N) {
-        float v[N];
-        load_widened(x, e, to, -INFINITY, v);
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = f * exp_neg(v[i] - r.m);
-        if ((unsigned)(target - e) < N)
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (target == e + i) v[i] += slope;
-        store_narrowed(g, e, to, v);
+    if (full + t < to) {
+        const float v = factor * exp_neg((float)x[full + t] - m);
+        g[full + t] = (T)(target == full + t ? v + slope : v);
     }
+    raw16 raw[DEPTH];
+    int e = from + t * N;
+    for (; e + (DEPTH - 1) * LANES * N < full; e += DEPTH * LANES * N) {
+#pragma unroll
+        for (int j = 0; j < DEPTH; ++j) raw[j] = load_vec_once(x + e + j * LANES * N);
+#pragma unroll
+        for (int j = 0; j < DEPTH; ++j)
+            store_vec_once(g + e + j * LANES * N, gradient<T>(raw[j], target - e - j * LANES * N, m, factor, slope));
+    }
+    for (; e < full; e += LANES * N) store_vec_once(g + e, gradient<T>(load_vec_once(x + e), target - e, m, factor, slope));
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -160,82 +234,233 @@ struct PolicyArgs {
 };
 
 // counting rows of a sequence, a wavefront each
+__device__ __forceinline__ int count_rows(const RowArgs &a, int seq, int lane) {
+    const int from = max(a.seq_start[seq], 0), to = min(a.seq_start[seq + 1], a.n_rows);
+    if (!a.mask) return max(to - from, 0);
+    int n = 0;
+    for (int r = from + lane; r < to; r += 64) n += a.mask[r] != 0;
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) n += __shfl_xor(n, off, 64);
+    return n;
+}
 __global__ __launch_bounds__(256) void seq_count_kernel(RowArgs a) {
     const int seq = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (seq >= a.n_seq) return;
-    const int from = max(a.seq_start[seq], 0), to = min(a.seq_start[seq + 1], a.n_rows);
-    int n = 0;
-    if (!a.mask) {
-        n = max(to - from, 0);
-    } else {
-        for (int r = from + lane; r < to; r += 64) n += a.mask[r] != 0;
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) n += __shfl_xor(n, off, 64);
-    }
+    const int n = count_rows(a, seq, lane);
     if (lane == 0) a.count[seq] = n;
+}
+
+// Weight and advantage of `row`.  rows, used: counting rows of all sequences, and sequences that have any
+__device__ __forceinline__ float2 row_info(const RowArgs &a, const PolicyArgs &p, int row, int rows, int used) {
+    const int seq = !a.mask || a.mask[row] ? sequence_of(a.seq_start, a.n_seq, row) : -1;
+    if (seq < 0) return make_float2(0.f, 0.f);
+    const float w = p.reduce == SR_MEAN_TOKENS      ? 1.f / (float)rows
+                    : p.reduce == SR_MEAN_SEQUENCES ? 1.f / ((float)used * (float)a.count[seq])
+                                                    : 1.f / (float)used;
+    return make_float2(w, p.advantages[seq]);
+}
+
+// Sums of count[] and of its non-zero entries over all sequences, by every workgroup for itself.  s: two ints of LDS
+template <int THREADS>
+__device__ __forceinline__ void count_totals(const RowArgs &a, int *s) {
+    if (threadIdx.x < 2) s[threadIdx.x] = 0;
+    __syncthreads();
+    int rows = 0, used = 0;
+    for (int i = threadIdx.x; i < a.n_seq; i += THREADS) {
+        rows += a.count[i];
+        used += a.count[i] > 0;
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) {
+        rows += __shfl_xor(rows, off, 64);
+        used += __shfl_xor(used, off, 64);
+    }
+    if ((threadIdx.x & 63) == 0) {
+        atomicAdd(&s[0], rows);                              // whole numbers: the order does not matter
+        atomicAdd(&s[1], used);
+    }
+    __syncthreads();
+}
+
+__global__ __launch_bounds__(kTermThreads) void row_info_kernel(RowArgs a, PolicyArgs p) {
+    __shared__ int s[2];
+    count_totals<kTermThreads>(a, s);
+    const int row = blockIdx.x * kTermThreads + threadIdx.x;
+    if (row < a.n_rows) a.info[row] = row_info(a, p, row, s[0], s[1]);
+}
+
+// A counting row's slope, and its terms of the loss
+__device__ __forceinline__ float policy_row(const PolicyArgs &p, float2 info, float logprob, float old_logprob, float ref_logprob,
+                                            float4 *term) {
+    const float A = info.y, ratio = expf(logprob - old_logprob);
+    const float plain = ratio * A, clipped = fminf(fmaxf(ratio, 1.f - p.clip_low), 1.f + p.clip_high) * A;
+    const bool out = plain > clipped;
+    float slope = out ? 0.f : -plain;
+    *term = make_float4(out ? clipped : plain, 0.f, out ? 1.f : 0.f, info.x);
+    if (p.ref_logprob) {
+        const float d = ref_logprob - logprob, e = expm1f(d);
+        term->y = e - d;
+        if (p.kl_coef != 0.f) slope = fmaf(-p.kl_coef, e, slope);
+    }
+    return slope * info.x;
+}
+
+struct PolicySums {
+    double surrogate = 0.0, kl = 0.0, out = 0.0;
+    __device__ __forceinline__ void add(float4 t) {
+        if (t.w == 0.f) return;                              // a row that does not count
+        surrogate += (double)t.w * (double)t.x;
+        kl += (double)t.w * (double)t.y;
+        out += (double)t.w * (double)t.z;
+    }
+    // over the workgroup; s: kSumThreads / 64 doubles of LDS
+    __device__ __forceinline__ void finish(const PolicyArgs &p, double *s) {
+        surrogate = block_sum<kSumThreads / 64>(surrogate, s);
+        kl = block_sum<kSumThreads / 64>(kl, s);
+        out = block_sum<kSumThreads / 64>(out, s);
+        if (threadIdx.x != 0) return;
+        p.stats[0] = (float)((p.kl_coef != 0.f ? (double)p.kl_coef * kl : 0.0) - surrogate);
+        p.stats[1] = (float)surrogate;
+        p.stats[2] = (float)kl;
+        p.stats[3] = (float)out;
+    }
+};
+
+// What lies between a row's (m, s) and its gradient
+template <typename T>
+__device__ __forceinline__ float4 finish_row(const RowArgs &a, const PolicyArgs &p, int row, float2 info) {
+    float logprob = 0.f, slope = 0.f;
+    float4 term = make_float4(0.f, 0.f, 0.f, 0.f);
+    const RowSum r = whole_row(a, row);
+    if (info.x != 0.f) {
+        logprob = (logit_of<T>(a, row, a.targets[row]) - r.m) - logf(r.s);
+        slope = policy_row(p, info, logprob, p.old_logprob[row], p.ref_logprob ? p.ref_logprob[row] : 0.f, &term) * a.grad_scale;
+    }
+    if (a.token_logprob) a.token_logprob[row] = logprob;
+    a.slope[row] = slope;
+    a.whole[row] = make_float2(r.m, r.s);
+    return term;
 }
 
 template <typename T>
 __global__ __launch_bounds__(kTermThreads) void policy_rows_kernel(RowArgs a, PolicyArgs p) {
-    __shared__ int s_rows, s_used;
-    if (threadIdx.x == 0) s_rows = s_used = 0;
-    __syncthreads();
-    int rows = 0, used = 0;
-    for (int i = threadIdx.x; i < a.n_seq; i += kTermThreads) {
-        rows += a.count[i];
-        used += a.count[i] > 0;
-    }
-    atomicAdd(&s_rows, rows);             // whole numbers: the order does not matter
-    atomicAdd(&s_used, used);
-    __syncthreads();
     const int row = blockIdx.x * kTermThreads + threadIdx.x;
-    if (row >= a.n_rows) return;
-    float logprob = 0.f, slope = 0.f;
-    float4 term = make_float4(0.f, 0.f, 0.f, 0.f);
-    const RowSum r = whole_row(a, row);
-    const int seq = r.s == kNoRow ? -1 : sequence_of(a, row);
-    if (seq >= 0) {
-        logprob = (logit_of<T>(a, row, a.targets[row]) - r.m) - logf(r.s);
-        const float w = p.reduce == SR_MEAN_TOKENS      ? 1.f / (float)s_rows
-                        : p.reduce == SR_MEAN_SEQUENCES ? 1.f / ((float)s_used * (float)a.count[seq])
-                                                        : 1.f / (float)s_used;
-        const float A = p.advantages[seq], ratio = expf(logprob - p.old_logprob[row]);
-        const float plain = ratio * A, clipped = fminf(fmaxf(ratio, 1.f - p.clip_low), 1.f + p.clip_high) * A;
-        const bool out = plain > clipped;
-        slope = out ? 0.f : -plain;
-        term = make_float4(out ? clipped : plain, 0.f, out ? 1.f : 0.f, w);
-        if (p.ref_logprob) {
-            const float d = p.ref_logprob[row] - logprob, e = expm1f(d);
-            term.y = e - d;
-            if (p.kl_coef != 0.f) slope -= p.kl_coef * e;
-        }
-        slope *= w * a.grad_scale;
-    }
-    if (a.token_logprob) a.token_logprob[row] = logprob;
-    a.slope[row] = slope;
-    a.terms[row] = term;
+    if (row < a.n_rows) a.terms[row] = finish_row<T>(a, p, row, a.info[row]);
 }
-
-constexpr int kSumThreads = 1024;
-
 __global__ __launch_bounds__(kSumThreads) void policy_sum_kernel(RowArgs a, PolicyArgs p) {
     __shared__ double s[kSumThreads / 64];
-    double sur = 0.0, kl = 0.0, out = 0.0;
-    for (int i = threadIdx.x; i < a.n_rows; i += kSumThreads) {
-        const float4 t = a.terms[i];
-        if (t.w == 0.f) continue;         // a row that does not count
-        sur += (double)t.w * (double)t.x;
-        kl += (double)t.w * (double)t.y;
-        out += (double)t.w * (double)t.z;
+    PolicySums sums;
+    for (int i = threadIdx.x; i < a.n_rows; i += kSumThreads) sums.add(a.terms[i]);
+    sums.finish(p, s);
+}
+
+// The four kernels between row_stats_kernel and logit_grad_kernel by one workgroup: few rows
+template <typename T>
+__global__ __launch_bounds__(kSumThreads) void policy_small_kernel(RowArgs a, PolicyArgs p) {
+    __shared__ double s[kSumThreads / 64];
+    __shared__ int s_totals[2];
+    for (int seq = threadIdx.x >> 6; seq < a.n_seq; seq += kSumThreads / 64) {
+        const int n = count_rows(a, seq, threadIdx.x & 63);
+        if ((threadIdx.x & 63) == 0) a.count[seq] = n;
     }
-    sur = block_sum<kSumThreads / 64>(sur, s);
-    kl = block_sum<kSumThreads / 64>(kl, s);
-    out = block_sum<kSumThreads / 64>(out, s);
-    if (threadIdx.x == 0) {
-        p.stats[0] = (float)((p.kl_coef != 0.f ? (double)p.kl_coef * kl : 0.0) - sur);
-        p.stats[1] = (float)sur;
-        p.stats[2] = (float)kl;
-        p.stats[3] = (float)out;
+    __syncthreads();
+    count_totals<kSumThreads>(a, s_totals);
+    PolicySums sums;
+    for (int row = threadIdx.x; row < a.n_rows; row += kSumThreads)
+        sums.add(finish_row<T>(a, p, row, row_info(a, p, row, s_totals[0], s_totals[1])));
+    sums.finish(p, s);
+}
+
+// ---------------------------------------------------------------------------------------------
+// policy loss with its gradient, a row held in registers between the two
+// ---------------------------------------------------------------------------------------------
+// WAVES wavefronts take a row, NV vectors a thread: the row is read once and written once.  NV - kGroup vectors of every thread lie
+// inside the row, the last kGroup may not.  Rows of one wavefront: four to a workgroup.  LOOP: a workgroup takes every
+// gridDim-th row, and asks for the next row's vectors as the gradient's leave the registers.
+template <typename T, int WAVES, int NV, bool LOOP>
+__global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowArgs a, PolicyArgs p) {
+    constexpr int N = Elem<T>::kPerVec, LANES = 64 * WAVES, kGroup = 16 / N, SURE = NV - kGroup;
+    __shared__ RowSum s_part[2][WAVES];
+    const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+    int row = WAVES == 1 ? __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)) : blockIdx.x;
+    if (row >= a.n_rows) return;
+    const int full = a.vocab / N * N, tail = full + t;
+    raw16 raw[NV];
+    T last;                                                  // lanes behind the last whole vector: an element of the rest
+    int at = t * N;                                          // the thread's element of the row's first LANES vectors
+    auto fetch = [&](int j, const T *x) __attribute__((always_inline)) {
+        raw[j] = raw16(Elem<T>::kMinusInf);
+        if (j < SURE || at + j * LANES * N < full) raw[j] = load_vec_once(x + j * LANES * N + (unsigned)at);
+    };
+    auto put = [&](int j, T *g, raw16 v) __attribute__((always_inline)) {
+        if (j < SURE || at + j * LANES * N < full) store_vec_once(g + j * LANES * N + (unsigned)at, v);
+    };
+    // the first counting row from `row` on; those before it get their zeros
+    auto counting = [&](int row, float2 *info) __attribute__((always_inline)) {
+        for (; row < a.n_rows; row += gridDim.x) {
+            *info = a.info[row];
+            if (info->x != 0.f) break;
+            T *g = (T *)a.grad + row * a.ld_grad;
+            for (int j = 0; j < NV; ++j) put(j, g, raw16(0));
+            if (tail < a.vocab) g[tail] = (T)0.f;
+            if (t == 0) {
+                if (a.token_logprob) a.token_logprob[row] = 0.f;
+                a.terms[row] = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            if (!LOOP) return a.n_rows;
+        }
+        return row;
+    };
+    float2 info;
+    row = counting(row, &info);
+    if (row >= a.n_rows) return;
+    const T *x = (const T *)a.logits + row * a.ld_logits;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) fetch(j, x);
+    if (tail < a.vocab) last = x[tail];
+    for (int turn = 0;; turn ^= 1) {
+        asm volatile("" : "+v"(at));                         // or the loop keeps every vector's address and index in registers
+        T *g = (T *)a.grad + row * a.ld_grad;
+        const int target = a.targets[row];
+        const float chosen = logit_of<T>(a, row, target), old_logprob = p.old_logprob[row];
+        const float ref_logprob = p.ref_logprob ? p.ref_logprob[row] : 0.f;
+        float2 next_info;
+        const int next = LOOP ? counting(row + gridDim.x, &next_info) : a.n_rows;
+        RowSum r = {-FLT_MAX, 0.f};
+        if (tail < a.vocab) r = one_element((float)last);
+        add_vectors<T, NV>(r, raw);
+        // the gradient widens the vectors again: the widened ones would not fit the registers
+#pragma unroll
+        for (int j = 0; j < NV; ++j) asm volatile("" : "+v"(raw[j]));
+        merge_lanes<64>(r);
+        // the half of s_part that the row before used may still be read by wavefronts behind this barrier, but not the other
+        if (WAVES > 1) r = merge_waves<WAVES>(r, s_part[turn]);
+        const float logprob = (chosen - r.m) - logf(r.s);
+        float4 term;
+        const float slope = policy_row(p, info, logprob, old_logprob, ref_logprob, &term) * a.grad_scale, factor = -slope / r.s;
+        if (t == 0) {
+            if (a.token_logprob) a.token_logprob[row] = logprob;
+            a.terms[row] = term;
+        }
+        if (tail < a.vocab) {
+            const float v = factor * exp_neg((float)last - r.m);
+            g[tail] = (T)(target == tail ? v + slope : v);
+        }
+        if (next >= a.n_rows) {                              // the same for every wavefront of the row
+#pragma unroll
+            for (int j = 0; j < NV; ++j) put(j, g, gradient<T>(raw[j], target - at - j * LANES * N, r.m, factor, slope));
+            return;
+        }
+        x = (const T *)a.logits + next * a.ld_logits;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            put(j, g, gradient<T>(raw[j], target - at - j * LANES * N, r.m, factor, slope));
+            fetch(j, x);
+            __builtin_amdgcn_sched_barrier(0);               // one vector's widened values at a time
+        }
+        if (tail < a.vocab) last = x[tail];
+        row = next;
+        info = next_info;
     }
 }
 
@@ -260,12 +485,14 @@ __global__ __launch_bounds__(kTermThreads) void pair_kernel(RowArgs a, PairArgs 
         double acc = 0.0;
         for (int row = from + threadIdx.x; row < to; row += kTermThreads) {
             const RowSum r = whole_row(a, row);
-            float logprob = 0.f;
+            double logprob = 0.0;
             if (r.s != kNoRow) {
-                logprob = (logit_of<T>(a, row, a.targets[row]) - r.m) - logf(r.s);
-                acc += (double)logprob - (p.ref_logprob ? (double)p.ref_logprob[row] : 0.0);
+                // l in double: a pair adds hundreds of them, and rounds to single precision once
+                logprob = (double)(logit_of<T>(a, row, a.targets[row]) - r.m) - log((double)r.s);
+                acc += logprob - (p.ref_logprob ? (double)p.ref_logprob[row] : 0.0);
             }
-            if (a.token_logprob) a.token_logprob[row] = logprob;
+            a.whole[row] = make_float2(r.m, r.s);
+            if (a.token_logprob) a.token_logprob[row] = (float)logprob;
         }
         ratio[k] = block_sum<kTermThreads / 64>(acc, s);
     }
@@ -284,12 +511,14 @@ __global__ __launch_bounds__(kTermThreads) void pair_kernel(RowArgs a, PairArgs 
     __syncthreads();
     const int start = max(a.seq_start[2 * pair], 0), mid = a.seq_start[2 * pair + 1], end = min(a.seq_start[2 * pair + 2], a.n_rows);
     for (int row = start + threadIdx.x; row < end; row += kTermThreads) a.slope[row] = row < mid ? s_slope : -s_slope;
-    if (a.token_logprob) {
-        if (pair == 0)
-            for (int row = threadIdx.x; row < min(start, a.n_rows); row += kTermThreads) a.token_logprob[row] = 0.f;
-        if (pair == pairs - 1)
-            for (int row = max(a.seq_start[a.n_seq], 0) + threadIdx.x; row < a.n_rows; row += kTermThreads) a.token_logprob[row] = 0.f;
-    }
+    auto outside = [&](int row) {
+        a.whole[row] = make_float2(0.f, kNoRow);
+        if (a.token_logprob) a.token_logprob[row] = 0.f;
+    };
+    if (pair == 0)
+        for (int row = threadIdx.x; row < min(start, a.n_rows); row += kTermThreads) outside(row);
+    if (pair == pairs - 1)
+        for (int row = max(a.seq_start[a.n_seq], 0) + threadIdx.x; row < a.n_rows; row += kTermThreads) outside(row);
 }
 
 __global__ __launch_bounds__(kSumThreads) void pair_sum_kernel(RowArgs a, PairArgs p) {
@@ -324,8 +553,9 @@ int check_rows(const sr_token_rows *x, const void *workspace, size_t bytes) {
     return x->grad == x->logits && x->ld_grad != x->ld_logits ? SR_E_ARG : SR_OK;
 }
 
-// SR_TOKEN_LOSS_WORKSPACE: 40 bytes a row and 16 a sequence used here, the constant part for the parts of few rows
-RowArgs row_args(const sr_token_rows *x, void *workspace) {
+// SR_TOKEN_LOSS_WORKSPACE: of every row 16 bytes of terms, 8 each of (m, s) as parts, whole, and of weight and advantage, 4 of slope;
+// of every sequence 16 (a pair's terms) and 4; the constant part for more parts than rows
+RowArgs row_args(const sr_token_rows *x, const RowPlan &plan, void *workspace) {
     RowArgs a{};
     a.logits = x->logits;
     a.grad = x->grad;
@@ -339,16 +569,21 @@ RowArgs row_args(const sr_token_rows *x, void *workspace) {
     a.vocab = x->vocab;
     a.n_seq = x->n_seq;
     a.grad_scale = x->grad_scale;
+    const size_t rows = (size_t)x->n_rows;
     char *w = (char *)workspace;
-    a.terms = (float4 *)w;                               // 16 bytes a row, or a pair
-    w += 16 * ((size_t)x->n_rows + x->n_seq);
-    a.part = (float2 *)w;                                // 8 bytes a row, or 48 KiB
-    w += 8 * (size_t)x->n_rows + 49152;
-    a.slope = (float *)w;
-    w += 4 * (size_t)x->n_rows;
-    a.count = (int32_t *)w;
-    a.splits = 1;
-    a.split_elems = x->vocab;
+    auto take = [&](size_t bytes) {
+        char *p = w;
+        w += bytes;
+        return p;
+    };
+    a.terms = (float4 *)take(16 * (rows + x->n_seq));
+    a.part = (float2 *)take(8 * (rows > kParts ? rows : kParts));
+    a.whole = (float2 *)take(8 * rows);
+    a.info = (float2 *)take(8 * rows);
+    a.slope = (float *)take(4 * rows);
+    a.count = (int32_t *)take(4 * (size_t)x->n_seq);
+    a.splits = plan.parts;
+    a.split_elems = plan.elems;
     return a;
 }
 
@@ -360,43 +595,87 @@ int with_type(int dtype, F &&f) {
 }
 
 template <typename T>
-int launch_row_stats(const RowArgs &a, hipStream_t stream) {
-    row_stats_kernel<T><<<dim3((unsigned)(a.n_rows * a.splits)), dim3(kRowThreads), 0, stream>>>(a);
+int launch_row_stats(const RowArgs &a, int waves, hipStream_t stream) {
+    const int units = a.n_rows * a.splits;
+    if (waves == 1) row_stats_kernel<T, 1><<<dim3(ceil_div(units, 4)), dim3(row_block(1)), 0, stream>>>(a);
+    else if (waves == 4) row_stats_kernel<T, 4><<<dim3(units), dim3(row_block(4)), 0, stream>>>(a);
+    else row_stats_kernel<T, 16><<<dim3(units), dim3(row_block(16)), 0, stream>>>(a);
     SR_HIP(hipGetLastError());
     return SR_OK;
 }
 template <typename T>
-int launch_logit_grad(const RowArgs &a, hipStream_t stream) {
-    logit_grad_kernel<T><<<dim3((unsigned)(a.n_rows * a.splits)), dim3(kRowThreads), 0, stream>>>(a);
+int launch_logit_grad(const RowArgs &a, int waves, hipStream_t stream) {
+    const int units = a.n_rows * a.splits;
+    if (waves == 1) logit_grad_kernel<T, 1><<<dim3(ceil_div(units, 4)), dim3(row_block(1)), 0, stream>>>(a);
+    else logit_grad_kernel<T, 4><<<dim3(units), dim3(row_block(4)), 0, stream>>>(a);
     SR_HIP(hipGetLastError());
     return SR_OK;
 }
 
+int launch_row_info(const RowArgs &a, const PolicyArgs &p, hipStream_t stream) {
+    seq_count_kernel<<<dim3(ceil_div(a.n_seq, 4)), dim3(256), 0, stream>>>(a);
+    SR_HIP(hipGetLastError());
+    row_info_kernel<<<dim3(ceil_div(a.n_rows, kTermThreads)), dim3(kTermThreads), 0, stream>>>(a, p);
+    SR_HIP(hipGetLastError());
+    return SR_OK;
+}
+
+// vecs: vectors of a thread; the kernels have whole groups of them
+template <typename T, int WAVES, int NV>
+int launch_resident(const RowArgs &a, const PolicyArgs &p, int vecs, hipStream_t stream) {
+    constexpr int kGroup = 16 / Elem<T>::kPerVec;
+    constexpr bool LOOP = WAVES == 16;
+    if constexpr (NV + kGroup <= (WAVES == 1 ? kMostOneWave : kMostResident))
+        if (vecs > NV) return launch_resident<T, WAVES, NV + kGroup>(a, p, vecs, stream);
+    const int blocks = WAVES == 1 ? ceil_div(a.n_rows, 4) : LOOP && a.n_rows > 256 ? 256 : a.n_rows;
+    policy_resident_kernel<T, WAVES, NV, LOOP><<<dim3(blocks), dim3(row_block(WAVES)), 0, stream>>>(a, p);
+    SR_HIP(hipGetLastError());
+    return SR_OK;
+}
+template <typename T>
+int launch_resident(const RowArgs &a, const PolicyArgs &p, int waves, int vecs, hipStream_t stream) {
+    if (waves == 1) return launch_resident<T, 1, 16 / Elem<T>::kPerVec>(a, p, vecs, stream);
+    if (waves == 4) return launch_resident<T, 4, 4>(a, p, vecs, stream);
+    return launch_resident<T, 16, 8>(a, p, vecs, stream);
+}
+
 int policy_loss(const sr_token_rows *x, const PolicyArgs &p, void *workspace, hipStream_t stream) {
-    RowArgs a = row_args(x, workspace);
-    if (x->n_rows > 0)
+    const RowPlan plan = plan_policy_rows(x->n_rows, x->vocab, x->dtype == SR_F32 ? 4 : 2);
+    const RowArgs a = row_args(x, plan, workspace);
+    const bool small = a.n_rows <= kSumThreads && !(a.grad && plan.resident);
+    if (a.n_rows > 0)
         SR_TRY(with_type(x->dtype, [&](auto *t) -> int {
             typedef std::remove_pointer_t<decltype(t)> T;
-            SR_TRY(launch_row_stats<T>(a, stream));
-            seq_count_kernel<<<dim3((a.n_seq + 3) / 4), dim3(256), 0, stream>>>(a);
-            SR_HIP(hipGetLastError());
-            policy_rows_kernel<T><<<dim3((a.n_rows + kTermThreads - 1) / kTermThreads), dim3(kTermThreads), 0, stream>>>(a, p);
-            SR_HIP(hipGetLastError());
-            return a.grad ? launch_logit_grad<T>(a, stream) : SR_OK;
+            if (a.grad && plan.resident) {
+                SR_TRY(launch_row_info(a, p, stream));
+                return launch_resident<T>(a, p, plan.waves, plan.resident, stream);
+            }
+            SR_TRY(launch_row_stats<T>(a, plan.waves, stream));
+            if (small) {
+                policy_small_kernel<T><<<dim3(1), dim3(kSumThreads), 0, stream>>>(a, p);
+                SR_HIP(hipGetLastError());
+            } else {
+                SR_TRY(launch_row_info(a, p, stream));
+                policy_rows_kernel<T><<<dim3(ceil_div(a.n_rows, kTermThreads)), dim3(kTermThreads), 0, stream>>>(a, p);
+                SR_HIP(hipGetLastError());
+            }
+            return a.grad ? launch_logit_grad<T>(a, plan.waves, stream) : SR_OK;
         }));
+    if (a.n_rows > 0 && small) return SR_OK;
     policy_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(a, p);
     SR_HIP(hipGetLastError());
     return SR_OK;
 }
 
 int preference_loss(const sr_token_rows *x, const PairArgs &p, void *workspace, hipStream_t stream) {
-    RowArgs a = row_args(x, workspace);
+    const RowPlan plan = plan_streamed_rows(x->n_rows, x->vocab, x->dtype == SR_F32 ? 4 : 2);
+    const RowArgs a = row_args(x, plan, workspace);
     return with_type(x->dtype, [&](auto *t) -> int {
         typedef std::remove_pointer_t<decltype(t)> T;
-        if (a.n_rows > 0) SR_TRY(launch_row_stats<T>(a, stream));
+        if (a.n_rows > 0) SR_TRY(launch_row_stats<T>(a, plan.waves, stream));
         pair_kernel<T><<<dim3(a.n_seq / 2), dim3(kTermThreads), 0, stream>>>(a, p);
         SR_HIP(hipGetLastError());
-        if (a.n_rows > 0 && a.grad) SR_TRY(launch_logit_grad<T>(a, stream));
+        if (a.n_rows > 0 && a.grad) SR_TRY(launch_logit_grad<T>(a, plan.waves, stream));
         pair_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(a, p);
         SR_HIP(hipGetLastError());
         return SR_OK;
