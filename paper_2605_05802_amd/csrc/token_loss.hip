@@ -77,6 +77,7 @@ __device__ __forceinline__ void add_vectors(RowSum &r, const raw16 *raw) {
         for (int i = 0; i < 16; ++i) sum += exp_neg_exact(v[i] - mn);
         r.s = fmaf(r.s, exp_neg_exact(r.m - mn), sum);
         r.m = mn;
+        __builtin_amdgcn_sched_barrier(0);                   // one group's widened values at a time
     }
 }
 
@@ -175,9 +176,10 @@ __device__ __forceinline__ RowSum whole_row(const RowArgs &a, int row) {
 
 // The gradient of the elements of a vector; the row's token is its element number `hot`, if that is one
 template <typename T>
-__device__ __forceinline__ raw16 gradient(const raw16 &raw, int hot, float m, float factor, float slope) {
+__device__ __forceinline__ raw16 gradient(raw16 raw, int hot, float m, float factor, float slope) {
     constexpr int N = Elem<T>::kPerVec;
     float v[N];
+    asm volatile("" : "+v"(raw));                            // widened again: what the maximum widened would not fit the registers
     Elem<T>::widen(raw, v);
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = factor * exp_neg(v[i] - m);
@@ -418,6 +420,9 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
 #pragma unroll
     for (int j = 0; j < NV; ++j) fetch(j, x);
     if (tail < a.vocab) last = x[tail];
+    RowSum r = {-FLT_MAX, 0.f};
+    if (tail < a.vocab) r = one_element((float)last);
+    add_vectors<T, NV>(r, raw);
     for (int turn = 0;; turn ^= 1) {
         asm volatile("" : "+v"(at));                         // or the loop keeps every vector's address and index in registers
         T *g = (T *)a.grad + row * a.ld_grad;
@@ -426,16 +431,10 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
         const float ref_logprob = p.ref_logprob ? p.ref_logprob[row] : 0.f;
         float2 next_info;
         const int next = LOOP ? counting(row + gridDim.x, &next_info) : a.n_rows;
-        RowSum r = {-FLT_MAX, 0.f};
-        if (tail < a.vocab) r = one_element((float)last);
-        add_vectors<T, NV>(r, raw);
-        // the gradient widens the vectors again: the widened ones would not fit the registers
-#pragma unroll
-        for (int j = 0; j < NV; ++j) asm volatile("" : "+v"(raw[j]));
         merge_lanes<64>(r);
         // the half of s_part that the row before used may still be read by wavefronts behind this barrier, but not the other
         if (WAVES > 1) r = merge_waves<WAVES>(r, s_part[turn]);
-        const float logprob = (chosen - r.m) - logf(r.s);
+        const float logprob = (chosen - r.m) - logf(r.s), m = r.m;
         float4 term;
         const float slope = policy_row(p, info, logprob, old_logprob, ref_logprob, &term) * a.grad_scale, factor = -slope / r.s;
         if (t == 0) {
@@ -443,22 +442,33 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
             a.terms[row] = term;
         }
         if (tail < a.vocab) {
-            const float v = factor * exp_neg((float)last - r.m);
+            const float v = factor * exp_neg((float)last - m);
             g[tail] = (T)(target == tail ? v + slope : v);
         }
         if (next >= a.n_rows) {                              // the same for every wavefront of the row
 #pragma unroll
-            for (int j = 0; j < NV; ++j) put(j, g, gradient<T>(raw[j], target - at - j * LANES * N, r.m, factor, slope));
+            for (int j = 0; j < NV; ++j) put(j, g, gradient<T>(raw[j], target - at - j * LANES * N, m, factor, slope));
             return;
         }
+        // A group of vectors at a time: this row's gradient leaves, the next row's vectors are asked for, and those that were asked
+        // for AHEAD vectors earlier are added up, so that neither the memory nor the arithmetic waits for the other.
+        constexpr int AHEAD = NV / 2 / kGroup * kGroup;
         x = (const T *)a.logits + next * a.ld_logits;
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            put(j, g, gradient<T>(raw[j], target - at - j * LANES * N, r.m, factor, slope));
-            fetch(j, x);
-            __builtin_amdgcn_sched_barrier(0);               // one vector's widened values at a time
-        }
         if (tail < a.vocab) last = x[tail];
+        r = RowSum{-FLT_MAX, 0.f};
+#pragma unroll
+        for (int k = 0; k < NV; k += kGroup) {
+#pragma unroll
+            for (int j = k; j < k + kGroup; ++j) {
+                put(j, g, gradient<T>(raw[j], target - at - j * LANES * N, m, factor, slope));
+                fetch(j, x);
+                __builtin_amdgcn_sched_barrier(0);           // one vector's widened values at a time
+            }
+            if (k == AHEAD && tail < a.vocab) r = one_element((float)last);
+            if (k >= AHEAD) add_vectors<T, kGroup>(r, raw + k - AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        add_vectors<T, AHEAD>(r, raw + NV - AHEAD);
         row = next;
         info = next_info;
     }
