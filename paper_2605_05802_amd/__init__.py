@@ -23,8 +23,7 @@ EXPORTS = ("sr_init", "sr_destroy", "sr_load_weights", "sr_prefill_chunk", "sr_d
            "sr_probe_hbm", "sr_probe_mfma_bf16", "sr_probe_mfma_under_loads", "sr_gate_batch_antidiag",
            "sr_probe_decode_attention", "sr_policy_loss", "sr_preference_loss", "sr_grad_norm", "sr_clip_grad_norm")
 
-# element types of the update step (sr_dtype) by the name that torch gives them, and ways to take the mean (sr_reduce)
-DTYPES = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}
+# ways to take the mean (sr_reduce)
 REDUCE = {"tokens": 0, "sequences": 1, "sums": 2}
 GRAD_NORM_WORKSPACE = 65536
 
@@ -224,31 +223,41 @@ def token_loss_workspace(n_rows: int, n_seq: int) -> int:
     return 65536 + 64 * n_rows + 32 * n_seq
 
 
-def _of_type(t, name: str, n: int, what: str):
-    """Address of a contiguous tensor of n elements of that type, or None."""
+_types = {}
+
+
+def _dtypes():
+    """torch's element types -> sr_dtype."""
+    if not _types:
+        import torch
+        _types.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+        _types["f4"], _types["i4"], _types["u1"] = torch.float32, torch.int32, torch.uint8
+    return _types
+
+
+def _of_type(t, kind: str, n: int, what: str):
+    """Address of a contiguous tensor of n elements of type f4, i4 or u1, or None."""
     if t is None:
         return None
-    if str(t.dtype) != name or t.numel() != n or not t.is_contiguous():
-        raise SrError(SR_E_ARG, f"{what}: contiguous {name} tensor of {n} elements expected, got {t.dtype} {tuple(t.shape)}")
+    if t.dtype is not _types[kind] or t.numel() != n or not t.is_contiguous():
+        raise SrError(SR_E_ARG, f"{what}: contiguous {_types[kind]} tensor of {n} elements expected, got {t.dtype} {tuple(t.shape)}")
     return t.data_ptr()
 
 
 def _token_rows(where, logits, targets, seq_start, mask, grad, token_logprob, grad_scale):
-    if logits.dim() != 2 or str(logits.dtype) not in DTYPES or (logits.shape[1] > 1 and logits.stride(1) != 1):
+    dtype = _dtypes().get(logits.dtype)
+    if dtype is None or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise SrError(SR_E_ARG, f"{where}: logits: [rows, vocab] of float32, bfloat16 or float16 with adjacent columns expected")
     n, vocab = logits.shape
-    ld_grad = 0
+    ld_grad, to = 0, None
     if grad is not None:
-        if grad.shape != logits.shape or grad.dtype != logits.dtype or (vocab > 1 and grad.stride(1) != 1):
+        if grad.shape != logits.shape or grad.dtype is not logits.dtype or (vocab > 1 and grad.stride(1) != 1):
             raise SrError(SR_E_ARG, f"{where}: grad: shape and type of the logits, with adjacent columns, expected")
-        ld_grad = grad.stride(0) if n > 1 else vocab
-        grad = grad.data_ptr()
+        ld_grad, to = grad.stride(0) if n > 1 else vocab, grad.data_ptr()
     n_seq = seq_start.numel() - 1
-    return TokenRows(logits.data_ptr(), grad, logits.stride(0) if n > 1 else vocab, ld_grad,
-                     _of_type(targets, "torch.int32", n, "targets"), _of_type(mask, "torch.uint8", n, "mask"),
-                     _of_type(seq_start, "torch.int32", n_seq + 1, "seq_start"),
-                     _of_type(token_logprob, "torch.float32", n, "token_logprob"), DTYPES[str(logits.dtype)], n, vocab, n_seq,
-                     grad_scale, 0)
+    return TokenRows(logits.data_ptr(), to, logits.stride(0) if n > 1 else vocab, ld_grad, _of_type(targets, "i4", n, "targets"),
+                     _of_type(mask, "u1", n, "mask"), _of_type(seq_start, "i4", n_seq + 1, "seq_start"),
+                     _of_type(token_logprob, "f4", n, "token_logprob"), dtype, n, vocab, n_seq, grad_scale, 0), n, n_seq
 
 
 def sr_policy_loss(logits, targets, seq_start, old_logprob, advantages, stats, workspace, *, mask=None, ref_logprob=None,
@@ -260,13 +269,11 @@ def sr_policy_loss(logits, targets, seq_start, old_logprob, advantages, stats, w
     targets int32 [rows]; seq_start int32 [sequences + 1]; old_logprob, ref_logprob, token_logprob float32 [rows];
     advantages float32 [sequences]; mask uint8 [rows]; stats float32 [4] receives loss, surrogate, KL, clipped fraction;
     workspace: device bytes, token_loss_workspace(rows, sequences) of them; reduce: "tokens", "sequences" or "sums"."""
-    rows = _token_rows("sr_policy_loss", logits, targets, seq_start, mask, grad, token_logprob, grad_scale)
+    rows, n, n_seq = _token_rows("sr_policy_loss", logits, targets, seq_start, mask, grad, token_logprob, grad_scale)
     opt = PolicyOptions(clip_low, clip_high, kl_coef, REDUCE[reduce])
-    _check(lib().sr_policy_loss(ctypes.byref(rows), _of_type(old_logprob, "torch.float32", rows.n_rows, "old_logprob"),
-                                _of_type(ref_logprob, "torch.float32", rows.n_rows, "ref_logprob"),
-                                _of_type(advantages, "torch.float32", rows.n_seq, "advantages"), ctypes.byref(opt),
-                                _of_type(stats, "torch.float32", 4, "stats"), workspace.data_ptr(),
-                                workspace.numel() * workspace.element_size(), _stream(stream)), "sr_policy_loss")
+    _check(lib().sr_policy_loss(rows, _of_type(old_logprob, "f4", n, "old_logprob"), _of_type(ref_logprob, "f4", n, "ref_logprob"),
+                                _of_type(advantages, "f4", n_seq, "advantages"), opt, _of_type(stats, "f4", 4, "stats"),
+                                workspace.data_ptr(), workspace.nbytes, _stream(stream)), "sr_policy_loss")
 
 
 def sr_preference_loss(logits, targets, seq_start, stats, workspace, *, mask=None, ref_logprob=None, grad=None,
@@ -274,11 +281,10 @@ def sr_preference_loss(logits, targets, seq_start, stats, workspace, *, mask=Non
     """Preference loss over pairs of sequences (2 i preferred to 2 i + 1), and its gradient in `grad`; arguments as for
     sr_policy_loss.  stats float32 [4] receives loss, fraction of pairs in the right order, mean reward of the preferred
     and of the other sequences; log_ratio float32 [sequences]."""
-    rows = _token_rows("sr_preference_loss", logits, targets, seq_start, mask, grad, token_logprob, grad_scale)
-    _check(lib().sr_preference_loss(ctypes.byref(rows), _of_type(ref_logprob, "torch.float32", rows.n_rows, "ref_logprob"), beta,
-                                    label_smoothing, _of_type(log_ratio, "torch.float32", rows.n_seq, "log_ratio"),
-                                    _of_type(stats, "torch.float32", 4, "stats"), workspace.data_ptr(),
-                                    workspace.numel() * workspace.element_size(), _stream(stream)), "sr_preference_loss")
+    rows, n, n_seq = _token_rows("sr_preference_loss", logits, targets, seq_start, mask, grad, token_logprob, grad_scale)
+    _check(lib().sr_preference_loss(rows, _of_type(ref_logprob, "f4", n, "ref_logprob"), beta, label_smoothing,
+                                    _of_type(log_ratio, "f4", n_seq, "log_ratio"), _of_type(stats, "f4", 4, "stats"),
+                                    workspace.data_ptr(), workspace.nbytes, _stream(stream)), "sr_preference_loss")
 
 
 class TensorList:
@@ -288,14 +294,14 @@ class TensorList:
         self.tensors, self.out = list(tensors), None if out is None else list(out)
         if self.out is not None and len(self.out) != len(self.tensors):
             raise SrError(SR_E_ARG, "tensor_list: one output per tensor expected")
-        self.array = (Tensor * len(self.tensors))()
+        types = _dtypes()
+        rows = []
         for i, t in enumerate(self.tensors):
-            o = self.out[i] if self.out is not None else None
-            for x in (t, o):
-                if x is not None and (str(x.dtype) not in DTYPES or not x.is_contiguous() or x.numel() != t.numel()):
-                    raise SrError(SR_E_ARG, f"tensor_list: contiguous float32, bfloat16 or float16 tensors expected ({i})")
-            self.array[i] = Tensor(t.data_ptr(), None if o is None else o.data_ptr(), t.numel(), DTYPES[str(t.dtype)],
-                                   DTYPES[str((t if o is None else o).dtype)])
+            o = t if self.out is None else self.out[i]
+            if t.dtype not in types or o.dtype not in types or not t.is_contiguous() or not o.is_contiguous() or o.numel() != t.numel():
+                raise SrError(SR_E_ARG, f"tensor_list: contiguous float32, bfloat16 or float16 tensors expected ({i})")
+            rows.append((t.data_ptr(), o.data_ptr(), t.numel(), types[t.dtype], types[o.dtype]))
+        self.array = (Tensor * len(rows))(*rows)
 
 
 def tensor_list(tensors, out=None) -> TensorList:
@@ -307,8 +313,8 @@ def tensor_list(tensors, out=None) -> TensorList:
 def _norm_args(tensors, norm, workspace):
     if not isinstance(tensors, TensorList):
         tensors = TensorList(tensors)
-    return (tensors.array, len(tensors.array)), (_of_type(norm, "torch.float32", 1, "norm"), workspace.data_ptr(),
-                                                 workspace.numel() * workspace.element_size())
+    _dtypes()
+    return (tensors.array, len(tensors.array)), (_of_type(norm, "f4", 1, "norm"), workspace.data_ptr(), workspace.nbytes)
 
 
 def sr_grad_norm(tensors, norm, workspace, *, scale=1.0, stream=None):

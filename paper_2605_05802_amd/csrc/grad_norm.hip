@@ -2,11 +2,11 @@
 //
 // norm = |scale| sqrt(sum g^2), out = scale * min(1, max_norm / norm) * g.  Two passes over the data, because no element
 // may be written before the last one has been read: what has to move is each gradient read once and written once, and the
-// second reading on top wherever the list does not fit the caches.
+// second reading on top wherever the list does not fit the caches.  The second pass goes through the list from its end, where the
+// first one has just been.
 //
 // The list travels in the kernel arguments, kListTensors tensors a launch: no copy to the device, nothing kept between calls, and a
-// captured launch holds its own list.  A workgroup takes chunks of kChunk elements in turn and finds a chunk's tensor by
-// bisection over the uniform prefix counts.
+// captured launch holds its own list.  Workgroups copy it to LDS and take chunks of kChunk elements in turn.
 #include <cmath>
 
 #include "row_vectors.h"
@@ -14,38 +14,80 @@
 namespace sr {
 namespace {
 
-constexpr int kListTensors = 120;      // 3.5 KB of kernel arguments
+constexpr int kListTensors = 184;      // with the hidden ones 4 KB of kernel arguments
 constexpr int kChunk = 8192;           // elements
 constexpr int kNormThreads = 256;
-constexpr int kMostBlocks = 2048;      // workgroups of a launch
-constexpr int kSlots = SR_GRAD_NORM_WORKSPACE / 8;
+constexpr int kMostBlocks = 1024;      // workgroups of a launch
+constexpr int kSlots = 2048;           // sums that the workspace holds
+static_assert(kSlots * 8 <= SR_GRAD_NORM_WORKSPACE, "workspace");
 
+// A tensor is an address of 48 bits with, above them, the elements of its last chunk (13 bits, 0 for all of them) and its type.
+constexpr int kAddressBits = 48, kTypeShift = 61;
 struct TensorList {
-    const void *data[kListTensors];
-    void *out[kListTensors];
-    int64_t n[kListTensors];
+    uint64_t data[kListTensors];
+    uint64_t out[kListTensors];        // address and type
     uint32_t first[kListTensors + 1];  // chunk at which a tensor begins; behind the last one the number of chunks
-    uint8_t dtype[kListTensors], out_dtype[kListTensors];
     int32_t tensors;
 };
+static_assert(sizeof(TensorList) + 32 + 256 <= 4096, "kernel arguments");
 
-// tensor of a chunk: the last one that begins at or before it (empty tensors begin where the next one does)
-__device__ __forceinline__ int tensor_of(const TensorList &l, uint32_t chunk) {
-    int lo = 0, hi = l.tensors;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (l.first[mid] <= chunk) lo = mid;
-        else hi = mid;
+struct Chunk {
+    char *data, *out;                  // of the chunk's first element
+    int n, type, out_type;
+};
+
+// The workgroup's copy of the list
+struct ListInLds {
+    uint64_t data[kListTensors], out[kListTensors];
+    uint32_t first[256];               // behind the tensors: no chunk
+
+    __device__ __forceinline__ void fill(const TensorList &l) {
+        const int i = threadIdx.x;
+        if (i < l.tensors) {
+            data[i] = l.data[i];
+            out[i] = l.out[i];
+        }
+        first[i] = i <= l.tensors ? l.first[i] : 0xffffffffu;
     }
-    return lo;
-}
+    // Every wavefront for itself: tensors that begin at or before the chunk, 64 compared at a time.  reversed: the tensor's chunks
+    // are counted from its end.
+    __device__ __forceinline__ Chunk find(uint32_t chunk, bool reversed) const {
+        int t = -1;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) t += __popcll(__ballot(first[64 * k + (threadIdx.x & 63)] <= chunk));
+        const uint64_t d = data[t], o = out[t];
+        const uint32_t from = first[t], count = first[t + 1] - from, at = reversed ? from + count - 1 - chunk : chunk - from;
+        const int rest = (int)(d >> kAddressBits) & (kChunk - 1);
+        Chunk c;
+        c.n = at + 1 == count && rest ? rest : kChunk;
+        c.type = (int)(d >> kTypeShift);
+        c.out_type = (int)(o >> kTypeShift);
+        constexpr uint64_t address = ((uint64_t)1 << kAddressBits) - 1;
+        c.data = (char *)(d & address) + (uint64_t)at * (kChunk * (c.type == SR_F32 ? 4 : 2));
+        c.out = (char *)(o & address) + (uint64_t)at * (kChunk * (c.out_type == SR_F32 ? 4 : 2));
+        return c;
+    }
+};
+static_assert(kNormThreads == 256 && kListTensors < 256, "one entry a thread");
 
 template <typename T>
-__device__ __forceinline__ double squares(const T *p, int64_t at, int64_t n) {
-    constexpr int N = Elem<T>::kPerVec;
-    const int64_t end = at + kChunk < n ? at + kChunk : n;
+__device__ __forceinline__ double squares(const T *p, int n) {
+    constexpr int N = Elem<T>::kPerVec, VECS = kChunk / (kNormThreads * N);
     double acc = 0.0;
-    for (int64_t e = at + (int64_t)threadIdx.x * N; e < end; e += kNormThreads * N) {
+    if (n == kChunk) {
+        raw16 raw[VECS];
+#pragma unroll
+        for (int j = 0; j < VECS; ++j) raw[j] = load_vec(p + (j * kNormThreads + (int)threadIdx.x) * N);
+#pragma unroll
+        for (int j = 0; j < VECS; ++j) {
+            float x[N];
+            Elem<T>::widen(raw[j], x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) acc = fma((double)x[i], (double)x[i], acc);
+        }
+        return acc;
+    }
+    for (int e = threadIdx.x * N; e < n; e += kNormThreads * N) {
         float x[N];
         load_widened(p, e, n, 0.f, x);
 #pragma unroll
@@ -56,63 +98,96 @@ __device__ __forceinline__ double squares(const T *p, int64_t at, int64_t n) {
 
 // add: the slots hold the sums of an earlier launch of the same call
 __global__ __launch_bounds__(kNormThreads) void square_sum_kernel(TensorList l, double *__restrict__ slots, int add) {
+    __shared__ ListInLds list;
     __shared__ double s[kNormThreads / 64];
-    const uint32_t chunks = l.first[l.tensors];
+    list.fill(l);
+    __syncthreads();
+    const uint32_t chunks = list.first[l.tensors];
     double acc = 0.0;
-    for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const int t = tensor_of(l, c);
-        const int64_t at = (int64_t)(c - l.first[t]) * kChunk;
-        acc += l.dtype[t] == SR_F32    ? squares((const float *)l.data[t], at, l.n[t])
-               : l.dtype[t] == SR_BF16 ? squares((const __bf16 *)l.data[t], at, l.n[t])
-                                       : squares((const f16_t *)l.data[t], at, l.n[t]);
+    for (uint32_t k = blockIdx.x; k < chunks; k += gridDim.x) {
+        const Chunk c = list.find(k, false);
+        acc += c.type == SR_F32    ? squares((const float *)c.data, c.n)
+               : c.type == SR_BF16 ? squares((const __bf16 *)c.data, c.n)
+                                   : squares((const f16_t *)c.data, c.n);
     }
     acc = block_sum<kNormThreads / 64>(acc, s);
     if (threadIdx.x == 0) slots[blockIdx.x] = (add ? slots[blockIdx.x] : 0.0) + acc;
 }
 
-__global__ __launch_bounds__(kNormThreads) void norm_kernel(double *__restrict__ slots, int used, float scale, float *__restrict__ norm) {
-    __shared__ double s[kNormThreads / 64];
+// The norm from the slots, in every thread; s: kNormThreads / 64 + 1 doubles of LDS.  The order of the sum is that of the slots' numbers.
+__device__ __forceinline__ double norm_of(const double *__restrict__ slots, int used, float scale, double *s) {
     double acc = 0.0;
     for (int i = threadIdx.x; i < used; i += kNormThreads) acc += slots[i];
     acc = block_sum<kNormThreads / 64>(acc, s);
-    if (threadIdx.x == 0) {
-        const double x = fabs((double)scale) * sqrt(acc);
-        slots[0] = x;
-        *norm = (float)x;
-    }
+    if (threadIdx.x == 0) s[kNormThreads / 64] = fabs((double)scale) * sqrt(acc);
+    __syncthreads();
+    return s[kNormThreads / 64];
 }
 
+__global__ __launch_bounds__(kNormThreads) void norm_kernel(const double *__restrict__ slots, int used, float scale, float *__restrict__ norm) {
+    __shared__ double s[kNormThreads / 64 + 1];
+    const double x = norm_of(slots, used, scale, s);
+    if (threadIdx.x == 0) *norm = (float)x;
+}
+
+// Four elements a thread and step where 16-bit data become single precision, so that whole lines are written at once
 template <typename T, typename U>
-__device__ __forceinline__ void scale_chunk(const T *p, U *q, int64_t at, int64_t n, float c) {
-    constexpr int N = Elem<T>::kPerVec, NU = Elem<U>::kPerVec;
-    const int64_t end = at + kChunk < n ? at + kChunk : n;
-    for (int64_t e = at + (int64_t)threadIdx.x * N; e < end; e += kNormThreads * N) {
-        float x[N];
-        load_widened(p, e, n, 0.f, x);
+__device__ __forceinline__ void scale_chunk(const T *p, U *q, int n, float c) {
+    if constexpr (sizeof(T) == sizeof(U)) {
+        constexpr int N = Elem<T>::kPerVec, VECS = kChunk / (kNormThreads * N);
+        if (n == kChunk) {
+            raw16 raw[VECS];
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] *= c;
+            for (int j = 0; j < VECS; ++j) raw[j] = load_vec_once(p + (j * kNormThreads + (int)threadIdx.x) * N);
 #pragma unroll
-        for (int i = 0; i < N; i += NU) store_narrowed(q, e + i, n, x + i);
+            for (int j = 0; j < VECS; ++j) {
+                float x[N];
+                Elem<T>::widen(raw[j], x);
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] *= c;
+                store_vec_once(q + (j * kNormThreads + (int)threadIdx.x) * N, Elem<T>::narrow(x));
+            }
+            return;
+        }
+    } else {
+        constexpr int VECS = kChunk / (kNormThreads * 4);
+        if (n == kChunk) {
+            raw8 raw[VECS];
+#pragma unroll
+            for (int j = 0; j < VECS; ++j) raw[j] = load_half_vec_once(p + (j * kNormThreads + (int)threadIdx.x) * 4);
+#pragma unroll
+            for (int j = 0; j < VECS; ++j) {
+                float x[8];
+                Elem<T>::widen(raw16{raw[j].x, raw[j].y, 0u, 0u}, x);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] *= c;
+                store_vec_once(q + (j * kNormThreads + (int)threadIdx.x) * 4, Elem<U>::narrow(x));
+            }
+            return;
+        }
     }
+    for (int e = threadIdx.x; e < n; e += kNormThreads) q[e] = (U)((float)p[e] * c);
 }
 
-__global__ __launch_bounds__(kNormThreads) void scale_kernel(TensorList l, const double *__restrict__ slots, float scale, float max_norm) {
-    const double norm = slots[0];
+__global__ __launch_bounds__(kNormThreads) void scale_kernel(TensorList l, const double *__restrict__ slots, int used, float scale,
+                                                             float max_norm, float *__restrict__ norm_out) {
+    __shared__ ListInLds list;
+    __shared__ double s[kNormThreads / 64 + 1];
+    list.fill(l);
+    const double norm = norm_of(slots, used, scale, s);      // and a barrier behind list.fill
+    if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
     // a quotient of doubles, rounded once; false for NaN
     const float c = norm > (double)max_norm && norm <= DBL_MAX ? (float)((double)scale * ((double)max_norm / norm)) : scale;
-    const uint32_t chunks = l.first[l.tensors];
-    for (uint32_t k = blockIdx.x; k < chunks; k += gridDim.x) {
-        const int t = tensor_of(l, k);
-        const int64_t at = (int64_t)(k - l.first[t]) * kChunk, n = l.n[t];
-        const void *p = l.data[t];
-        void *q = l.out[t];
-        if (p == q && c == 1.f) continue;
-        switch (l.dtype[t] * 4 + l.out_dtype[t]) {
-            case SR_F32 * 4 + SR_F32: scale_chunk((const float *)p, (float *)q, at, n, c); break;
-            case SR_BF16 * 4 + SR_F32: scale_chunk((const __bf16 *)p, (float *)q, at, n, c); break;
-            case SR_F16 * 4 + SR_F32: scale_chunk((const f16_t *)p, (float *)q, at, n, c); break;
-            case SR_BF16 * 4 + SR_BF16: scale_chunk((const __bf16 *)p, (__bf16 *)q, at, n, c); break;
-            case SR_F16 * 4 + SR_F16: scale_chunk((const f16_t *)p, (f16_t *)q, at, n, c); break;
+    const uint32_t chunks = list.first[l.tensors];
+    for (uint32_t i = blockIdx.x; i < chunks; i += gridDim.x) {
+        const Chunk k = list.find(i, true);
+        if (k.data == k.out && c == 1.f) continue;
+        switch (k.type * 4 + k.out_type) {
+            case SR_F32 * 4 + SR_F32: scale_chunk((const float *)k.data, (float *)k.out, k.n, c); break;
+            case SR_BF16 * 4 + SR_F32: scale_chunk((const __bf16 *)k.data, (float *)k.out, k.n, c); break;
+            case SR_F16 * 4 + SR_F32: scale_chunk((const f16_t *)k.data, (float *)k.out, k.n, c); break;
+            case SR_BF16 * 4 + SR_BF16: scale_chunk((const __bf16 *)k.data, (__bf16 *)k.out, k.n, c); break;
+            case SR_F16 * 4 + SR_F16: scale_chunk((const f16_t *)k.data, (f16_t *)k.out, k.n, c); break;
         }
     }
 }
@@ -120,29 +195,26 @@ __global__ __launch_bounds__(kNormThreads) void scale_kernel(TensorList l, const
 int check_tensor(const sr_tensor &t, bool clip) {
     if (t.n < 0 || t.n >= (int64_t)1 << 43 || t.dtype < SR_F32 || t.dtype > SR_F16) return SR_E_ARG;
     if (t.n == 0) return SR_OK;
-    if (!t.data || (uintptr_t)t.data % (t.dtype == SR_F32 ? 4 : 2)) return SR_E_ARG;
+    if (!t.data || (uintptr_t)t.data % (t.dtype == SR_F32 ? 4 : 2) || (uintptr_t)t.data >> kAddressBits) return SR_E_ARG;
     if (!clip || !t.out) return SR_OK;
     if (t.out_dtype != t.dtype && t.out_dtype != SR_F32) return SR_E_ARG;
-    if ((uintptr_t)t.out % (t.out_dtype == SR_F32 ? 4 : 2)) return SR_E_ARG;
+    if ((uintptr_t)t.out % (t.out_dtype == SR_F32 ? 4 : 2) || (uintptr_t)t.out >> kAddressBits) return SR_E_ARG;
     return t.out == t.data && t.out_dtype != t.dtype ? SR_E_ARG : SR_OK;
 }
 
-// The next launch's share of the list, from tensor `at` on; returns where the one behind it begins.  The counts of chunks stay
-// below 2^31.
-int take(const sr_tensor *tensors, int n_tensors, int at, TensorList *l) {
+// A launch's share of the list: tensors from `at` on, `step` (1 or -1) forward; returns where the next share begins.  The counts of
+// chunks stay below 2^31.
+int take(const sr_tensor *tensors, int n_tensors, int at, int step, TensorList *l) {
     l->tensors = 0;
     l->first[0] = 0;
-    for (; at < n_tensors && l->tensors < kListTensors; ++at) {
+    for (; at >= 0 && at < n_tensors && l->tensors < kListTensors; at += step) {
         const sr_tensor &t = tensors[at];
         if (t.n == 0) continue;
         const int64_t chunks = (t.n + kChunk - 1) / kChunk + l->first[l->tensors];
         if (chunks > INT32_MAX) break;
         const int i = l->tensors++;
-        l->data[i] = t.data;
-        l->out[i] = t.out ? t.out : t.data;
-        l->n[i] = t.n;
-        l->dtype[i] = (uint8_t)t.dtype;
-        l->out_dtype[i] = (uint8_t)(t.out ? t.out_dtype : t.dtype);
+        l->data[i] = (uint64_t)(uintptr_t)t.data | (uint64_t)(t.n % kChunk) << kAddressBits | (uint64_t)t.dtype << kTypeShift;
+        l->out[i] = (uint64_t)(uintptr_t)(t.out ? t.out : t.data) | (uint64_t)(t.out ? t.out_dtype : t.dtype) << kTypeShift;
         l->first[i + 1] = (uint32_t)chunks;
     }
     return at;
@@ -158,24 +230,27 @@ int norm_and_clip(const sr_tensor *tensors, int n_tensors, float scale, float ma
     TensorList l;
     int used = 0;
     for (int at = 0; at < n_tensors;) {
-        at = take(tensors, n_tensors, at, &l);
+        at = take(tensors, n_tensors, at, 1, &l);
         if (!l.tensors) continue;
         const int blocks = l.first[l.tensors] < kMostBlocks ? (int)l.first[l.tensors] : kMostBlocks;
-        const bool fits = used + blocks <= kSlots;       // if not, at least kMostBlocks slots have been written
+        const bool fits = used + blocks <= kSlots;       // if not, more than kSlots - kMostBlocks >= kMostBlocks of them are in use
         square_sum_kernel<<<dim3(blocks), dim3(kNormThreads), 0, stream>>>(l, fits ? slots + used : slots, !fits);
         SR_HIP(hipGetLastError());
         if (fits) used += blocks;
     }
+    bool written = false;
+    if (clip)
+        for (int at = n_tensors - 1; at >= 0;) {
+            at = take(tensors, n_tensors, at, -1, &l);
+            if (!l.tensors) continue;
+            const int blocks = l.first[l.tensors] < kMostBlocks ? (int)l.first[l.tensors] : kMostBlocks;
+            scale_kernel<<<dim3(blocks), dim3(kNormThreads), 0, stream>>>(l, slots, used, scale, max_norm, written ? nullptr : norm);
+            SR_HIP(hipGetLastError());
+            written = true;
+        }
+    if (written) return SR_OK;
     norm_kernel<<<dim3(1), dim3(kNormThreads), 0, stream>>>(slots, used, scale, norm);
     SR_HIP(hipGetLastError());
-    if (!clip) return SR_OK;
-    for (int at = 0; at < n_tensors;) {
-        at = take(tensors, n_tensors, at, &l);
-        if (!l.tensors) continue;
-        const int blocks = l.first[l.tensors] < kMostBlocks ? (int)l.first[l.tensors] : kMostBlocks;
-        scale_kernel<<<dim3(blocks), dim3(kNormThreads), 0, stream>>>(l, slots, scale, max_norm);
-        SR_HIP(hipGetLastError());
-    }
     return SR_OK;
 }
 

@@ -74,6 +74,11 @@ template <typename T> __device__ __forceinline__ void store_vec(T *p, raw16 v) {
 template <typename T> __device__ __forceinline__ raw16 load_vec_once(const T *p) { return __builtin_nontemporal_load((const raw16_any *)p); }
 template <typename T> __device__ __forceinline__ void store_vec_once(T *p, raw16 v) { __builtin_nontemporal_store(v, (raw16_any *)p); }
 
+// 8 bytes
+typedef uint32_t raw8 __attribute__((ext_vector_type(2), aligned(8)));
+typedef uint32_t raw8_any __attribute__((ext_vector_type(2), aligned(2)));
+template <typename T> __device__ __forceinline__ raw8 load_half_vec_once(const T *p) { return __builtin_nontemporal_load((const raw8_any *)p); }
+
 // Elements [at, at + kPerVec) of a run of n, `fill` behind its end
 template <typename T>
 __device__ __forceinline__ void load_widened(const T *p, int64_t at, int64_t n, float fill, float *x) {
@@ -85,16 +90,19 @@ __device__ __forceinline__ void load_widened(const T *p, int64_t at, int64_t n, 
         for (int i = 0; i < N; ++i) x[i] = at + i < n ? (float)p[at + i] : fill;
     }
 }
-template <typename T>
-__device__ __forceinline__ void store_narrowed(T *p, int64_t at, int64_t n, const float *x) {
-    constexpr int N = Elem<T>::kPerVec;
-    if (at + N <= n) {
-        store_vec(p + at, Elem<T>::narrow(x));
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (at + i < n) p[at + i] = (T)x[i];
-    }
+// Reductions whose result every lane receives, by rotations within 16 lanes and swaps between them: no trip through LDS
+template <typename F>
+__device__ __forceinline__ float reduce_16(float x, F &&f) {
+#define SR_ROTATE(n) f(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + n, 0xf, 0xf, false)))
+    x = SR_ROTATE(8);
+    x = SR_ROTATE(4);
+    x = SR_ROTATE(2);
+    return SR_ROTATE(1);
+#undef SR_ROTATE
+}
+template <typename F>
+__device__ __forceinline__ float reduce_64(float x, F &&f) {
+    return row_reduce(reduce_16(x, f), f);
 }
 
 // Sum over the workgroup, in an order that depends on the thread number alone; valid in thread 0.  s: WAVES doubles of LDS,

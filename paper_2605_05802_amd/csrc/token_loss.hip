@@ -25,13 +25,14 @@ constexpr int kTermThreads = 256;
 constexpr int kSumThreads = 1024;
 constexpr int kParts = 1024;           // parts of rows that the workspace holds
 
-// exp(x) for x <= 0 by the exponential instruction; results below 2^-126 are 0.  The product with log2(e) in single precision is
-// off by 1.3e-8 |x| relative, in one direction: nothing in a probability, but in a sum of exponentials the same for every row, so
-// that a log ratio of 150 tokens was off by 2e-5.  The second form adds what the constant lacks.
-constexpr float kLog2e = 1.44269504088896341f, kLog2eRest = (float)(1.44269504088896341 - (double)1.44269504088896341f);
+// exp(x) for x <= 0 by the exponential instruction; results below 2^-126 are 0.
+// log2(e) in single precision is 1.33e-8 too small, relative: nothing in a probability, but in a sum of exponentials an error of
+// one sign, the same for every row, and a log ratio adds hundreds of rows (150 of them: 2e-5).  The next number up is 6.93e-8 too
+// large; thirteen elements of sixteen taken with the one and three with the other are right to 2e-9 on average.
+constexpr float kLog2e = 0x1.715476p+0f, kLog2eUp = 0x1.715478p+0f;
+static_assert((float)1.44269504088896341 == kLog2e, "the nearest one is the lower one");
 __device__ __forceinline__ float exp_neg(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
-__device__ __forceinline__ float exp_neg_exact(float x) { return __builtin_amdgcn_exp2f(fmaf(x, kLog2eRest, x * kLog2e)); }
-static_assert(kLog2eRest > 0.f, "-infinity has to stay -infinity");
+__device__ __forceinline__ float exp_neg_of_16(float x, int i) { return __builtin_amdgcn_exp2f(x * (i % 5 == 2 ? kLog2eUp : kLog2e)); }
 
 // Running maximum and sum of exponentials relative to it; nothing seen: (-FLT_MAX, 0).  Products and sums that the compiler might
 // fuse in one kernel and not in another are written as they are meant: a row comes out the same whichever kernel takes it.
@@ -40,26 +41,28 @@ struct RowSum {
 };
 __device__ __forceinline__ void merge(RowSum &a, float m2, float s2) {
     const float mn = fmaxf(a.m, m2);
-    a.s = fmaf(a.s, exp_neg_exact(a.m - mn), s2 * exp_neg_exact(m2 - mn));
+    a.s = fmaf(a.s, expf(a.m - mn), s2 * expf(m2 - mn));
     a.m = mn;
 }
 __device__ __forceinline__ RowSum one_element(float x) {
     const float m = fmaxf(x, -FLT_MAX);
-    return RowSum{m, exp_neg_exact(x - m)};
+    return RowSum{m, exp_neg(x - m)};
 }
+// over a wavefront, or over each 16 lanes of it, in every lane
 template <int LANES>
-__device__ __forceinline__ void merge_lanes(RowSum &r) {
-#pragma unroll
-    for (int off = LANES / 2; off >= 1; off >>= 1) merge(r, __shfl_xor(r.m, off, 64), __shfl_xor(r.s, off, 64));
+__device__ __forceinline__ RowSum merge_lanes(RowSum r) {
+    auto larger = [](float x, float y) { return fmaxf(x, y); };
+    auto add = [](float x, float y) { return x + y; };
+    const float m = LANES == 16 ? reduce_16(r.m, larger) : reduce_64(r.m, larger), s = r.s * expf(r.m - m);
+    return RowSum{m, LANES == 16 ? reduce_16(s, add) : reduce_64(s, add)};
 }
-// over the wavefronts of a workgroup, in every lane; s: LDS that nobody reads any more
+// over the wavefronts of a workgroup, in every lane; s: 16 entries of LDS that nobody reads any more
 template <int WAVES>
 __device__ __forceinline__ RowSum merge_waves(RowSum r, RowSum *s) {
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = r;
     __syncthreads();
-    r = s[threadIdx.x & (WAVES - 1)];
-    merge_lanes<WAVES>(r);
-    return r;
+    const int w = threadIdx.x & 15;
+    return merge_lanes<16>(w < WAVES ? s[w] : RowSum{-FLT_MAX, 0.f});
 }
 // The elements of COUNT vectors, sixteen at a time
 template <typename T, int COUNT>
@@ -74,8 +77,8 @@ __device__ __forceinline__ void add_vectors(RowSum &r, const raw16 *raw) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) mn = fmaxf(mn, v[i]);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sum += exp_neg_exact(v[i] - mn);
-        r.s = fmaf(r.s, exp_neg_exact(r.m - mn), sum);
+        for (int i = 0; i < 16; ++i) sum += exp_neg_of_16(v[i] - mn, i);
+        r.s = fmaf(r.s, exp_neg(r.m - mn), sum);
         r.m = mn;
         __builtin_amdgcn_sched_barrier(0);                   // one group's widened values at a time
     }
@@ -133,7 +136,7 @@ constexpr int row_block(int waves) { return waves == 1 ? 256 : 64 * waves; }
 template <typename T, int WAVES>
 __global__ __launch_bounds__(row_block(WAVES)) void row_stats_kernel(RowArgs a) {
     constexpr int N = Elem<T>::kPerVec, LANES = 64 * WAVES, DEPTH = 4;
-    __shared__ RowSum s_part[WAVES];
+    __shared__ RowSum s_part[16];
     const int unit = WAVES == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
     const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
     if (unit >= a.n_rows * a.splits) return;                 // wavefronts without a barrier to come, if any
@@ -160,7 +163,7 @@ __global__ __launch_bounds__(row_block(WAVES)) void row_stats_kernel(RowArgs a) 
             raw[j] = e + j * LANES * N < full ? load_vec(x + e + j * LANES * N) : raw16(Elem<T>::kMinusInf);
         add_vectors<T, DEPTH>(r, raw);
     }
-    merge_lanes<64>(r);
+    r = merge_lanes<64>(r);
     if (WAVES > 1) r = merge_waves<WAVES>(r, s_part);
     if (t == 0) *out = make_float2(r.m, r.s);
 }
@@ -382,7 +385,7 @@ __global__ __launch_bounds__(kSumThreads) void policy_small_kernel(RowArgs a, Po
 template <typename T, int WAVES, int NV, bool LOOP>
 __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowArgs a, PolicyArgs p) {
     constexpr int N = Elem<T>::kPerVec, LANES = 64 * WAVES, kGroup = 16 / N, SURE = NV - kGroup;
-    __shared__ RowSum s_part[2][WAVES];
+    __shared__ RowSum s_part[2][16];
     const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
     int row = WAVES == 1 ? __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)) : blockIdx.x;
     if (row >= a.n_rows) return;
@@ -431,7 +434,7 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
         const float ref_logprob = p.ref_logprob ? p.ref_logprob[row] : 0.f;
         float2 next_info;
         const int next = LOOP ? counting(row + gridDim.x, &next_info) : a.n_rows;
-        merge_lanes<64>(r);
+        r = merge_lanes<64>(r);
         // the half of s_part that the row before used may still be read by wavefronts behind this barrier, but not the other
         if (WAVES > 1) r = merge_waves<WAVES>(r, s_part[turn]);
         const float logprob = (chosen - r.m) - logf(r.s), m = r.m;
