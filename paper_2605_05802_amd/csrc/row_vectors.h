@@ -79,17 +79,6 @@ typedef uint32_t raw8 __attribute__((ext_vector_type(2), aligned(8)));
 typedef uint32_t raw8_any __attribute__((ext_vector_type(2), aligned(2)));
 template <typename T> __device__ __forceinline__ raw8 load_half_vec_once(const T *p) { return __builtin_nontemporal_load((const raw8_any *)p); }
 
-// Elements [at, at + kPerVec) of a run of n, `fill` behind its end
-template <typename T>
-__device__ __forceinline__ void load_widened(const T *p, int64_t at, int64_t n, float fill, float *x) {
-    constexpr int N = Elem<T>::kPerVec;
-    if (at + N <= n) {
-        Elem<T>::widen(load_vec(p + at), x);
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = at + i < n ? (float)p[at + i] : fill;
-    }
-}
 // Reductions whose result every lane receives, by rotations within 16 lanes and swaps between them: no trip through LDS
 template <typename F>
 __device__ __forceinline__ float reduce_16(float x, F &&f) {

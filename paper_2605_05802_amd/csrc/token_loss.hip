@@ -23,7 +23,7 @@ namespace {
 
 constexpr int kTermThreads = 256;
 constexpr int kSumThreads = 1024;
-constexpr int kParts = 1024;           // parts of rows that the workspace holds
+constexpr int kParts = 8192;           // parts of rows that the workspace holds
 
 // exp(x) for x <= 0 by the exponential instruction; results below 2^-126 are 0.
 // log2(e) in single precision is 1.33e-8 too small, relative: nothing in a probability, but in a sum of exponentials an error of
