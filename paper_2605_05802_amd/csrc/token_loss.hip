@@ -23,6 +23,8 @@ namespace {
 
 constexpr int kTermThreads = 256;
 constexpr int kSumThreads = 1024;
+constexpr int kMostInline = 1024;      // sequences of a small call
+constexpr int kMostInfoSmall = 4096;   // rows whose weights one workgroup looks up
 constexpr int kParts = 8192;           // parts of rows that the workspace holds
 
 // exp(x) for x <= 0 by the exponential instruction; results below 2^-126 are 0.
@@ -255,43 +257,82 @@ __global__ __launch_bounds__(256) void seq_count_kernel(RowArgs a) {
     if (lane == 0) a.count[seq] = n;
 }
 
-// Weight and advantage of `row`.  rows, used: counting rows of all sequences, and sequences that have any
-__device__ __forceinline__ float2 row_info(const RowArgs &a, const PolicyArgs &p, int row, int rows, int used) {
-    const int seq = !a.mask || a.mask[row] ? sequence_of(a.seq_start, a.n_seq, row) : -1;
-    if (seq < 0) return make_float2(0.f, 0.f);
+// Weight and advantage of a counting row.  count: its sequence's counting rows; rows, used: those of all sequences, and the sequences
+// that have any
+__device__ __forceinline__ float2 row_info(const PolicyArgs &p, int seq, int count, int rows, int used) {
     const float w = p.reduce == SR_MEAN_TOKENS      ? 1.f / (float)rows
-                    : p.reduce == SR_MEAN_SEQUENCES ? 1.f / ((float)used * (float)a.count[seq])
+                    : p.reduce == SR_MEAN_SEQUENCES ? 1.f / ((float)used * (float)count)
                                                     : 1.f / (float)used;
     return make_float2(w, p.advantages[seq]);
 }
 
-// Sums of count[] and of its non-zero entries over all sequences, by every workgroup for itself.  s: two ints of LDS
-template <int THREADS>
-__device__ __forceinline__ void count_totals(const RowArgs &a, int *s) {
-    if (threadIdx.x < 2) s[threadIdx.x] = 0;
-    __syncthreads();
-    int rows = 0, used = 0;
-    for (int i = threadIdx.x; i < a.n_seq; i += THREADS) {
-        rows += a.count[i];
-        used += a.count[i] > 0;
+// The sequences of a small call in LDS
+struct SeqTable {
+    int start[kMostInline + 1], count[kMostInline], rows, used;
+
+    // by the whole workgroup; barriers inside and behind
+    template <int THREADS>
+    __device__ __forceinline__ void fill(const RowArgs &a) {
+        for (int i = threadIdx.x; i <= a.n_seq; i += THREADS) start[i] = a.seq_start[i];
+        for (int i = threadIdx.x; i < a.n_seq; i += THREADS) count[i] = 0;
+        if (threadIdx.x == 0) rows = used = 0;
+        __syncthreads();
+        if (a.mask) {
+            const int to = min(start[a.n_seq], a.n_rows);
+            for (int r = max(start[0], 0) + (int)threadIdx.x; r < to; r += THREADS) {
+                const int seq = a.mask[r] ? sequence_of(start, a.n_seq, r) : -1;
+                if (seq >= 0) atomicAdd(&count[seq], 1);     // whole numbers: the order does not matter
+            }
+            __syncthreads();
+        }
+        int n = 0, some = 0;
+        for (int i = threadIdx.x; i < a.n_seq; i += THREADS) {
+            const int c = a.mask ? count[i] : max(min(start[i + 1], a.n_rows) - max(start[i], 0), 0);
+            if (!a.mask) count[i] = c;
+            n += c;
+            some += c > 0;
+        }
+        add_up(n, some, &rows, &used);
+        __syncthreads();
     }
+    static __device__ __forceinline__ void add_up(int n, int some, int *rows, int *used) {
 #pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) {
-        rows += __shfl_xor(rows, off, 64);
-        used += __shfl_xor(used, off, 64);
+        for (int off = 32; off >= 1; off >>= 1) {
+            n += __shfl_xor(n, off, 64);
+            some += __shfl_xor(some, off, 64);
+        }
+        if ((threadIdx.x & 63) == 0) {
+            atomicAdd(rows, n);
+            atomicAdd(used, some);
+        }
     }
-    if ((threadIdx.x & 63) == 0) {
-        atomicAdd(&s[0], rows);                              // whole numbers: the order does not matter
-        atomicAdd(&s[1], used);
+    __device__ __forceinline__ float2 info(const RowArgs &a, const PolicyArgs &p, int row) const {
+        const int seq = !a.mask || a.mask[row] ? sequence_of(start, a.n_seq, row) : -1;
+        return seq < 0 ? make_float2(0.f, 0.f) : row_info(p, seq, count[seq], rows, used);
     }
-    __syncthreads();
-}
+};
 
 __global__ __launch_bounds__(kTermThreads) void row_info_kernel(RowArgs a, PolicyArgs p) {
-    __shared__ int s[2];
-    count_totals<kTermThreads>(a, s);
+    __shared__ int s_rows, s_used;
+    if (threadIdx.x == 0) s_rows = s_used = 0;
+    __syncthreads();
+    int n = 0, some = 0;                                     // of all sequences, by every workgroup for itself
+    for (int i = threadIdx.x; i < a.n_seq; i += kTermThreads) {
+        n += a.count[i];
+        some += a.count[i] > 0;
+    }
+    SeqTable::add_up(n, some, &s_rows, &s_used);
+    __syncthreads();
     const int row = blockIdx.x * kTermThreads + threadIdx.x;
-    if (row < a.n_rows) a.info[row] = row_info(a, p, row, s[0], s[1]);
+    if (row >= a.n_rows) return;
+    const int seq = !a.mask || a.mask[row] ? sequence_of(a.seq_start, a.n_seq, row) : -1;
+    a.info[row] = seq < 0 ? make_float2(0.f, 0.f) : row_info(p, seq, a.count[seq], s_rows, s_used);
+}
+// seq_count_kernel and row_info_kernel by one workgroup
+__global__ __launch_bounds__(kSumThreads) void row_info_small_kernel(RowArgs a, PolicyArgs p) {
+    __shared__ SeqTable table;
+    table.fill<kSumThreads>(a);
+    for (int row = threadIdx.x; row < a.n_rows; row += kSumThreads) a.info[row] = table.info(a, p, row);
 }
 
 // A counting row's slope, and its terms of the loss
@@ -310,6 +351,20 @@ __device__ __forceinline__ float policy_row(const PolicyArgs &p, float2 info, fl
     return slope * info.x;
 }
 
+// What a row's slope takes beside its logits, by scalar loads: they do not queue behind the row's stores
+struct RowScalars {
+    int target;
+    float old_logprob, ref_logprob;
+};
+template <typename V> __device__ __forceinline__ V read_uniform(const V *p) {
+    typedef std::conditional_t<sizeof(V) == 8, uint64_t, uint32_t> bits;
+    return __builtin_bit_cast(V, *(const __attribute__((address_space(4))) bits *)p);
+}
+__device__ __forceinline__ RowScalars row_scalars(const RowArgs &a, const PolicyArgs &p, int row) {
+    return RowScalars{read_uniform(a.targets + row), read_uniform(p.old_logprob + row),
+                      p.ref_logprob ? read_uniform(p.ref_logprob + row) : 0.f};
+}
+
 struct PolicySums {
     double surrogate = 0.0, kl = 0.0, out = 0.0;
     __device__ __forceinline__ void add(float4 t) {
@@ -318,11 +373,33 @@ struct PolicySums {
         kl += (double)t.w * (double)t.y;
         out += (double)t.w * (double)t.z;
     }
-    // over the workgroup; s: kSumThreads / 64 doubles of LDS
+    // over the workgroup; s: 3 * kSumThreads / 64 doubles of LDS
     __device__ __forceinline__ void finish(const PolicyArgs &p, double *s) {
-        surrogate = block_sum<kSumThreads / 64>(surrogate, s);
-        kl = block_sum<kSumThreads / 64>(kl, s);
-        out = block_sum<kSumThreads / 64>(out, s);
+        constexpr int WAVES = kSumThreads / 64;
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) {
+            surrogate += __shfl_xor(surrogate, off, 64);
+            kl += __shfl_xor(kl, off, 64);
+            out += __shfl_xor(out, off, 64);
+        }
+        if ((threadIdx.x & 63) == 0) {
+            double *mine = s + threadIdx.x / 64;
+            mine[0] = surrogate;
+            mine[WAVES] = kl;
+            mine[2 * WAVES] = out;
+        }
+        __syncthreads();
+        if (threadIdx.x >= 64) return;
+        const int k = threadIdx.x & (WAVES - 1);             // the first 16 lanes have all they need
+        surrogate = s[k];
+        kl = s[WAVES + k];
+        out = s[2 * WAVES + k];
+#pragma unroll
+        for (int off = WAVES / 2; off >= 1; off >>= 1) {
+            surrogate += __shfl_xor(surrogate, off, 64);
+            kl += __shfl_xor(kl, off, 64);
+            out += __shfl_xor(out, off, 64);
+        }
         if (threadIdx.x != 0) return;
         p.stats[0] = (float)((p.kl_coef != 0.f ? (double)p.kl_coef * kl : 0.0) - surrogate);
         p.stats[1] = (float)surrogate;
@@ -353,26 +430,20 @@ __global__ __launch_bounds__(kTermThreads) void policy_rows_kernel(RowArgs a, Po
     if (row < a.n_rows) a.terms[row] = finish_row<T>(a, p, row, a.info[row]);
 }
 __global__ __launch_bounds__(kSumThreads) void policy_sum_kernel(RowArgs a, PolicyArgs p) {
-    __shared__ double s[kSumThreads / 64];
+    __shared__ double s[3 * kSumThreads / 64];
     PolicySums sums;
     for (int i = threadIdx.x; i < a.n_rows; i += kSumThreads) sums.add(a.terms[i]);
     sums.finish(p, s);
 }
 
-// The four kernels between row_stats_kernel and logit_grad_kernel by one workgroup: few rows
+// The kernels between row_stats_kernel and logit_grad_kernel, and policy_sum_kernel, by one workgroup: few rows
 template <typename T>
 __global__ __launch_bounds__(kSumThreads) void policy_small_kernel(RowArgs a, PolicyArgs p) {
-    __shared__ double s[kSumThreads / 64];
-    __shared__ int s_totals[2];
-    for (int seq = threadIdx.x >> 6; seq < a.n_seq; seq += kSumThreads / 64) {
-        const int n = count_rows(a, seq, threadIdx.x & 63);
-        if ((threadIdx.x & 63) == 0) a.count[seq] = n;
-    }
-    __syncthreads();
-    count_totals<kSumThreads>(a, s_totals);
+    __shared__ double s[3 * kSumThreads / 64];
+    __shared__ SeqTable table;
+    table.fill<kSumThreads>(a);
     PolicySums sums;
-    for (int row = threadIdx.x; row < a.n_rows; row += kSumThreads)
-        sums.add(finish_row<T>(a, p, row, row_info(a, p, row, s_totals[0], s_totals[1])));
+    for (int row = threadIdx.x; row < a.n_rows; row += kSumThreads) sums.add(finish_row<T>(a, p, row, table.info(a, p, row)));
     sums.finish(p, s);
 }
 
@@ -382,13 +453,14 @@ __global__ __launch_bounds__(kSumThreads) void policy_small_kernel(RowArgs a, Po
 // WAVES wavefronts take a row, NV vectors a thread: the row is read once and written once.  NV - kGroup vectors of every thread lie
 // inside the row, the last kGroup may not.  Rows of one wavefront: four to a workgroup.  LOOP: a workgroup takes every
 // gridDim-th row, and asks for the next row's vectors as the gradient's leave the registers.
-template <typename T, int WAVES, int NV, bool LOOP>
+// TABLE: the workgroups look the weights up for themselves (small calls), else they are in a.info.
+template <typename T, int WAVES, int NV, bool LOOP, bool TABLE>
 __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowArgs a, PolicyArgs p) {
+    static_assert(!(LOOP && TABLE), "a workgroup of many rows reads what row_info_kernel wrote");
     constexpr int N = Elem<T>::kPerVec, LANES = 64 * WAVES, kGroup = 16 / N, SURE = NV - kGroup;
     __shared__ RowSum s_part[2][16];
     const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
     int row = WAVES == 1 ? __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)) : blockIdx.x;
-    if (row >= a.n_rows) return;
     const int full = a.vocab / N * N, tail = full + t;
     raw16 raw[NV];
     T last;                                                  // lanes behind the last whole vector: an element of the rest
@@ -400,46 +472,71 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
     auto put = [&](int j, T *g, raw16 v) __attribute__((always_inline)) {
         if (j < SURE || at + j * LANES * N < full) store_vec_once(g + j * LANES * N + (unsigned)at, v);
     };
-    // the first counting row from `row` on; those before it get their zeros
+    auto zeros = [&](int row) __attribute__((always_inline)) {
+        T *g = (T *)a.grad + row * a.ld_grad;
+        for (int j = 0; j < NV; ++j) put(j, g, raw16(0));
+        if (tail < a.vocab) g[tail] = (T)0.f;
+        if (t == 0) {
+            if (a.token_logprob) a.token_logprob[row] = 0.f;
+            a.terms[row] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+    };
+    // the first counting row from `row` on in steps of the grid; those before it get their zeros
     auto counting = [&](int row, float2 *info) __attribute__((always_inline)) {
         for (; row < a.n_rows; row += gridDim.x) {
-            *info = a.info[row];
+            *info = read_uniform(a.info + row);
             if (info->x != 0.f) break;
-            T *g = (T *)a.grad + row * a.ld_grad;
-            for (int j = 0; j < NV; ++j) put(j, g, raw16(0));
-            if (tail < a.vocab) g[tail] = (T)0.f;
-            if (t == 0) {
-                if (a.token_logprob) a.token_logprob[row] = 0.f;
-                a.terms[row] = make_float4(0.f, 0.f, 0.f, 0.f);
-            }
-            if (!LOOP) return a.n_rows;
+            zeros(row);
         }
         return row;
     };
     float2 info;
-    row = counting(row, &info);
-    if (row >= a.n_rows) return;
+    bool mine = row < a.n_rows;                              // false for a wavefront of a small call that has no counting row
+    if constexpr (LOOP) {
+        row = counting(row, &info);
+        if (row >= a.n_rows) return;
+    } else if (TABLE) {
+        if (mine && !row_counts(a, row)) {
+            zeros(row);
+            mine = false;
+        }
+    } else {
+        if (!mine) return;
+        info = read_uniform(a.info + row);
+        if (info.x == 0.f) return zeros(row);
+    }
     const T *x = (const T *)a.logits + row * a.ld_logits;
+    if (mine) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) fetch(j, x);
-    if (tail < a.vocab) last = x[tail];
+        for (int j = 0; j < NV; ++j) fetch(j, x);
+        if (tail < a.vocab) last = x[tail];
+    }
+    if constexpr (TABLE) {
+        __shared__ SeqTable table;
+        table.template fill<row_block(WAVES)>(a);
+        if (!mine) return;
+        info = table.info(a, p, row);
+    }
+    RowScalars scalars = row_scalars(a, p, row);
+    float chosen = logit_of<T>(a, row, scalars.target);
     RowSum r = {-FLT_MAX, 0.f};
     if (tail < a.vocab) r = one_element((float)last);
     add_vectors<T, NV>(r, raw);
     for (int turn = 0;; turn ^= 1) {
         asm volatile("" : "+v"(at));                         // or the loop keeps every vector's address and index in registers
         T *g = (T *)a.grad + row * a.ld_grad;
-        const int target = a.targets[row];
-        const float chosen = logit_of<T>(a, row, target), old_logprob = p.old_logprob[row];
-        const float ref_logprob = p.ref_logprob ? p.ref_logprob[row] : 0.f;
         float2 next_info;
         const int next = LOOP ? counting(row + gridDim.x, &next_info) : a.n_rows;
+        RowScalars next_scalars;
+        if (LOOP && next < a.n_rows) next_scalars = row_scalars(a, p, next);
         r = merge_lanes<64>(r);
         // the half of s_part that the row before used may still be read by wavefronts behind this barrier, but not the other
         if (WAVES > 1) r = merge_waves<WAVES>(r, s_part[turn]);
         const float logprob = (chosen - r.m) - logf(r.s), m = r.m;
         float4 term;
-        const float slope = policy_row(p, info, logprob, old_logprob, ref_logprob, &term) * a.grad_scale, factor = -slope / r.s;
+        const float slope = policy_row(p, info, logprob, scalars.old_logprob, scalars.ref_logprob, &term) * a.grad_scale;
+        const float factor = -slope / r.s;
+        const int target = scalars.target;
         if (t == 0) {
             if (a.token_logprob) a.token_logprob[row] = logprob;
             a.terms[row] = term;
@@ -458,6 +555,7 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
         constexpr int AHEAD = NV / 2 / kGroup * kGroup;
         x = (const T *)a.logits + next * a.ld_logits;
         if (tail < a.vocab) last = x[tail];
+        chosen = logit_of<T>(a, next, next_scalars.target);
         r = RowSum{-FLT_MAX, 0.f};
 #pragma unroll
         for (int k = 0; k < NV; k += kGroup) {
@@ -474,6 +572,7 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
         add_vectors<T, AHEAD>(r, raw + NV - AHEAD);
         row = next;
         info = next_info;
+        scalars = next_scalars;
     }
 }
 
@@ -626,6 +725,11 @@ int launch_logit_grad(const RowArgs &a, int waves, hipStream_t stream) {
 }
 
 int launch_row_info(const RowArgs &a, const PolicyArgs &p, hipStream_t stream) {
+    if (a.n_seq <= kMostInline && a.n_rows <= kMostInfoSmall) {
+        row_info_small_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(a, p);
+        SR_HIP(hipGetLastError());
+        return SR_OK;
+    }
     seq_count_kernel<<<dim3(ceil_div(a.n_seq, 4)), dim3(256), 0, stream>>>(a);
     SR_HIP(hipGetLastError());
     row_info_kernel<<<dim3(ceil_div(a.n_rows, kTermThreads)), dim3(kTermThreads), 0, stream>>>(a, p);
@@ -637,11 +741,20 @@ int launch_row_info(const RowArgs &a, const PolicyArgs &p, hipStream_t stream) {
 template <typename T, int WAVES, int NV>
 int launch_resident(const RowArgs &a, const PolicyArgs &p, int vecs, hipStream_t stream) {
     constexpr int kGroup = 16 / Elem<T>::kPerVec;
-    constexpr bool LOOP = WAVES == 16;
     if constexpr (NV + kGroup <= (WAVES == 1 ? kMostOneWave : kMostResident))
         if (vecs > NV) return launch_resident<T, WAVES, NV + kGroup>(a, p, vecs, stream);
-    const int blocks = WAVES == 1 ? ceil_div(a.n_rows, 4) : LOOP && a.n_rows > 256 ? 256 : a.n_rows;
-    policy_resident_kernel<T, WAVES, NV, LOOP><<<dim3(blocks), dim3(row_block(WAVES)), 0, stream>>>(a, p);
+    if constexpr (WAVES == 16) {
+        SR_TRY(launch_row_info(a, p, stream));
+        policy_resident_kernel<T, WAVES, NV, true, false><<<dim3(a.n_rows < 256 ? a.n_rows : 256), dim3(row_block(WAVES)), 0, stream>>>(a, p);
+    } else {
+        const int blocks = WAVES == 1 ? ceil_div(a.n_rows, 4) : a.n_rows;
+        if (a.n_rows <= kSumThreads && a.n_seq <= kMostInline) {
+            policy_resident_kernel<T, WAVES, NV, false, true><<<dim3(blocks), dim3(row_block(WAVES)), 0, stream>>>(a, p);
+        } else {
+            SR_TRY(launch_row_info(a, p, stream));
+            policy_resident_kernel<T, WAVES, NV, false, false><<<dim3(blocks), dim3(row_block(WAVES)), 0, stream>>>(a, p);
+        }
+    }
     SR_HIP(hipGetLastError());
     return SR_OK;
 }
@@ -649,20 +762,17 @@ template <typename T>
 int launch_resident(const RowArgs &a, const PolicyArgs &p, int waves, int vecs, hipStream_t stream) {
     if (waves == 1) return launch_resident<T, 1, 16 / Elem<T>::kPerVec>(a, p, vecs, stream);
     if (waves == 4) return launch_resident<T, 4, 4>(a, p, vecs, stream);
-    return launch_resident<T, 16, 8>(a, p, vecs, stream);
+    return launch_resident<T, 16, 4>(a, p, vecs, stream);
 }
 
 int policy_loss(const sr_token_rows *x, const PolicyArgs &p, void *workspace, hipStream_t stream) {
     const RowPlan plan = plan_policy_rows(x->n_rows, x->vocab, x->dtype == SR_F32 ? 4 : 2);
     const RowArgs a = row_args(x, plan, workspace);
-    const bool small = a.n_rows <= kSumThreads && !(a.grad && plan.resident);
+    const bool small = a.n_rows <= kSumThreads && a.n_seq <= kMostInline && !(a.grad && plan.resident);
     if (a.n_rows > 0)
         SR_TRY(with_type(x->dtype, [&](auto *t) -> int {
             typedef std::remove_pointer_t<decltype(t)> T;
-            if (a.grad && plan.resident) {
-                SR_TRY(launch_row_info(a, p, stream));
-                return launch_resident<T>(a, p, plan.waves, plan.resident, stream);
-            }
+            if (a.grad && plan.resident) return launch_resident<T>(a, p, plan.waves, plan.resident, stream);
             SR_TRY(launch_row_stats<T>(a, plan.waves, stream));
             if (small) {
                 policy_small_kernel<T><<<dim3(1), dim3(kSumThreads), 0, stream>>>(a, p);
