@@ -24,7 +24,9 @@ namespace {
 constexpr int kTermThreads = 256;
 constexpr int kSumThreads = 1024;
 constexpr int kMostInline = 1024;      // sequences of a small call
-constexpr int kMostInfoSmall = 4096;   // rows whose weights one workgroup looks up
+constexpr int kMostTableRows = 4096;   // its rows
+constexpr int kMostTableBlocks = 512;  // workgroups that look the weights up for themselves
+constexpr int kMostPairRows = 512, kMostPairSeqs = 32;     // of a small call of the preference loss
 constexpr int kParts = 8192;           // parts of rows that the workspace holds
 
 // exp(x) for x <= 0 by the exponential instruction; results below 2^-126 are 0.
@@ -96,6 +98,7 @@ struct RowArgs {
     float *token_logprob;
     int n_rows, vocab, n_seq;
     int splits, split_elems;           // parts of a row, whole vectors each
+    int grad_splits, grad_elems;       // of the gradient's
     float grad_scale;
     // workspace
     float2 *part;        // [n_rows][splits] (m, s)
@@ -195,17 +198,17 @@ __device__ __forceinline__ raw16 gradient(raw16 raw, int hot, float m, float fac
     return Elem<T>::narrow(v);
 }
 
-// The parts of row_stats_kernel.  In place: a thread reads what it then writes.
+// WAVES wavefronts per (row, part).  In place: a thread reads what it then writes.
 template <typename T, int WAVES>
 __global__ __launch_bounds__(row_block(WAVES)) void logit_grad_kernel(RowArgs a) {
     constexpr int N = Elem<T>::kPerVec, LANES = 64 * WAVES, DEPTH = 4;
     const int unit = WAVES == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
     const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
-    if (unit >= a.n_rows * a.splits) return;
-    const int row = unit / a.splits, part = unit - row * a.splits;
+    if (unit >= a.n_rows * a.grad_splits) return;
+    const int row = unit / a.grad_splits, part = unit - row * a.grad_splits;
     const T *x = (const T *)a.logits + row * a.ld_logits;
     T *g = (T *)a.grad + row * a.ld_grad;
-    const int from = part * a.split_elems, to = min(from + a.split_elems, a.vocab), full = from + (to - from) / N * N;
+    const int from = part * a.grad_elems, to = min(from + a.grad_elems, a.vocab), full = from + (to - from) / N * N;
     const float2 whole = a.whole[row];
     if (whole.y == kNoRow) {
         for (int e = from + t * N; e < full; e += LANES * N) store_vec_once(g + e, raw16(0));
@@ -266,29 +269,66 @@ __device__ __forceinline__ float2 row_info(const PolicyArgs &p, int seq, int cou
     return make_float2(w, p.advantages[seq]);
 }
 
-// The sequences of a small call in LDS
+// One bit for every byte of a word that is not zero
+__device__ __forceinline__ unsigned set_bytes(unsigned w) {
+    const unsigned top = (((w & 0x7f7f7f7fu) + 0x7f7f7f7fu) | w) & 0x80808080u;
+    return ((top >> 7) * 0x10204080u) >> 28;                 // bits 0, 8, 16, 24 to 28 .. 31, the other products apart from each other
+}
+
+// The sequences of a small call in LDS.  Counting rows in front of a row: sixteen rows of the mask are a word of bits, with the number
+// of set bits before it.
 struct SeqTable {
-    int start[kMostInline + 1], count[kMostInline], rows, used;
+    int start[kMostInline + 1], count[kMostInline], before[kMostTableRows / 16 + 1], rows, used;
+    uint16_t bits[kMostTableRows / 16 + 1];
+    int wave_total[kMostTableRows / 16 / 64];
+
+    __device__ __forceinline__ int rank(int row) const { return before[row >> 4] + __popc(bits[row >> 4] & ((1u << (row & 15)) - 1u)); }
 
     // by the whole workgroup; barriers inside and behind
     template <int THREADS>
     __device__ __forceinline__ void fill(const RowArgs &a) {
-        for (int i = threadIdx.x; i <= a.n_seq; i += THREADS) start[i] = a.seq_start[i];
-        for (int i = threadIdx.x; i < a.n_seq; i += THREADS) count[i] = 0;
-        if (threadIdx.x == 0) rows = used = 0;
-        __syncthreads();
+        static_assert(kMostTableRows / 16 == 256 && THREADS >= 256, "a word a thread");
+        const int t = threadIdx.x;
+        for (int i = t; i <= a.n_seq; i += THREADS) start[i] = a.seq_start[i];
+        if (t == 0) rows = used = 0;
         if (a.mask) {
-            const int to = min(start[a.n_seq], a.n_rows);
-            for (int r = max(start[0], 0) + (int)threadIdx.x; r < to; r += THREADS) {
-                const int seq = a.mask[r] ? sequence_of(start, a.n_seq, r) : -1;
-                if (seq >= 0) atomicAdd(&count[seq], 1);     // whole numbers: the order does not matter
+            unsigned mine = 0;
+            int ahead = 0;
+            if (t < 256) {
+                const int n = a.n_rows - 16 * t;
+                if (n >= 16) {
+                    const raw16 m = load_vec((const __bf16 *)(a.mask + 16 * t));
+                    mine = set_bytes(m[0]) | set_bytes(m[1]) << 4 | set_bytes(m[2]) << 8 | set_bytes(m[3]) << 12;
+                } else {
+                    for (int i = 0; i < n; ++i) mine |= (unsigned)(a.mask[16 * t + i] != 0) << i;
+                }
+                const int own = __popc(mine);
+                ahead = own;
+#pragma unroll
+                for (int off = 1; off < 64; off <<= 1) {
+                    const int x = __shfl_up(ahead, off, 64);
+                    if ((t & 63) >= off) ahead += x;
+                }
+                if ((t & 63) == 63) wave_total[t >> 6] = ahead;
+                ahead -= own;
             }
             __syncthreads();
+            if (t < 256) {
+                for (int w = 0; w < t >> 6; ++w) ahead += wave_total[w];
+                before[t] = ahead;
+                bits[t] = (uint16_t)mine;
+                if (t == 255) {
+                    before[256] = ahead + __popc(mine);
+                    bits[256] = 0;
+                }
+            }
         }
+        __syncthreads();
         int n = 0, some = 0;
-        for (int i = threadIdx.x; i < a.n_seq; i += THREADS) {
-            const int c = a.mask ? count[i] : max(min(start[i + 1], a.n_rows) - max(start[i], 0), 0);
-            if (!a.mask) count[i] = c;
+        for (int i = t; i < a.n_seq; i += THREADS) {
+            const int from = max(start[i], 0), to = min(start[i + 1], a.n_rows);
+            const int c = from >= to ? 0 : a.mask ? rank(to) - rank(from) : to - from;
+            count[i] = c;
             n += c;
             some += c > 0;
         }
@@ -585,56 +625,66 @@ struct PairArgs {
     float *log_ratio, *stats;
 };
 
-// One workgroup per pair.  Rows outside every sequence are left to the first and the last one.
-template <typename T>
-__global__ __launch_bounds__(kTermThreads) void pair_kernel(RowArgs a, PairArgs p) {
-    __shared__ double s[kTermThreads / 64];
-    __shared__ float s_slope;
-    const int pair = blockIdx.x, pairs = a.n_seq / 2;
-    double ratio[2];
-    for (int k = 0; k < 2; ++k) {
-        const int from = max(a.seq_start[2 * pair + k], 0), to = min(a.seq_start[2 * pair + k + 1], a.n_rows);
-        double acc = 0.0;
-        for (int row = from + threadIdx.x; row < to; row += kTermThreads) {
-            const RowSum r = whole_row(a, row);
-            double logprob = 0.0;
-            if (r.s != kNoRow) {
-                // l in double: a pair adds hundreds of them, and rounds to single precision once
-                logprob = (double)(logit_of<T>(a, row, a.targets[row]) - r.m) - log((double)r.s);
-                acc += logprob - (p.ref_logprob ? (double)p.ref_logprob[row] : 0.0);
-            }
-            a.whole[row] = make_float2(r.m, r.s);
-            if (a.token_logprob) a.token_logprob[row] = (float)logprob;
-        }
-        ratio[k] = block_sum<kTermThreads / 64>(acc, s);
-    }
-    if (threadIdx.x == 0) {
-        const double reward0 = (double)p.beta * ratio[0], reward1 = (double)p.beta * ratio[1], m = reward0 - reward1;
-        const double tail = log1p(exp(-fabs(m)));
-        const double sm = p.smoothing;                   // a term with weight 0 is left out: it may be infinite
-        const double loss = (sm < 1.0 ? (1.0 - sm) * (fmax(-m, 0.0) + tail) : 0.0) + (sm > 0.0 ? sm * (fmax(m, 0.0) + tail) : 0.0);
-        s_slope = (float)((double)p.beta / pairs * (sm / (1.0 + exp(-m)) - (1.0 - sm) / (1.0 + exp(m))) * (double)a.grad_scale);
-        if (p.log_ratio) {
-            p.log_ratio[2 * pair] = (float)ratio[0];
-            p.log_ratio[2 * pair + 1] = (float)ratio[1];
-        }
-        a.terms[pair] = make_float4((float)loss, m > 0.0 ? 1.f : 0.f, (float)reward0, (float)reward1);
-    }
-    __syncthreads();
+// A pair, by LANES threads of which this is number t: log ratios, margin, slopes.  sum(x): over the LANES threads, in all of them.
+// Returns the pair's terms of the loss.  Rows outside every sequence are left to the first and the last pair.
+template <typename T, int LANES, typename F>
+__device__ __forceinline__ float4 finish_pair(const RowArgs &a, const PairArgs &p, int pair, int t, F &&sum) {
+    const int pairs = a.n_seq / 2;
     const int start = max(a.seq_start[2 * pair], 0), mid = a.seq_start[2 * pair + 1], end = min(a.seq_start[2 * pair + 2], a.n_rows);
-    for (int row = start + threadIdx.x; row < end; row += kTermThreads) a.slope[row] = row < mid ? s_slope : -s_slope;
+    double ratio[2] = {};
+    for (int row = start + t; row < end; row += LANES) {
+        const int target = a.targets[row];
+        const double ref = p.ref_logprob ? (double)p.ref_logprob[row] : 0.0;
+        const RowSum r = whole_row(a, row);
+        double logprob = 0.0;
+        if (r.s != kNoRow) {
+            // l in double: a pair adds hundreds of them, and rounds to single precision once
+            logprob = (double)(logit_of<T>(a, row, target) - r.m) - log((double)r.s);
+            if (row < mid) ratio[0] += logprob - ref;
+            else ratio[1] += logprob - ref;
+        }
+        a.whole[row] = make_float2(r.m, r.s);
+        if (a.token_logprob) a.token_logprob[row] = (float)logprob;
+    }
+    ratio[0] = sum(ratio[0]);
+    ratio[1] = sum(ratio[1]);
+    const double reward0 = (double)p.beta * ratio[0], reward1 = (double)p.beta * ratio[1];
+    // The margin is a difference of sums in double; what becomes of it is good to single precision from there on.
+    const float m = (float)(reward0 - reward1), e = expf(-fabsf(m)), tail = log1pf(e), sm = p.smoothing;
+    // a term with weight 0 is left out: it may be infinite
+    const float loss = (sm < 1.f ? (1.f - sm) * (fmaxf(-m, 0.f) + tail) : 0.f) + (sm > 0.f ? sm * (fmaxf(m, 0.f) + tail) : 0.f);
+    const float small = e / (1.f + e), large = 1.f / (1.f + e);      // sigmoid(-|m|), sigmoid(|m|)
+    const float slope = p.beta / (float)pairs * (sm * (m >= 0.f ? large : small) - (1.f - sm) * (m >= 0.f ? small : large)) * a.grad_scale;
+    if (t == 0 && p.log_ratio) {
+        p.log_ratio[2 * pair] = (float)ratio[0];
+        p.log_ratio[2 * pair + 1] = (float)ratio[1];
+    }
+    for (int row = start + t; row < end; row += LANES) a.slope[row] = row < mid ? slope : -slope;
     auto outside = [&](int row) {
         a.whole[row] = make_float2(0.f, kNoRow);
         if (a.token_logprob) a.token_logprob[row] = 0.f;
     };
     if (pair == 0)
-        for (int row = threadIdx.x; row < min(start, a.n_rows); row += kTermThreads) outside(row);
+        for (int row = t; row < min(start, a.n_rows); row += LANES) outside(row);
     if (pair == pairs - 1)
-        for (int row = max(a.seq_start[a.n_seq], 0) + threadIdx.x; row < a.n_rows; row += kTermThreads) outside(row);
+        for (int row = max(a.seq_start[a.n_seq], 0) + t; row < a.n_rows; row += LANES) outside(row);
+    return make_float4(loss, m > 0.f ? 1.f : 0.f, (float)reward0, (float)reward1);
 }
 
-__global__ __launch_bounds__(kSumThreads) void pair_sum_kernel(RowArgs a, PairArgs p) {
-    __shared__ double s[kSumThreads / 64];
+template <typename T>
+__global__ __launch_bounds__(kTermThreads) void pair_kernel(RowArgs a, PairArgs p) {
+    __shared__ double s[kTermThreads / 64 + 1];
+    const float4 term = finish_pair<T, kTermThreads>(a, p, blockIdx.x, threadIdx.x, [&](double x) {
+        x = block_sum<kTermThreads / 64>(x, s);
+        if (threadIdx.x == 0) s[kTermThreads / 64] = x;
+        __syncthreads();
+        return s[kTermThreads / 64];
+    });
+    if (threadIdx.x == 0) a.terms[blockIdx.x] = term;
+}
+
+// The mean over pairs, by a workgroup of kSumThreads; s: kSumThreads / 64 doubles of LDS
+__device__ __forceinline__ void sum_pairs(const RowArgs &a, const PairArgs &p, double *s) {
     const int pairs = a.n_seq / 2;
     double x[4] = {};
     for (int i = threadIdx.x; i < pairs; i += kSumThreads) {
@@ -648,6 +698,27 @@ __global__ __launch_bounds__(kSumThreads) void pair_sum_kernel(RowArgs a, PairAr
         const double sum = block_sum<kSumThreads / 64>(x[k], s);
         if (threadIdx.x == 0) p.stats[k] = (float)(sum / pairs);
     }
+}
+__global__ __launch_bounds__(kSumThreads) void pair_sum_kernel(RowArgs a, PairArgs p) {
+    __shared__ double s[kSumThreads / 64];
+    sum_pairs(a, p, s);
+}
+
+// Both by one workgroup, a wavefront a pair: few pairs of few rows
+template <typename T>
+__global__ __launch_bounds__(kSumThreads) void pair_small_kernel(RowArgs a, PairArgs p) {
+    __shared__ double s[kSumThreads / 64];
+    const int lane = threadIdx.x & 63;
+    for (int pair = threadIdx.x >> 6; pair < a.n_seq / 2; pair += kSumThreads / 64) {
+        const float4 term = finish_pair<T, 64>(a, p, pair, lane, [](double x) {
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off, 64);
+            return x;
+        });
+        if (lane == 0) a.terms[pair] = term;
+    }
+    __syncthreads();
+    sum_pairs(a, p, s);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -696,6 +767,8 @@ RowArgs row_args(const sr_token_rows *x, const RowPlan &plan, void *workspace) {
     a.count = (int32_t *)take(4 * (size_t)x->n_seq);
     a.splits = plan.parts;
     a.split_elems = plan.elems;
+    a.grad_splits = plan.grad_parts;
+    a.grad_elems = plan.grad_elems;
     return a;
 }
 
@@ -717,7 +790,7 @@ int launch_row_stats(const RowArgs &a, int waves, hipStream_t stream) {
 }
 template <typename T>
 int launch_logit_grad(const RowArgs &a, int waves, hipStream_t stream) {
-    const int units = a.n_rows * a.splits;
+    const int units = a.n_rows * a.grad_splits;
     if (waves == 1) logit_grad_kernel<T, 1><<<dim3(ceil_div(units, 4)), dim3(row_block(1)), 0, stream>>>(a);
     else logit_grad_kernel<T, 4><<<dim3(units), dim3(row_block(4)), 0, stream>>>(a);
     SR_HIP(hipGetLastError());
@@ -725,7 +798,7 @@ int launch_logit_grad(const RowArgs &a, int waves, hipStream_t stream) {
 }
 
 int launch_row_info(const RowArgs &a, const PolicyArgs &p, hipStream_t stream) {
-    if (a.n_seq <= kMostInline && a.n_rows <= kMostInfoSmall) {
+    if (a.n_seq <= kMostInline && a.n_rows <= kMostTableRows) {
         row_info_small_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(a, p);
         SR_HIP(hipGetLastError());
         return SR_OK;
@@ -748,7 +821,7 @@ int launch_resident(const RowArgs &a, const PolicyArgs &p, int vecs, hipStream_t
         policy_resident_kernel<T, WAVES, NV, true, false><<<dim3(a.n_rows < 256 ? a.n_rows : 256), dim3(row_block(WAVES)), 0, stream>>>(a, p);
     } else {
         const int blocks = WAVES == 1 ? ceil_div(a.n_rows, 4) : a.n_rows;
-        if (a.n_rows <= kSumThreads && a.n_seq <= kMostInline) {
+        if (blocks <= kMostTableBlocks && a.n_seq <= kMostInline && a.n_rows <= kMostTableRows) {
             policy_resident_kernel<T, WAVES, NV, false, true><<<dim3(blocks), dim3(row_block(WAVES)), 0, stream>>>(a, p);
         } else {
             SR_TRY(launch_row_info(a, p, stream));
@@ -782,7 +855,7 @@ int policy_loss(const sr_token_rows *x, const PolicyArgs &p, void *workspace, hi
                 policy_rows_kernel<T><<<dim3(ceil_div(a.n_rows, kTermThreads)), dim3(kTermThreads), 0, stream>>>(a, p);
                 SR_HIP(hipGetLastError());
             }
-            return a.grad ? launch_logit_grad<T>(a, plan.waves, stream) : SR_OK;
+            return a.grad ? launch_logit_grad<T>(a, plan.grad_waves, stream) : SR_OK;
         }));
     if (a.n_rows > 0 && small) return SR_OK;
     policy_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(a, p);
@@ -796,9 +869,12 @@ int preference_loss(const sr_token_rows *x, const PairArgs &p, void *workspace, 
     return with_type(x->dtype, [&](auto *t) -> int {
         typedef std::remove_pointer_t<decltype(t)> T;
         if (a.n_rows > 0) SR_TRY(launch_row_stats<T>(a, plan.waves, stream));
-        pair_kernel<T><<<dim3(a.n_seq / 2), dim3(kTermThreads), 0, stream>>>(a, p);
+        const bool small = a.n_rows <= kMostPairRows && a.n_seq <= kMostPairSeqs;
+        if (small) pair_small_kernel<T><<<dim3(1), dim3(kSumThreads), 0, stream>>>(a, p);
+        else pair_kernel<T><<<dim3(a.n_seq / 2), dim3(kTermThreads), 0, stream>>>(a, p);
         SR_HIP(hipGetLastError());
-        if (a.n_rows > 0 && a.grad) SR_TRY(launch_logit_grad<T>(a, plan.waves, stream));
+        if (a.n_rows > 0 && a.grad) SR_TRY(launch_logit_grad<T>(a, plan.grad_waves, stream));
+        if (small) return SR_OK;
         pair_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(a, p);
         SR_HIP(hipGetLastError());
         return SR_OK;

@@ -8,19 +8,33 @@ struct RowPlan {
     int waves;           // wavefronts per row or part: 1, 4 or 16
     int resident;        // > 0: vectors of a row that a thread of the register-resident kernel holds (at most kMostResident)
     int parts, elems;    // parts of a row that the streaming kernels give to workgroups of their own, and their elements
+    int grad_waves, grad_parts, grad_elems;    // the same of the gradient
 };
 constexpr int kMostResident = 20, kMostOneWave = 8;
+constexpr int kGradPartBytes = 16384;
+
+// A row of `vecs` vectors in at most `parts` equal ones
+inline void split_row(int vecs, int per_vec, int parts, int *n, int *elems) {
+    if (parts < 1) parts = 1;
+    const int each = vecs > 0 ? ceil_div(vecs, parts) : 1;
+    *n = vecs > 0 ? ceil_div(vecs, each) : 1;
+    *elems = each * per_vec;
+}
 
 // Rows that are read twice
 inline RowPlan plan_streamed_rows(int n_rows, int vocab, int elem_bytes) {
     const int per_vec = 16 / elem_bytes, vecs = ceil_div(vocab, per_vec);
-    int parts = n_rows > 0 ? 1024 / n_rows : 1;
+    int parts = n_rows > 0 ? (n_rows < 1024 ? 1024 : 8192) / n_rows : 1;
     const int most = vecs / 512;                         // 8 KiB each at least
     if (parts > most) parts = most;
     if (parts > 64) parts = 64;
-    if (parts < 1) parts = 1;
-    const int each = ceil_div(vecs, parts);
-    return RowPlan{each <= 512 ? 1 : 4, 0, ceil_div(vecs, each), each * per_vec};
+    RowPlan p{};
+    split_row(vecs, per_vec, parts, &p.parts, &p.elems);
+    p.waves = p.elems <= 512 * per_vec ? 1 : 4;
+    const int grad_parts = n_rows < 1024 ? parts : vecs / (kGradPartBytes / 16);
+    split_row(vecs, per_vec, grad_parts, &p.grad_parts, &p.grad_elems);
+    p.grad_waves = p.grad_elems <= 512 * per_vec ? 1 : 4;
+    return p;
 }
 
 // Rows of the policy loss: held in registers between maximum and gradient where they fit
@@ -28,7 +42,9 @@ inline RowPlan plan_policy_rows(int n_rows, int vocab, int elem_bytes) {
     const int per_vec = 16 / elem_bytes, vecs = vocab / per_vec;
     const int waves = vecs <= 64 * kMostOneWave ? 1 : vecs <= 256 * kMostResident ? 4 : 16, each = ceil_div(vecs, 64 * waves);
     if (each > kMostResident || (waves == 16 && n_rows < 192)) return plan_streamed_rows(n_rows, vocab, elem_bytes);
-    return RowPlan{waves, each > 0 ? each : 1, 1, ceil_div(vocab, per_vec) * per_vec};
+    RowPlan p{waves, each > 0 ? each : 1};
+    split_row(ceil_div(vocab, per_vec), per_vec, 1, &p.parts, &p.elems);
+    return p;
 }
 
 }  // namespace sr
