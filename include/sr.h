@@ -334,8 +334,8 @@ typedef struct {
  * tokens that the clip takes out of the gradient).
  * old_logprob, ref_logprob: device float [n_rows], as sr_score_chunk writes them; ref_logprob may be NULL if kl_coef == 0.
  * advantages: device float [n_seq].
- * SR_E_ARG: null pointers, a bad dtype, shape, stride or option, a workspace that is too small or not 16-byte aligned.
- * n_rows may be 0.
+ * SR_E_ARG: null pointers, a bad dtype, shape, stride or option, a workspace that is too small or not 16-byte aligned;
+ * SR_E_LIMIT: more than 2^26 rows or 2^23 sequences.  n_rows may be 0.
  */
 typedef enum { SR_MEAN_TOKENS = 0, SR_MEAN_SEQUENCES = 1, SR_MEAN_SUMS = 2 } sr_reduce;
 typedef struct {
@@ -371,7 +371,8 @@ int sr_preference_loss(const sr_token_rows *rows, const float *ref_logprob, floa
  * allows.  `out` may be `data` itself or NULL (in place; then nothing is written where scale * c is 1) and must not overlap any
  * tensor otherwise; its type is that of the data, or SR_F32.  sr_grad_norm reads `data` only.
  * workspace: SR_GRAD_NORM_WORKSPACE bytes of device memory, 16-byte aligned.
- * SR_E_ARG: null pointers, n < 0, a bad type, scale or max_norm not finite, max_norm < 0.  The list and its tensors may be empty.
+ * SR_E_ARG: null pointers, n < 0 or > 2^36, a bad type, scale or max_norm not finite, max_norm < 0.  The list and its tensors may
+ * be empty.
  */
 typedef struct {
     void *data;

@@ -19,6 +19,8 @@ constexpr int kListTensors = 184;      // with the hidden ones 4 KB of kernel ar
 constexpr int kChunk = 8192;           // elements
 constexpr int kNormThreads = 256;
 constexpr int kMostBlocks = 1024;      // workgroups of a launch
+constexpr int64_t kMostChunks = 1 << 23;                   // of a launch: 2^31 threads
+constexpr int64_t kMostElements = kMostChunks * kChunk;    // of a tensor
 constexpr int kSlots = 2048;           // sums that the workspace holds
 constexpr int kMostSummed = 2048;      // chunks whose workgroups each add the slots up
 constexpr int64_t kKeepBytes = 256 << 20;
@@ -210,7 +212,7 @@ __global__ __launch_bounds__(kNormThreads) void scale_kernel(TensorList l, const
 }
 
 int check_tensor(const sr_tensor &t, bool clip) {
-    if (t.n < 0 || t.n >= (int64_t)1 << 43 || t.dtype < SR_F32 || t.dtype > SR_F16) return SR_E_ARG;
+    if (t.n < 0 || t.n > kMostElements || t.dtype < SR_F32 || t.dtype > SR_F16) return SR_E_ARG;
     if (t.n == 0) return SR_OK;
     if (!t.data || (uintptr_t)t.data % (t.dtype == SR_F32 ? 4 : 2) || (uintptr_t)t.data >> kAddressBits) return SR_E_ARG;
     if (!clip || !t.out) return SR_OK;
@@ -221,7 +223,7 @@ int check_tensor(const sr_tensor &t, bool clip) {
 
 int64_t tensor_bytes(const sr_tensor &t) { return t.n * (t.dtype == SR_F32 ? 4 : 2); }
 
-// A launch's share of the list: tensors from `at` on; returns where the next share begins.  The counts of chunks stay below 2^31.
+// A launch's share of the list: tensors from `at` on; returns where the next share begins.  A launch has at most kMostChunks chunks.
 int take(const sr_tensor *tensors, int n_tensors, int at, TensorList *l) {
     l->tensors = 0;
     l->first[0] = 0;
@@ -229,7 +231,7 @@ int take(const sr_tensor *tensors, int n_tensors, int at, TensorList *l) {
         const sr_tensor &t = tensors[at];
         if (t.n == 0) continue;
         const int64_t chunks = (t.n + kChunk - 1) / kChunk + l->first[l->tensors];
-        if (chunks > INT32_MAX) break;
+        if (chunks > kMostChunks) break;
         const int i = l->tensors++;
         l->data[i] = (uint64_t)(uintptr_t)t.data | (uint64_t)(t.n % kChunk) << kAddressBits | (uint64_t)t.dtype << kTypeShift;
         l->out[i] = (uint64_t)(uintptr_t)(t.out ? t.out : t.data) | (uint64_t)(t.out ? t.out_dtype : t.dtype) << kTypeShift;

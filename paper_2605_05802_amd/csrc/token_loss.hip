@@ -23,6 +23,7 @@ namespace {
 
 constexpr int kTermThreads = 256;
 constexpr int kSumThreads = 1024;
+constexpr int kMostSummedRows = 16384, kShares = 256;      // rows whose terms one workgroup adds; else the workgroups that add them
 constexpr int kMostInline = 1024;      // sequences of a small call
 constexpr int kMostTableRows = 4096;   // its rows
 constexpr int kMostTableBlocks = 512;  // workgroups that look the weights up for themselves
@@ -106,7 +107,7 @@ struct RowArgs {
     float2 *info;        // [n_rows] policy: weight (0: does not count), advantage
     float *slope;        // [n_rows], grad_scale included
     float4 *terms;       // [n_rows] policy: surrogate, kl, clipped, weight; [n_seq / 2] pairs: loss, m > 0, rewards
-    int32_t *count;      // [n_seq] counting rows
+    int32_t *count;      // [n_seq + 2] counting rows of the sequences, of all, and the number of sequences that have any
 };
 
 // s of a row that does not count
@@ -243,21 +244,64 @@ struct PolicyArgs {
     float *stats;
 };
 
-// counting rows of a sequence, a wavefront each
-__device__ __forceinline__ int count_rows(const RowArgs &a, int seq, int lane) {
-    const int from = max(a.seq_start[seq], 0), to = min(a.seq_start[seq + 1], a.n_rows);
-    if (!a.mask) return max(to - from, 0);
-    int n = 0;
-    for (int r = from + lane; r < to; r += 64) n += a.mask[r] != 0;
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) n += __shfl_xor(n, off, 64);
-    return n;
+// One bit for every byte of a word that is not zero
+__device__ __forceinline__ unsigned set_bytes(unsigned w) {
+    const unsigned top = (((w & 0x7f7f7f7fu) + 0x7f7f7f7fu) | w) & 0x80808080u;
+    return ((top >> 7) * 0x10204080u) >> 28;                 // bits 0, 8, 16, 24 to 28 .. 31, the other products apart from each other
 }
-__global__ __launch_bounds__(256) void seq_count_kernel(RowArgs a) {
-    const int seq = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (seq >= a.n_seq) return;
-    const int n = count_rows(a, seq, lane);
-    if (lane == 0) a.count[seq] = n;
+// ... and for sixteen bytes of a mask
+__device__ __forceinline__ unsigned set_bytes_16(const uint8_t *p) {
+    typedef uint32_t raw16_bytes __attribute__((ext_vector_type(4), aligned(1)));
+    const raw16 m = *(const raw16_bytes *)p;
+    return set_bytes(m[0]) | set_bytes(m[1]) << 4 | set_bytes(m[2]) << 8 | set_bytes(m[3]) << 12;
+}
+// Sums of two whole numbers over the wavefronts of a workgroup, into LDS
+__device__ __forceinline__ void add_up(int n, int some, int *rows, int *used) {
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) {
+        n += __shfl_xor(n, off, 64);
+        some += __shfl_xor(some, off, 64);
+    }
+    if ((threadIdx.x & 63) == 0) {
+        atomicAdd(rows, n);                                  // whole numbers: the order does not matter
+        atomicAdd(used, some);
+    }
+}
+
+// counting rows of a sequence, a workgroup each
+__global__ __launch_bounds__(kTermThreads) void seq_count_kernel(RowArgs a) {
+    __shared__ int s_n, s_unused;
+    const int seq = blockIdx.x, t = threadIdx.x;
+    const int from = max(a.seq_start[seq], 0), to = min(a.seq_start[seq + 1], a.n_rows);
+    if (!a.mask) {
+        if (t == 0) a.count[seq] = max(to - from, 0);
+        return;
+    }
+    if (t == 0) s_n = s_unused = 0;
+    __syncthreads();
+    int n = 0;
+    for (int r = from + 16 * t; r < to; r += 16 * kTermThreads) {
+        if (r + 16 <= to) n += __popc(set_bytes_16(a.mask + r));
+        else
+            for (int i = r; i < to; ++i) n += a.mask[i] != 0;
+    }
+    add_up(n, 0, &s_n, &s_unused);
+    __syncthreads();
+    if (t == 0) a.count[seq] = s_n;
+}
+// behind the counts of the sequences: their sum, and the number of those that are not 0
+__global__ __launch_bounds__(kSumThreads) void seq_total_kernel(RowArgs a) {
+    __shared__ int s[2];
+    if (threadIdx.x < 2) s[threadIdx.x] = 0;
+    __syncthreads();
+    int n = 0, some = 0;
+    for (int i = threadIdx.x; i < a.n_seq; i += kSumThreads) {
+        n += a.count[i];
+        some += a.count[i] > 0;
+    }
+    add_up(n, some, &s[0], &s[1]);
+    __syncthreads();
+    if (threadIdx.x < 2) a.count[a.n_seq + threadIdx.x] = s[threadIdx.x];
 }
 
 // Weight and advantage of a counting row.  count: its sequence's counting rows; rows, used: those of all sequences, and the sequences
@@ -267,12 +311,6 @@ __device__ __forceinline__ float2 row_info(const PolicyArgs &p, int seq, int cou
                     : p.reduce == SR_MEAN_SEQUENCES ? 1.f / ((float)used * (float)count)
                                                     : 1.f / (float)used;
     return make_float2(w, p.advantages[seq]);
-}
-
-// One bit for every byte of a word that is not zero
-__device__ __forceinline__ unsigned set_bytes(unsigned w) {
-    const unsigned top = (((w & 0x7f7f7f7fu) + 0x7f7f7f7fu) | w) & 0x80808080u;
-    return ((top >> 7) * 0x10204080u) >> 28;                 // bits 0, 8, 16, 24 to 28 .. 31, the other products apart from each other
 }
 
 // The sequences of a small call in LDS.  Counting rows in front of a row: sixteen rows of the mask are a word of bits, with the number
@@ -297,8 +335,7 @@ struct SeqTable {
             if (t < 256) {
                 const int n = a.n_rows - 16 * t;
                 if (n >= 16) {
-                    const raw16 m = load_vec((const __bf16 *)(a.mask + 16 * t));
-                    mine = set_bytes(m[0]) | set_bytes(m[1]) << 4 | set_bytes(m[2]) << 8 | set_bytes(m[3]) << 12;
+                    mine = set_bytes_16(a.mask + 16 * t);
                 } else {
                     for (int i = 0; i < n; ++i) mine |= (unsigned)(a.mask[16 * t + i] != 0) << i;
                 }
@@ -335,17 +372,6 @@ struct SeqTable {
         add_up(n, some, &rows, &used);
         __syncthreads();
     }
-    static __device__ __forceinline__ void add_up(int n, int some, int *rows, int *used) {
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) {
-            n += __shfl_xor(n, off, 64);
-            some += __shfl_xor(some, off, 64);
-        }
-        if ((threadIdx.x & 63) == 0) {
-            atomicAdd(rows, n);
-            atomicAdd(used, some);
-        }
-    }
     __device__ __forceinline__ float2 info(const RowArgs &a, const PolicyArgs &p, int row) const {
         const int seq = !a.mask || a.mask[row] ? sequence_of(start, a.n_seq, row) : -1;
         return seq < 0 ? make_float2(0.f, 0.f) : row_info(p, seq, count[seq], rows, used);
@@ -353,22 +379,12 @@ struct SeqTable {
 };
 
 __global__ __launch_bounds__(kTermThreads) void row_info_kernel(RowArgs a, PolicyArgs p) {
-    __shared__ int s_rows, s_used;
-    if (threadIdx.x == 0) s_rows = s_used = 0;
-    __syncthreads();
-    int n = 0, some = 0;                                     // of all sequences, by every workgroup for itself
-    for (int i = threadIdx.x; i < a.n_seq; i += kTermThreads) {
-        n += a.count[i];
-        some += a.count[i] > 0;
-    }
-    SeqTable::add_up(n, some, &s_rows, &s_used);
-    __syncthreads();
     const int row = blockIdx.x * kTermThreads + threadIdx.x;
     if (row >= a.n_rows) return;
     const int seq = !a.mask || a.mask[row] ? sequence_of(a.seq_start, a.n_seq, row) : -1;
-    a.info[row] = seq < 0 ? make_float2(0.f, 0.f) : row_info(p, seq, a.count[seq], s_rows, s_used);
+    a.info[row] = seq < 0 ? make_float2(0.f, 0.f) : row_info(p, seq, a.count[seq], a.count[a.n_seq], a.count[a.n_seq + 1]);
 }
-// seq_count_kernel and row_info_kernel by one workgroup
+// The same three by one workgroup
 __global__ __launch_bounds__(kSumThreads) void row_info_small_kernel(RowArgs a, PolicyArgs p) {
     __shared__ SeqTable table;
     table.fill<kSumThreads>(a);
@@ -413,8 +429,8 @@ struct PolicySums {
         kl += (double)t.w * (double)t.y;
         out += (double)t.w * (double)t.z;
     }
-    // over the workgroup; s: 3 * kSumThreads / 64 doubles of LDS
-    __device__ __forceinline__ void finish(const PolicyArgs &p, double *s) {
+    // over the workgroup, valid in thread 0; s: 3 * kSumThreads / 64 doubles of LDS
+    __device__ __forceinline__ void gather(double *s) {
         constexpr int WAVES = kSumThreads / 64;
 #pragma unroll
         for (int off = 32; off >= 1; off >>= 1) {
@@ -440,6 +456,9 @@ struct PolicySums {
             kl += __shfl_xor(kl, off, 64);
             out += __shfl_xor(out, off, 64);
         }
+    }
+    __device__ __forceinline__ void finish(const PolicyArgs &p, double *s) {
+        gather(s);
         if (threadIdx.x != 0) return;
         p.stats[0] = (float)((p.kl_coef != 0.f ? (double)p.kl_coef * kl : 0.0) - surrogate);
         p.stats[1] = (float)surrogate;
@@ -473,6 +492,21 @@ __global__ __launch_bounds__(kSumThreads) void policy_sum_kernel(RowArgs a, Poli
     __shared__ double s[3 * kSumThreads / 64];
     PolicySums sums;
     for (int i = threadIdx.x; i < a.n_rows; i += kSumThreads) sums.add(a.terms[i]);
+    sums.finish(p, s);
+}
+// The same in two steps, for more rows than one workgroup adds in the time of a launch: a share of them each, then the shares
+__global__ __launch_bounds__(kSumThreads) void policy_share_kernel(RowArgs a, PolicySums *shares) {
+    __shared__ double s[3 * kSumThreads / 64];
+    PolicySums sums;
+    const int each = (a.n_rows + gridDim.x - 1) / gridDim.x, from = blockIdx.x * each, to = min(from + each, a.n_rows);
+    for (int i = from + threadIdx.x; i < to; i += kSumThreads) sums.add(a.terms[i]);
+    sums.gather(s);
+    if (threadIdx.x == 0) shares[blockIdx.x] = sums;
+}
+__global__ __launch_bounds__(kSumThreads) void policy_shares_kernel(PolicyArgs p, const PolicySums *shares, int n) {
+    __shared__ double s[3 * kSumThreads / 64];
+    PolicySums sums;
+    if ((int)threadIdx.x < n) sums = shares[threadIdx.x];
     sums.finish(p, s);
 }
 
@@ -728,6 +762,7 @@ int check_rows(const sr_token_rows *x, const void *workspace, size_t bytes) {
     if (!x || !workspace || (uintptr_t)workspace % 16) return SR_E_ARG;
     if (x->dtype < SR_F32 || x->dtype > SR_F16 || x->n_rows < 0 || x->vocab < 1 || x->n_seq < 1) return SR_E_ARG;
     if (x->vocab > 1 << 30 || !x->seq_start || !std::isfinite(x->grad_scale)) return SR_E_ARG;
+    if (x->n_rows > 1 << 26 || x->n_seq > 1 << 23) return SR_E_LIMIT;     // threads of a launch
     if (bytes < SR_TOKEN_LOSS_WORKSPACE(x->n_rows, x->n_seq)) return SR_E_ARG;
     if (x->n_rows == 0) return SR_OK;
     const unsigned elem = x->dtype == SR_F32 ? 4 : 2;
@@ -764,7 +799,7 @@ RowArgs row_args(const sr_token_rows *x, const RowPlan &plan, void *workspace) {
     a.whole = (float2 *)take(8 * rows);
     a.info = (float2 *)take(8 * rows);
     a.slope = (float *)take(4 * rows);
-    a.count = (int32_t *)take(4 * (size_t)x->n_seq);
+    a.count = (int32_t *)take(4 * ((size_t)x->n_seq + 2));
     a.splits = plan.parts;
     a.split_elems = plan.elems;
     a.grad_splits = plan.grad_parts;
@@ -803,7 +838,9 @@ int launch_row_info(const RowArgs &a, const PolicyArgs &p, hipStream_t stream) {
         SR_HIP(hipGetLastError());
         return SR_OK;
     }
-    seq_count_kernel<<<dim3(ceil_div(a.n_seq, 4)), dim3(256), 0, stream>>>(a);
+    seq_count_kernel<<<dim3(a.n_seq), dim3(kTermThreads), 0, stream>>>(a);
+    SR_HIP(hipGetLastError());
+    seq_total_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(a);
     SR_HIP(hipGetLastError());
     row_info_kernel<<<dim3(ceil_div(a.n_rows, kTermThreads)), dim3(kTermThreads), 0, stream>>>(a, p);
     SR_HIP(hipGetLastError());
@@ -858,7 +895,14 @@ int policy_loss(const sr_token_rows *x, const PolicyArgs &p, void *workspace, hi
             return a.grad ? launch_logit_grad<T>(a, plan.grad_waves, stream) : SR_OK;
         }));
     if (a.n_rows > 0 && small) return SR_OK;
-    policy_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(a, p);
+    if (a.n_rows > kMostSummedRows) {
+        PolicySums *shares = (PolicySums *)a.part;           // 64 KiB at least, and no longer read
+        policy_share_kernel<<<dim3(kShares), dim3(kSumThreads), 0, stream>>>(a, shares);
+        SR_HIP(hipGetLastError());
+        policy_shares_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(p, shares, kShares);
+    } else {
+        policy_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(a, p);
+    }
     SR_HIP(hipGetLastError());
     return SR_OK;
 }

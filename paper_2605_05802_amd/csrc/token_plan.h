@@ -37,11 +37,15 @@ inline RowPlan plan_streamed_rows(int n_rows, int vocab, int elem_bytes) {
     return p;
 }
 
-// Rows of the policy loss: held in registers between maximum and gradient where they fit
+// Rows of the policy loss: held in registers between maximum and gradient where they fit.  Rows of sixteen wavefronts are one to a
+// compute unit: below 112 of them too few compute units work (64 rows of 152064 bf16: 28 us, streamed 21; 128: 28 and 28; 192: 30 and 39),
+// and a few more than 256 wait for a second round (300 rows of 152064 bf16: 57 us, streamed 52; of 50000: 30 and 24; 384: 58 and 63;
+// of 64000 fp32, which take longer in either way, 42 and 47).
 inline RowPlan plan_policy_rows(int n_rows, int vocab, int elem_bytes) {
     const int per_vec = 16 / elem_bytes, vecs = vocab / per_vec;
     const int waves = vecs <= 64 * kMostOneWave ? 1 : vecs <= 256 * kMostResident ? 4 : 16, each = ceil_div(vecs, 64 * waves);
-    if (each > kMostResident || (waves == 16 && n_rows < 192)) return plan_streamed_rows(n_rows, vocab, elem_bytes);
+    const bool uneven = n_rows < 112 || (elem_bytes == 2 && n_rows > 256 && n_rows <= 320);
+    if (each > kMostResident || (waves == 16 && uneven)) return plan_streamed_rows(n_rows, vocab, elem_bytes);
     RowPlan p{waves, each > 0 ? each : 1};
     split_row(ceil_div(vocab, per_vec), per_vec, 1, &p.parts, &p.elems);
     return p;

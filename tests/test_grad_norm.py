@@ -117,6 +117,30 @@ def test_more_tensors_than_any_launch_takes():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,out", [(F32, F32), (BF16, BF16), (BF16, F32), (F16, F16)])
+@pytest.mark.parametrize("shift", [0, 1, 3])
+def test_nothing_but_the_outputs_is_written(dtype, out, shift):
+    sizes = [1, 8192, 5, 8191, 20000, 3]
+    ts = tensors_of(sizes, [dtype], 9, shift=shift)
+    before = [t.clone() for t in ts]
+    buf = torch.full((sum(sizes) + 16 * len(sizes) + 64,), 3.0, dtype=out, device="cuda")
+    outs, at, gaps = [], shift, torch.ones_like(buf, dtype=torch.bool)
+    for n in sizes:
+        outs.append(buf[at:at + n])
+        gaps[at:at + n] = False
+        at += n + 3
+    norm = torch.full((3,), 7.0, device="cuda")
+    ws = torch.full((sr.GRAD_NORM_WORKSPACE + 512,), 77, dtype=torch.uint8, device="cuda")
+    want = norm_of(ts)
+    sr.sr_clip_grad_norm(sr.tensor_list(ts, outs), 0.5 * want, norm[1:2], ws[:sr.GRAD_NORM_WORKSPACE])
+    for o, t in zip(outs, ts):
+        e = t.double() * 0.5
+        assert bool(((o.double() - e).abs() <= e.abs() * (4 * U + ROUND[out]) + SMALLEST[out]).all())
+    assert bool((buf[gaps] == 3.0).all()) and all(torch.equal(a, b) for a, b in zip(ts, before))
+    assert norm[0].item() == norm[2].item() == 7.0 and bool((ws[sr.GRAD_NORM_WORKSPACE:] == 77).all())
+
+
+@pytest.mark.gpu
 def test_nothing_at_all():
     norm, ws = work()
     sr.sr_clip_grad_norm([], 1.0, norm, ws)
@@ -178,7 +202,7 @@ def test_refusals():
         a, n, scale, limit, norm, ws, size, None)
     for r in (clip(a=None), clip(n=-1), clip(scale=math.nan), clip(limit=math.inf), clip(limit=-1.0), clip(norm=None), clip(ws=None),
               clip(ws=ctypes.c_void_p(4100)), clip(size=sr.GRAD_NORM_WORKSPACE - 1), clip(a=one(data=None)), clip(a=one(data=4098)),
-              clip(a=one(n=-1)), clip(a=one(n=1 << 50)), clip(a=one(dtype=3)), clip(a=one(dtype=1, out=8192, out_dtype=2)),
+              clip(a=one(n=-1)), clip(a=one(n=1 << 50)), clip(a=one(n=(1 << 36) + 1)), clip(a=one(dtype=3)), clip(a=one(dtype=1, out=8192, out_dtype=2)),
               clip(a=one(out=8192, out_dtype=1)), clip(a=one(dtype=1, out=8193, out_dtype=1)), clip(a=one(dtype=1, out=4096, out_dtype=0))):
         assert r == sr.SR_E_ARG
     assert L.sr_grad_norm(one(data=None), 1, 1.0, fake, fake, sr.GRAD_NORM_WORKSPACE, None) == sr.SR_E_ARG

@@ -415,6 +415,53 @@ def test_preference_gradient_against_differences():
 # both
 # ---------------------------------------------------------------------------------------------
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,n_seq,vocab", [(20011, 3, 40), (20000, 1, 17), (33001, 2, 300), (5000, 3001, 50), (4097, 1024, 600), (4096, 1024, 2100),
+                                              (1100, 1100, 6001), (2049, 40, 9001)])
+@pytest.mark.parametrize("masked", [0.0, 0.4])
+def test_many_rows_and_many_sequences(rows, n_seq, vocab, masked):
+    """On both sides of the numbers of rows and sequences up to which one workgroup counts, looks weights up and adds."""
+    x = make(rows, n_seq, vocab, torch.bfloat16, 11, masked=masked, lead=1, tail=2)
+    for reduce in ("tokens", "sequences", "sums"):
+        check_policy(x, reduce, 0.04)
+    run = run_policy(x, "sequences", 0.04, grad=False)
+    assert torch.equal(run[0], run_policy(x, "sequences", 0.04)[0])
+    if n_seq % 2 == 0:
+        check_pairs(x, 0.1, 0.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n_seq,vocab", [(7, 2, 100), (3, 2, 50003), (40, 4, 2049), (300, 8, 30001), (260, 2, 90001), (1030, 4, 9999)])
+@pytest.mark.parametrize("shift", [0, 1, 5])
+def test_nothing_but_the_outputs_is_written(dtype, rows, n_seq, vocab, shift):
+    """Columns between the gradient's rows, elements in front of and behind it, bytes behind the workspace and the small outputs."""
+    x = make(rows, n_seq, vocab, dtype, 13, pad=3, masked=0.2)
+    ld = vocab + 7
+    for pairs in (False, True):
+        buf = torch.full((rows * ld + 64,), 3.0, dtype=dtype, device="cuda")
+        g = buf[shift:shift + rows * ld].view(rows, ld)[:, :vocab]
+        need = sr.token_loss_workspace(rows, n_seq)
+        ws = torch.full((need + 4096,), 77, dtype=torch.uint8, device="cuda")
+        small = torch.full((4 + rows + n_seq + 16,), 5.0, device="cuda")
+        stats, lp, lr = small[:4], small[4:4 + rows], small[4 + rows:4 + rows + n_seq]
+        before = x["logits"].clone()
+        if pairs:
+            sr.sr_preference_loss(x["logits"], x["targets"], x["seq_start"], stats, ws[:need], mask=x["mask"], ref_logprob=x["ref_logprob"],
+                                  grad=g, token_logprob=lp, log_ratio=lr)
+            check_grad(g, pairs_reference(x, 0.1, 0.0, True, 1.0))
+        else:
+            sr.sr_policy_loss(x["logits"], x["targets"], x["seq_start"], x["old_logprob"], x["advantages"], stats, ws[:need], mask=x["mask"],
+                              ref_logprob=x["ref_logprob"], grad=g, token_logprob=lp, clip_low=LOW, clip_high=HIGH, kl_coef=0.04)
+            check_grad(g, policy_reference(x, "tokens", 0.04, True))
+            assert bool((lr == 5.0).all())
+        assert bool((ws[need:] == 77).all()) and bool((small[4 + rows + n_seq:] == 5.0).all())
+        rest = buf.clone()
+        rest[shift:shift + rows * ld].view(rows, ld)[:, :vocab] = 3.0
+        assert bool((rest == 3.0).all())
+        assert torch.equal(before, x["logits"])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("rows,vocab", [(20, 900), (6, 60001), (300, 30001)])
 def test_side_streams_repetitions_and_graphs(rows, vocab):
     """Bit-identical from call to call, on another stream, and in every replay of a captured graph, also with new inputs."""
@@ -463,7 +510,7 @@ def _rows(**kw):
 
 @pytest.mark.parametrize("bad", [dict(logits=None), dict(targets=None), dict(seq_start=None), dict(dtype=3), dict(dtype=-1), dict(n_rows=-1), dict(vocab=0),
                                  dict(n_seq=0), dict(ld_logits=99), dict(ld_grad=99), dict(logits=4097), dict(grad=8193), dict(grad_scale=math.nan),
-                                 dict(dtype=0, logits=4098), dict(grad=4096, ld_grad=104)])
+                                 dict(dtype=0, logits=4098), dict(grad=4096, ld_grad=104), dict(vocab=(1 << 30) + 1, ld_logits=1 << 31, ld_grad=1 << 31)])
 def test_refusals_of_rows(bad):
     L, fake = sr.lib(), ctypes.c_void_p(4096)                      # never dereferenced: validation fails first
     big = 1 << 20
@@ -489,6 +536,53 @@ def test_refusals_of_options_and_workspaces():
     q = lambda r=rows, beta=0.1, s=0.0, stats=fake, n=big: L.sr_preference_loss(r, None, beta, s, None, stats, fake, n, None)
     assert q(r=ctypes.byref(_rows(n_seq=3))) == q(beta=math.inf) == q(s=-0.1) == q(s=1.1) == q(s=math.nan) == sr.SR_E_ARG
     assert q(stats=None) == q(n=need - 1) == q(r=None) == sr.SR_E_ARG
+
+
+def test_sizes_beyond_a_launch():
+    L, fake = sr.lib(), ctypes.c_void_p(4096)
+    opt = sr.PolicyOptions(0.2, 0.2, 0.0, 0)
+    for bad in (dict(n_rows=(1 << 26) + 1), dict(n_seq=(1 << 23) + 2)):
+        rows = ctypes.byref(_rows(**bad))
+        assert L.sr_policy_loss(rows, fake, None, fake, ctypes.byref(opt), fake, fake, 1 << 40, None) == sr.SR_E_LIMIT
+        assert L.sr_preference_loss(rows, fake, 0.1, 0.0, None, fake, fake, 1 << 40, None) == sr.SR_E_LIMIT
+
+
+RULES = """
+#include "token_plan.h"
+extern "C" void rows_plan(int policy, int n_rows, int vocab, int bytes, int *out) {
+    const sr::RowPlan p = policy ? sr::plan_policy_rows(n_rows, vocab, bytes) : sr::plan_streamed_rows(n_rows, vocab, bytes);
+    const int v[] = {p.waves, p.resident, p.parts, p.elems, p.grad_waves, p.grad_parts, p.grad_elems};
+    for (int i = 0; i < 7; ++i) out[i] = v[i];
+}
+"""
+
+
+def test_parts_cover_rows_and_fit_the_workspace(tmp_path):
+    """Over sizes around every limit: parts are whole vectors, cover the row exactly, are none of them empty, and number at most what
+    the workspace holds; a resident row fits the registers that its kernel has."""
+    import subprocess
+    from paper_2605_05802_amd.build import CSRC
+    (tmp_path / "rules.cpp").write_text(RULES)
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I" + CSRC, str(tmp_path / "rules.cpp"), "-o", str(tmp_path / "rules.so")])
+    lib, out = ctypes.CDLL(str(tmp_path / "rules.so")), (ctypes.c_int * 7)()
+    rng = np.random.default_rng(0)
+    vocabs = sorted({1, 2, 7, 8, 9, 4095, 4096, 4097, 40959, 40960, 40961, 81920, 81921, 163839, 163840, 163841, 152064, 1 << 20, 1 << 30,
+                     *np.exp(rng.uniform(0, math.log(1 << 21), 200)).astype(int).tolist()})
+    for n_rows in (1, 2, 3, 100, 111, 112, 191, 256, 257, 320, 321, 1000, 1023, 1024, 1025, 4096, 8192, 8193, 100000, 1 << 26):
+        for vocab in vocabs:
+            for size in (2, 4):
+                for policy in (0, 1):
+                    lib.rows_plan(policy, n_rows, vocab, size, out)
+                    waves, resident, parts, elems, grad_waves, grad_parts, grad_elems = out
+                    per = 16 // size
+                    assert waves in (1, 4, 16) and parts >= 1 and elems % per == 0
+                    assert (parts - 1) * elems < vocab <= parts * elems
+                    assert parts == 1 or parts * n_rows <= 8192
+                    if resident:
+                        assert policy and parts == 1 and resident <= (8 if waves == 1 else 20)
+                        assert 64 * waves * (resident - 1) < max(vocab // per, 1) <= 64 * waves * resident
+                    else:
+                        assert grad_waves in (1, 4) and grad_elems % per == 0 and (grad_parts - 1) * grad_elems < vocab <= grad_parts * grad_elems
 
 
 def test_the_binding_refuses_wrong_tensors():
