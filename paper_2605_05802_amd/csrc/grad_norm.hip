@@ -162,9 +162,10 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(double *slots, int u
     *norm = (float)(fabs((double)scale) * sqrt(sum));
 }
 
-// Four elements a thread and step where 16-bit data become single precision, so that whole lines are written at once
-template <typename T, typename U, bool WHOLE>
-__device__ __forceinline__ void scale_some(const T *p, U *q, int n, float c) {
+// Four elements a thread and step where 16-bit data become single precision, so that whole lines are written at once.
+// factor(): what to multiply by, asked for when the loads are under way.
+template <typename T, typename U, bool WHOLE, typename F>
+__device__ __forceinline__ void scale_some(const T *p, U *q, int n, F &&factor) {
     constexpr bool WIDER = sizeof(U) > sizeof(T);
     constexpr int N = Elem<U>::kPerVec;
     raw16 raw[kChunk / (kNormThreads * N)];
@@ -177,7 +178,10 @@ __device__ __forceinline__ void scale_some(const T *p, U *q, int n, float c) {
         }
     });
     const int rest = n / N * N + (int)threadIdx.x;
-    if (!WHOLE && rest < n) q[rest] = (U)((float)p[rest] * c);
+    float last = 0.f;
+    if (!WHOLE && rest < n) last = (float)p[rest];
+    const float c = factor();
+    if (!WHOLE && rest < n) q[rest] = (U)(last * c);
     each_vector<N, WHOLE>(n, [&](int j, int e) __attribute__((always_inline)) {
         float x[Elem<T>::kPerVec];
         Elem<T>::widen(raw[j], x);
@@ -186,10 +190,10 @@ __device__ __forceinline__ void scale_some(const T *p, U *q, int n, float c) {
         store_vec_once(q + e, Elem<U>::narrow(x));
     });
 }
-template <typename T, typename U>
-__device__ __forceinline__ void scale_chunk(const T *p, U *q, int n, float c) {
-    if (n == kChunk) scale_some<T, U, true>(p, q, n, c);
-    else scale_some<T, U, false>(p, q, n, c);
+template <typename T, typename U, typename F>
+__device__ __forceinline__ void scale_chunk(const Chunk &k, F &&factor) {
+    if (k.n == kChunk) scale_some<T, U, true>((const T *)k.data, (U *)k.out, k.n, factor);
+    else scale_some<T, U, false>((const T *)k.data, (U *)k.out, k.n, factor);
 }
 
 // One chunk a workgroup, in the order of the list: 2 GB of bf16 in 657 us, 732 with 1024 workgroups that take chunks in turn
@@ -197,18 +201,24 @@ __global__ __launch_bounds__(kNormThreads) void scale_kernel(TensorList l, const
                                                              float max_norm, float *__restrict__ norm_out) {
     __shared__ double s[kNormThreads / 64 + 1];
     const Chunk k = find_chunk(l, blockIdx.x);
-    const double norm = fabs((double)scale) * sqrt(sum_slots(slots, used, s));
-    if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
-    // a quotient of doubles, rounded once; false for NaN
-    const float c = norm > (double)max_norm && norm <= DBL_MAX ? (float)((double)scale * ((double)max_norm / norm)) : scale;
-    if (k.data == k.out && c == 1.f) return;
-    switch (k.type * 4 + k.out_type) {
-        case SR_F32 * 4 + SR_F32: scale_chunk((const float *)k.data, (float *)k.out, k.n, c); break;
-        case SR_BF16 * 4 + SR_F32: scale_chunk((const __bf16 *)k.data, (float *)k.out, k.n, c); break;
-        case SR_F16 * 4 + SR_F32: scale_chunk((const f16_t *)k.data, (float *)k.out, k.n, c); break;
-        case SR_BF16 * 4 + SR_BF16: scale_chunk((const __bf16 *)k.data, (__bf16 *)k.out, k.n, c); break;
-        case SR_F16 * 4 + SR_F16: scale_chunk((const f16_t *)k.data, (f16_t *)k.out, k.n, c); break;
-    }
+    auto factor = [&]() __attribute__((always_inline)) {     // holds barriers: once, by the whole workgroup
+        const double norm = fabs((double)scale) * sqrt(sum_slots(slots, used, s));
+        if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
+        // a quotient of doubles, rounded once; false for NaN
+        return norm > (double)max_norm && norm <= DBL_MAX ? (float)((double)scale * ((double)max_norm / norm)) : scale;
+    };
+    auto scale_by = [&](auto &&f) __attribute__((always_inline)) {
+        switch (k.type * 4 + k.out_type) {
+            case SR_F32 * 4 + SR_F32: scale_chunk<float, float>(k, f); break;
+            case SR_BF16 * 4 + SR_F32: scale_chunk<__bf16, float>(k, f); break;
+            case SR_F16 * 4 + SR_F32: scale_chunk<f16_t, float>(k, f); break;
+            case SR_BF16 * 4 + SR_BF16: scale_chunk<__bf16, __bf16>(k, f); break;
+            case SR_F16 * 4 + SR_F16: scale_chunk<f16_t, f16_t>(k, f); break;
+        }
+    };
+    if (k.data != k.out) return scale_by(factor);
+    const float c = factor();                                // in place: nothing is read where nothing changes
+    if (c != 1.f) scale_by([&]() { return c; });
 }
 
 int check_tensor(const sr_tensor &t, bool clip) {
