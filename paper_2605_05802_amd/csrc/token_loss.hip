@@ -26,6 +26,7 @@ constexpr int kSumThreads = 1024;
 constexpr int kMostSummedRows = 16384, kShares = 256;      // rows whose terms one workgroup adds; else the workgroups that add them
 constexpr int kMostInline = 1024;      // sequences of a small call
 constexpr int kMostTableRows = 4096;   // its rows
+constexpr int kMostSmallRows = 2048;   // rows whose slopes and terms one workgroup computes
 constexpr int kMostTableBlocks = 512;  // workgroups that look the weights up for themselves
 constexpr int kMostPairRows = 512, kMostPairSeqs = 32;     // of a small call of the preference loss
 constexpr int kParts = 8192;           // parts of rows that the workspace holds
@@ -138,8 +139,8 @@ __device__ __forceinline__ float logit_of(const RowArgs &a, int row, int v) {
 // The threads and wavefronts of a workgroup for rows of WAVES wavefronts: four rows of one each
 constexpr int row_block(int waves) { return waves == 1 ? 256 : 64 * waves; }
 
-// WAVES wavefronts per (row, part).  Four vectors in flight per thread.
-template <typename T, int WAVES>
+// WAVES wavefronts per (row, part).  Four vectors in flight per thread.  ONCE: no gradient follows, the logits are not read again.
+template <typename T, int WAVES, bool ONCE>
 __global__ __launch_bounds__(row_block(WAVES)) void row_stats_kernel(RowArgs a) {
     constexpr int N = Elem<T>::kPerVec, LANES = 64 * WAVES, DEPTH = 4;
     __shared__ RowSum s_part[16];
@@ -160,13 +161,13 @@ __global__ __launch_bounds__(row_block(WAVES)) void row_stats_kernel(RowArgs a) 
     int e = from + t * N;
     for (; e + (DEPTH - 1) * LANES * N < full; e += DEPTH * LANES * N) {
 #pragma unroll
-        for (int j = 0; j < DEPTH; ++j) raw[j] = load_vec(x + e + j * LANES * N);
+        for (int j = 0; j < DEPTH; ++j) raw[j] = ONCE ? load_vec_once(x + e + j * LANES * N) : load_vec(x + e + j * LANES * N);
         add_vectors<T, DEPTH>(r, raw);
     }
     if (e < full) {
 #pragma unroll
         for (int j = 0; j < DEPTH; ++j)
-            raw[j] = e + j * LANES * N < full ? load_vec(x + e + j * LANES * N) : raw16(Elem<T>::kMinusInf);
+            raw[j] = e + j * LANES * N >= full ? raw16(Elem<T>::kMinusInf) : ONCE ? load_vec_once(x + e + j * LANES * N) : load_vec(x + e + j * LANES * N);
         add_vectors<T, DEPTH>(r, raw);
     }
     r = merge_lanes<64>(r);
@@ -814,14 +815,18 @@ int with_type(int dtype, F &&f) {
     return f((f16_t *)nullptr);
 }
 
-template <typename T>
+template <typename T, bool ONCE>
 int launch_row_stats(const RowArgs &a, int waves, hipStream_t stream) {
     const int units = a.n_rows * a.splits;
-    if (waves == 1) row_stats_kernel<T, 1><<<dim3(ceil_div(units, 4)), dim3(row_block(1)), 0, stream>>>(a);
-    else if (waves == 4) row_stats_kernel<T, 4><<<dim3(units), dim3(row_block(4)), 0, stream>>>(a);
-    else row_stats_kernel<T, 16><<<dim3(units), dim3(row_block(16)), 0, stream>>>(a);
+    if (waves == 1) row_stats_kernel<T, 1, ONCE><<<dim3(ceil_div(units, 4)), dim3(row_block(1)), 0, stream>>>(a);
+    else if (waves == 4) row_stats_kernel<T, 4, ONCE><<<dim3(units), dim3(row_block(4)), 0, stream>>>(a);
+    else row_stats_kernel<T, 16, ONCE><<<dim3(units), dim3(row_block(16)), 0, stream>>>(a);
     SR_HIP(hipGetLastError());
     return SR_OK;
+}
+template <typename T>
+int launch_row_stats(const RowArgs &a, int waves, hipStream_t stream) {
+    return a.grad ? launch_row_stats<T, false>(a, waves, stream) : launch_row_stats<T, true>(a, waves, stream);
 }
 template <typename T>
 int launch_logit_grad(const RowArgs &a, int waves, hipStream_t stream) {
@@ -878,7 +883,7 @@ int launch_resident(const RowArgs &a, const PolicyArgs &p, int waves, int vecs, 
 int policy_loss(const sr_token_rows *x, const PolicyArgs &p, void *workspace, hipStream_t stream) {
     const RowPlan plan = plan_policy_rows(x->n_rows, x->vocab, x->dtype == SR_F32 ? 4 : 2);
     const RowArgs a = row_args(x, plan, workspace);
-    const bool small = a.n_rows <= kSumThreads && a.n_seq <= kMostInline && !(a.grad && plan.resident);
+    const bool small = a.n_rows <= kMostSmallRows && a.n_seq <= kMostInline && !(a.grad && plan.resident);
     if (a.n_rows > 0)
         SR_TRY(with_type(x->dtype, [&](auto *t) -> int {
             typedef std::remove_pointer_t<decltype(t)> T;
