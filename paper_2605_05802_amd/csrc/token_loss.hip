@@ -8,8 +8,7 @@
 //   seq_count_kernel, policy_rows_kernel    slope of every row from its sequence's advantage and weight, and its terms of the loss
 //   policy_sum_kernel    the terms added up
 //   pair_kernel          log ratios of a pair's sequences, the margin, the slopes of the pair's rows
-//   pair_sum_kernel      the pairs added up
-//   logit_grad_kernel    the gradient, from the row, (m, s) and the slope
+//   logit_grad_kernel    the gradient, from the row, (m, s) and the slope; in passing the pairs added up (pair_sum_kernel without one)
 //
 // Differences x - m are taken before the multiplication by log2(e): rows whose entries all are the type's lowest
 // value, or that hold -infinity, come out as their definition has it, and the largest entry's exponential is exactly 1.
@@ -101,6 +100,7 @@ struct RowArgs {
     int n_rows, vocab, n_seq;
     int splits, split_elems;           // parts of a row, whole vectors each
     int grad_splits, grad_elems;       // of the gradient's
+    int once_units;                    // parts, of the first rows, that are read past the caches (row_stats_kernel)
     float grad_scale;
     // workspace
     float2 *part;        // [n_rows][splits] (m, s)
@@ -110,6 +110,11 @@ struct RowArgs {
     float4 *terms;       // [n_rows] policy: surrogate, kl, clipped, weight; [n_seq / 2] pairs: loss, m > 0, rewards
     int32_t *count;      // [n_seq + 2] counting rows of the sequences, of all, and the number of sequences that have any
 };
+
+// What the gradient reads again stays in the memory-side cache if it was read with default loads, and little else was: the last rows
+// of a call are, the others with the non-temporal hint (730 MB of bf16: 118 us, with default loads 130; but the gradient behind
+// takes 232 us where all of them were read with the hint, and 215 where none were, or all but the last 384 MB).
+constexpr int64_t kKeepBytes = 384 << 20;
 
 // s of a row that does not count
 constexpr float kNoRow = -1.f;
@@ -139,12 +144,32 @@ __device__ __forceinline__ float logit_of(const RowArgs &a, int row, int v) {
 // The threads and wavefronts of a workgroup for rows of WAVES wavefronts: four rows of one each
 constexpr int row_block(int waves) { return waves == 1 ? 256 : 64 * waves; }
 
-// WAVES wavefronts per (row, part).  Four vectors in flight per thread.  ONCE: no gradient follows, the logits are not read again.
-template <typename T, int WAVES, bool ONCE>
+// The whole vectors of [from, full) of a row, every LANES-th for this thread, four in flight.  ONCE: with the non-temporal hint.
+template <typename T, int LANES, bool ONCE>
+__device__ __forceinline__ void add_part(RowSum &r, const T *x, int e, int full) {
+    constexpr int N = Elem<T>::kPerVec, DEPTH = 4;
+    auto load = [&](int j) __attribute__((always_inline)) { return ONCE ? load_vec_once(x + e + j * LANES * N) : load_vec(x + e + j * LANES * N); };
+    raw16 raw[DEPTH];
+    asm volatile("; once %0" ::"n"((int)ONCE));              // the two forms differ in a hint alone: the compiler would merge them
+    for (; e + (DEPTH - 1) * LANES * N < full; e += DEPTH * LANES * N) {
+#pragma unroll
+        for (int j = 0; j < DEPTH; ++j) raw[j] = load(j);
+        add_vectors<T, DEPTH>(r, raw);
+    }
+    if (e < full) {
+#pragma unroll
+        for (int j = 0; j < DEPTH; ++j) raw[j] = e + j * LANES * N < full ? load(j) : raw16(Elem<T>::kMinusInf);
+        add_vectors<T, DEPTH>(r, raw);
+    }
+    asm volatile("; once %0" ::"n"((int)ONCE));
+}
+
+// WAVES wavefronts per (row, part)
+template <typename T, int WAVES>
 __global__ __launch_bounds__(row_block(WAVES)) void row_stats_kernel(RowArgs a) {
-    constexpr int N = Elem<T>::kPerVec, LANES = 64 * WAVES, DEPTH = 4;
+    constexpr int N = Elem<T>::kPerVec, LANES = 64 * WAVES;
     __shared__ RowSum s_part[16];
-    const int unit = WAVES == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+    const int unit = WAVES == 1 ? __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)) : blockIdx.x;
     const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
     if (unit >= a.n_rows * a.splits) return;                 // wavefronts without a barrier to come, if any
     const int row = unit / a.splits, part = unit - row * a.splits;
@@ -157,19 +182,8 @@ __global__ __launch_bounds__(row_block(WAVES)) void row_stats_kernel(RowArgs a) 
     const int from = part * a.split_elems, to = min(from + a.split_elems, a.vocab), full = from + (to - from) / N * N;
     RowSum r = {-FLT_MAX, 0.f};
     if (full + t < to) r = one_element((float)x[full + t]);
-    raw16 raw[DEPTH];
-    int e = from + t * N;
-    for (; e + (DEPTH - 1) * LANES * N < full; e += DEPTH * LANES * N) {
-#pragma unroll
-        for (int j = 0; j < DEPTH; ++j) raw[j] = ONCE ? load_vec_once(x + e + j * LANES * N) : load_vec(x + e + j * LANES * N);
-        add_vectors<T, DEPTH>(r, raw);
-    }
-    if (e < full) {
-#pragma unroll
-        for (int j = 0; j < DEPTH; ++j)
-            raw[j] = e + j * LANES * N >= full ? raw16(Elem<T>::kMinusInf) : ONCE ? load_vec_once(x + e + j * LANES * N) : load_vec(x + e + j * LANES * N);
-        add_vectors<T, DEPTH>(r, raw);
-    }
+    if (unit < a.once_units) add_part<T, LANES, true>(r, x, from + t * N, full);
+    else add_part<T, LANES, false>(r, x, from + t * N, full);
     r = merge_lanes<64>(r);
     if (WAVES > 1) r = merge_waves<WAVES>(r, s_part);
     if (t == 0) *out = make_float2(r.m, r.s);
@@ -200,10 +214,37 @@ __device__ __forceinline__ raw16 gradient(raw16 raw, int hot, float m, float fac
     return Elem<T>::narrow(v);
 }
 
-// WAVES wavefronts per (row, part).  In place: a thread reads what it then writes.
+// The preference loss
+struct PairArgs {
+    const float *ref_logprob;
+    float beta, smoothing;
+    float *log_ratio, *stats;
+};
+
+// The mean over pairs of their terms, by a workgroup; s: THREADS / 64 doubles of LDS
+template <int THREADS>
+__device__ __forceinline__ void sum_pairs(const RowArgs &a, const PairArgs &p, double *s) {
+    const int pairs = a.n_seq / 2;
+    double x[4] = {};
+    for (int i = threadIdx.x; i < pairs; i += THREADS) {
+        const float4 t = a.terms[i];
+        x[0] += t.x;
+        x[1] += t.y;
+        x[2] += t.z;
+        x[3] += t.w;
+    }
+    for (int k = 0; k < 4; ++k) {
+        const double sum = block_sum<THREADS / 64>(x[k], s);
+        if (threadIdx.x == 0) p.stats[k] = (float)(sum / pairs);
+    }
+}
+
+// WAVES wavefronts per (row, part).  In place: a thread reads what it then writes.  p.stats: the first workgroup adds the pairs up.
 template <typename T, int WAVES>
-__global__ __launch_bounds__(row_block(WAVES)) void logit_grad_kernel(RowArgs a) {
+__global__ __launch_bounds__(row_block(WAVES)) void logit_grad_kernel(RowArgs a, PairArgs p) {
     constexpr int N = Elem<T>::kPerVec, LANES = 64 * WAVES, DEPTH = 4;
+    __shared__ double s[row_block(WAVES) / 64];
+    if (p.stats && blockIdx.x == 0) sum_pairs<row_block(WAVES)>(a, p, s);
     const int unit = WAVES == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
     const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
     if (unit >= a.n_rows * a.grad_splits) return;
@@ -654,12 +695,6 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
 // ---------------------------------------------------------------------------------------------
 // preference loss
 // ---------------------------------------------------------------------------------------------
-struct PairArgs {
-    const float *ref_logprob;
-    float beta, smoothing;
-    float *log_ratio, *stats;
-};
-
 // A pair, by LANES threads of which this is number t: log ratios, margin, slopes.  sum(x): over the LANES threads, in all of them.
 // Returns the pair's terms of the loss.  Rows outside every sequence are left to the first and the last pair.
 template <typename T, int LANES, typename F>
@@ -718,25 +753,9 @@ __global__ __launch_bounds__(kTermThreads) void pair_kernel(RowArgs a, PairArgs 
     if (threadIdx.x == 0) a.terms[blockIdx.x] = term;
 }
 
-// The mean over pairs, by a workgroup of kSumThreads; s: kSumThreads / 64 doubles of LDS
-__device__ __forceinline__ void sum_pairs(const RowArgs &a, const PairArgs &p, double *s) {
-    const int pairs = a.n_seq / 2;
-    double x[4] = {};
-    for (int i = threadIdx.x; i < pairs; i += kSumThreads) {
-        const float4 t = a.terms[i];
-        x[0] += t.x;
-        x[1] += t.y;
-        x[2] += t.z;
-        x[3] += t.w;
-    }
-    for (int k = 0; k < 4; ++k) {
-        const double sum = block_sum<kSumThreads / 64>(x[k], s);
-        if (threadIdx.x == 0) p.stats[k] = (float)(sum / pairs);
-    }
-}
-__global__ __launch_bounds__(kSumThreads) void pair_sum_kernel(RowArgs a, PairArgs p) {
-    __shared__ double s[kSumThreads / 64];
-    sum_pairs(a, p, s);
+__global__ __launch_bounds__(kTermThreads) void pair_sum_kernel(RowArgs a, PairArgs p) {
+    __shared__ double s[kTermThreads / 64];
+    sum_pairs<kTermThreads>(a, p, s);
 }
 
 // Both by one workgroup, a wavefront a pair: few pairs of few rows
@@ -753,7 +772,7 @@ __global__ __launch_bounds__(kSumThreads) void pair_small_kernel(RowArgs a, Pair
         if (lane == 0) a.terms[pair] = term;
     }
     __syncthreads();
-    sum_pairs(a, p, s);
+    sum_pairs<kSumThreads>(a, p, s);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -803,6 +822,9 @@ RowArgs row_args(const sr_token_rows *x, const RowPlan &plan, void *workspace) {
     a.count = (int32_t *)take(4 * ((size_t)x->n_seq + 2));
     a.splits = plan.parts;
     a.split_elems = plan.elems;
+    const int units = a.n_rows * a.splits;
+    const int64_t kept = kKeepBytes / ((int64_t)a.split_elems * (x->dtype == SR_F32 ? 4 : 2));
+    a.once_units = !a.grad ? units : kept < units ? units - (int)kept : 0;
     a.grad_splits = plan.grad_parts;
     a.grad_elems = plan.grad_elems;
     return a;
@@ -815,24 +837,20 @@ int with_type(int dtype, F &&f) {
     return f((f16_t *)nullptr);
 }
 
-template <typename T, bool ONCE>
+template <typename T>
 int launch_row_stats(const RowArgs &a, int waves, hipStream_t stream) {
     const int units = a.n_rows * a.splits;
-    if (waves == 1) row_stats_kernel<T, 1, ONCE><<<dim3(ceil_div(units, 4)), dim3(row_block(1)), 0, stream>>>(a);
-    else if (waves == 4) row_stats_kernel<T, 4, ONCE><<<dim3(units), dim3(row_block(4)), 0, stream>>>(a);
-    else row_stats_kernel<T, 16, ONCE><<<dim3(units), dim3(row_block(16)), 0, stream>>>(a);
+    if (waves == 1) row_stats_kernel<T, 1><<<dim3(ceil_div(units, 4)), dim3(row_block(1)), 0, stream>>>(a);
+    else if (waves == 4) row_stats_kernel<T, 4><<<dim3(units), dim3(row_block(4)), 0, stream>>>(a);
+    else row_stats_kernel<T, 16><<<dim3(units), dim3(row_block(16)), 0, stream>>>(a);
     SR_HIP(hipGetLastError());
     return SR_OK;
 }
 template <typename T>
-int launch_row_stats(const RowArgs &a, int waves, hipStream_t stream) {
-    return a.grad ? launch_row_stats<T, false>(a, waves, stream) : launch_row_stats<T, true>(a, waves, stream);
-}
-template <typename T>
-int launch_logit_grad(const RowArgs &a, int waves, hipStream_t stream) {
+int launch_logit_grad(const RowArgs &a, const PairArgs &p, int waves, hipStream_t stream) {
     const int units = a.n_rows * a.grad_splits;
-    if (waves == 1) logit_grad_kernel<T, 1><<<dim3(ceil_div(units, 4)), dim3(row_block(1)), 0, stream>>>(a);
-    else logit_grad_kernel<T, 4><<<dim3(units), dim3(row_block(4)), 0, stream>>>(a);
+    if (waves == 1) logit_grad_kernel<T, 1><<<dim3(ceil_div(units, 4)), dim3(row_block(1)), 0, stream>>>(a, p);
+    else logit_grad_kernel<T, 4><<<dim3(units), dim3(row_block(4)), 0, stream>>>(a, p);
     SR_HIP(hipGetLastError());
     return SR_OK;
 }
@@ -897,7 +915,7 @@ int policy_loss(const sr_token_rows *x, const PolicyArgs &p, void *workspace, hi
                 policy_rows_kernel<T><<<dim3(ceil_div(a.n_rows, kTermThreads)), dim3(kTermThreads), 0, stream>>>(a, p);
                 SR_HIP(hipGetLastError());
             }
-            return a.grad ? launch_logit_grad<T>(a, plan.grad_waves, stream) : SR_OK;
+            return a.grad ? launch_logit_grad<T>(a, PairArgs{}, plan.grad_waves, stream) : SR_OK;
         }));
     if (a.n_rows > 0 && small) return SR_OK;
     if (a.n_rows > kMostSummedRows) {
@@ -922,9 +940,9 @@ int preference_loss(const sr_token_rows *x, const PairArgs &p, void *workspace, 
         if (small) pair_small_kernel<T><<<dim3(1), dim3(kSumThreads), 0, stream>>>(a, p);
         else pair_kernel<T><<<dim3(a.n_seq / 2), dim3(kTermThreads), 0, stream>>>(a, p);
         SR_HIP(hipGetLastError());
-        if (a.n_rows > 0 && a.grad) SR_TRY(launch_logit_grad<T>(a, plan.grad_waves, stream));
+        if (a.n_rows > 0 && a.grad) return launch_logit_grad<T>(a, small ? PairArgs{} : p, plan.grad_waves, stream);
         if (small) return SR_OK;
-        pair_sum_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(a, p);
+        pair_sum_kernel<<<dim3(1), dim3(kTermThreads), 0, stream>>>(a, p);
         SR_HIP(hipGetLastError());
         return SR_OK;
     });
