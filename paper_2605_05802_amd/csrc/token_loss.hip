@@ -119,6 +119,11 @@ constexpr int64_t kKeepBytes = 384 << 20;
 // s of a row that does not count
 constexpr float kNoRow = -1.f;
 
+// A uniform address by a scalar load: it does not queue behind vector loads and stores.  Nothing that the kernel itself writes.
+template <typename V> __device__ __forceinline__ V read_uniform(const V *p) {
+    typedef std::conditional_t<sizeof(V) == 8, uint64_t, uint32_t> bits;
+    return __builtin_bit_cast(V, *(const __attribute__((address_space(4))) bits *)p);
+}
 // the sequence of a row, or -1: the last one that begins at or before it
 __device__ __forceinline__ int sequence_of(const int32_t *seq_start, int n_seq, int row) {
     int lo = -1, hi = n_seq;
@@ -130,7 +135,7 @@ __device__ __forceinline__ int sequence_of(const int32_t *seq_start, int n_seq, 
     return lo >= 0 && row < seq_start[lo + 1] ? lo : -1;
 }
 __device__ __forceinline__ bool row_counts(const RowArgs &a, int row) {
-    return (!a.mask || a.mask[row]) && row >= a.seq_start[0] && row < a.seq_start[a.n_seq];
+    return (!a.mask || a.mask[row]) && row >= read_uniform(a.seq_start) && row < read_uniform(a.seq_start + a.n_seq);
 }
 
 template <typename T>
@@ -449,15 +454,11 @@ __device__ __forceinline__ float policy_row(const PolicyArgs &p, float2 info, fl
     return slope * info.x;
 }
 
-// What a row's slope takes beside its logits, by scalar loads: they do not queue behind the row's stores
+// What a row's slope takes beside its logits
 struct RowScalars {
     int target;
     float old_logprob, ref_logprob;
 };
-template <typename V> __device__ __forceinline__ V read_uniform(const V *p) {
-    typedef std::conditional_t<sizeof(V) == 8, uint64_t, uint32_t> bits;
-    return __builtin_bit_cast(V, *(const __attribute__((address_space(4))) bits *)p);
-}
 __device__ __forceinline__ RowScalars row_scalars(const RowArgs &a, const PolicyArgs &p, int row) {
     return RowScalars{read_uniform(a.targets + row), read_uniform(p.old_logprob + row),
                       p.ref_logprob ? read_uniform(p.ref_logprob + row) : 0.f};
