@@ -104,6 +104,7 @@ struct RowArgs {
     float grad_scale;
     // workspace
     float2 *part;        // [n_rows][splits] (m, s)
+    float *chosen;       // [n_rows] the logit of the row's token
     float2 *whole;       // [n_rows] (m, s)
     float2 *info;        // [n_rows] policy: weight (0: does not count), advantage
     float *slope;        // [n_rows], grad_scale included
@@ -185,13 +186,21 @@ __global__ __launch_bounds__(row_block(WAVES)) void row_stats_kernel(RowArgs a) 
     }
     const T *x = (const T *)a.logits + row * a.ld_logits;
     const int from = part * a.split_elems, to = min(from + a.split_elems, a.vocab), full = from + (to - from) / N * N;
+    const int target = read_uniform(a.targets + row);
     RowSum r = {-FLT_MAX, 0.f};
     if (full + t < to) r = one_element((float)x[full + t]);
     if (unit < a.once_units) add_part<T, LANES, true>(r, x, from + t * N, full);
     else add_part<T, LANES, false>(r, x, from + t * N, full);
+    // The token's logit for the kernel behind this one: there it would be a cache line and an address translation per row, cold
+    const bool holds = target >= from && target < to, none = part == 0 && (target < 0 || target >= a.vocab);
+    float chosen = NAN;
+    if (holds) chosen = (float)x[target];
     r = merge_lanes<64>(r);
     if (WAVES > 1) r = merge_waves<WAVES>(r, s_part);
-    if (t == 0) *out = make_float2(r.m, r.s);
+    if (t == 0) {
+        *out = make_float2(r.m, r.s);
+        if (holds || none) a.chosen[row] = chosen;
+    }
 }
 
 // (m, s) of a row from its parts, in their order
@@ -510,26 +519,30 @@ struct PolicySums {
     }
 };
 
-// What lies between a row's (m, s) and its gradient
-template <typename T>
-__device__ __forceinline__ float4 finish_row(const RowArgs &a, const PolicyArgs &p, int row, float2 info) {
+// What lies between a row's (m, s) and its gradient: what it reads, and what becomes of that
+struct RowInput {
+    RowSum r;
+    float chosen, old_logprob, ref_logprob;
+};
+__device__ __forceinline__ RowInput row_input(const RowArgs &a, const PolicyArgs &p, int row) {
+    return RowInput{whole_row(a, row), a.chosen[row], p.old_logprob[row], p.ref_logprob ? p.ref_logprob[row] : 0.f};
+}
+__device__ __forceinline__ float4 finish_row(const RowArgs &a, const PolicyArgs &p, int row, float2 info, const RowInput &in) {
     float logprob = 0.f, slope = 0.f;
     float4 term = make_float4(0.f, 0.f, 0.f, 0.f);
-    const RowSum r = whole_row(a, row);
     if (info.x != 0.f) {
-        logprob = (logit_of<T>(a, row, a.targets[row]) - r.m) - logf(r.s);
-        slope = policy_row(p, info, logprob, p.old_logprob[row], p.ref_logprob ? p.ref_logprob[row] : 0.f, &term) * a.grad_scale;
+        logprob = (in.chosen - in.r.m) - logf(in.r.s);
+        slope = policy_row(p, info, logprob, in.old_logprob, in.ref_logprob, &term) * a.grad_scale;
     }
     if (a.token_logprob) a.token_logprob[row] = logprob;
     a.slope[row] = slope;
-    a.whole[row] = make_float2(r.m, r.s);
+    a.whole[row] = make_float2(in.r.m, in.r.s);
     return term;
 }
 
-template <typename T>
 __global__ __launch_bounds__(kTermThreads) void policy_rows_kernel(RowArgs a, PolicyArgs p) {
     const int row = blockIdx.x * kTermThreads + threadIdx.x;
-    if (row < a.n_rows) a.terms[row] = finish_row<T>(a, p, row, a.info[row]);
+    if (row < a.n_rows) a.terms[row] = finish_row(a, p, row, a.info[row], row_input(a, p, row));
 }
 __global__ __launch_bounds__(kSumThreads) void policy_sum_kernel(RowArgs a, PolicyArgs p) {
     __shared__ double s[3 * kSumThreads / 64];
@@ -554,13 +567,21 @@ __global__ __launch_bounds__(kSumThreads) void policy_shares_kernel(PolicyArgs p
 }
 
 // The kernels between row_stats_kernel and logit_grad_kernel, and policy_sum_kernel, by one workgroup: few rows
-template <typename T>
 __global__ __launch_bounds__(kSumThreads) void policy_small_kernel(RowArgs a, PolicyArgs p) {
     __shared__ double s[3 * kSumThreads / 64];
     __shared__ SeqTable table;
+    constexpr int EACH = kMostSmallRows / kSumThreads;
+    RowInput in[EACH];                                       // asked for before the table is made
+#pragma unroll
+    for (int k = 0; k < EACH; ++k)
+        if ((int)threadIdx.x + k * kSumThreads < a.n_rows) in[k] = row_input(a, p, threadIdx.x + k * kSumThreads);
     table.fill<kSumThreads>(a);
     PolicySums sums;
-    for (int row = threadIdx.x; row < a.n_rows; row += kSumThreads) sums.add(finish_row<T>(a, p, row, table.info(a, p, row)));
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+        const int row = threadIdx.x + k * kSumThreads;
+        if (row < a.n_rows) sums.add(finish_row(a, p, row, table.info(a, p, row), in[k]));
+    }
     sums.finish(p, s);
 }
 
@@ -628,14 +649,18 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
         for (int j = 0; j < NV; ++j) fetch(j, x);
         if (tail < a.vocab) last = x[tail];
     }
+    RowScalars scalars;
+    float chosen;
+    if (mine) {
+        scalars = row_scalars(a, p, row);
+        chosen = logit_of<T>(a, row, scalars.target);
+    }
     if constexpr (TABLE) {
         __shared__ SeqTable table;
         table.template fill<row_block(WAVES)>(a);
         if (!mine) return;
         info = table.info(a, p, row);
     }
-    RowScalars scalars = row_scalars(a, p, row);
-    float chosen = logit_of<T>(a, row, scalars.target);
     RowSum r = {-FLT_MAX, 0.f};
     if (tail < a.vocab) r = one_element((float)last);
     add_vectors<T, NV>(r, raw);
@@ -698,19 +723,19 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
 // ---------------------------------------------------------------------------------------------
 // A pair, by LANES threads of which this is number t: log ratios, margin, slopes.  sum(x): over the LANES threads, in all of them.
 // Returns the pair's terms of the loss.  Rows outside every sequence are left to the first and the last pair.
-template <typename T, int LANES, typename F>
+template <int LANES, typename F>
 __device__ __forceinline__ float4 finish_pair(const RowArgs &a, const PairArgs &p, int pair, int t, F &&sum) {
     const int pairs = a.n_seq / 2;
     const int start = max(a.seq_start[2 * pair], 0), mid = a.seq_start[2 * pair + 1], end = min(a.seq_start[2 * pair + 2], a.n_rows);
     double ratio[2] = {};
     for (int row = start + t; row < end; row += LANES) {
-        const int target = a.targets[row];
+        const float chosen = a.chosen[row];
         const double ref = p.ref_logprob ? (double)p.ref_logprob[row] : 0.0;
         const RowSum r = whole_row(a, row);
         double logprob = 0.0;
         if (r.s != kNoRow) {
             // l in double: a pair adds hundreds of them, and rounds to single precision once
-            logprob = (double)(logit_of<T>(a, row, target) - r.m) - log((double)r.s);
+            logprob = (double)(chosen - r.m) - log((double)r.s);
             if (row < mid) ratio[0] += logprob - ref;
             else ratio[1] += logprob - ref;
         }
@@ -742,10 +767,9 @@ __device__ __forceinline__ float4 finish_pair(const RowArgs &a, const PairArgs &
     return make_float4(loss, m > 0.f ? 1.f : 0.f, (float)reward0, (float)reward1);
 }
 
-template <typename T>
 __global__ __launch_bounds__(kTermThreads) void pair_kernel(RowArgs a, PairArgs p) {
     __shared__ double s[kTermThreads / 64 + 1];
-    const float4 term = finish_pair<T, kTermThreads>(a, p, blockIdx.x, threadIdx.x, [&](double x) {
+    const float4 term = finish_pair<kTermThreads>(a, p, blockIdx.x, threadIdx.x, [&](double x) {
         x = block_sum<kTermThreads / 64>(x, s);
         if (threadIdx.x == 0) s[kTermThreads / 64] = x;
         __syncthreads();
@@ -760,12 +784,11 @@ __global__ __launch_bounds__(kTermThreads) void pair_sum_kernel(RowArgs a, PairA
 }
 
 // Both by one workgroup, a wavefront a pair: few pairs of few rows
-template <typename T>
 __global__ __launch_bounds__(kSumThreads) void pair_small_kernel(RowArgs a, PairArgs p) {
     __shared__ double s[kSumThreads / 64];
     const int lane = threadIdx.x & 63;
     for (int pair = threadIdx.x >> 6; pair < a.n_seq / 2; pair += kSumThreads / 64) {
-        const float4 term = finish_pair<T, 64>(a, p, pair, lane, [](double x) {
+        const float4 term = finish_pair<64>(a, p, pair, lane, [](double x) {
 #pragma unroll
             for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off, 64);
             return x;
@@ -792,7 +815,8 @@ int check_rows(const sr_token_rows *x, const void *workspace, size_t bytes) {
     return x->grad == x->logits && x->ld_grad != x->ld_logits ? SR_E_ARG : SR_OK;
 }
 
-// SR_TOKEN_LOSS_WORKSPACE: of every row 16 bytes of terms, 8 each of (m, s) as parts, whole, and of weight and advantage, 4 of slope;
+// SR_TOKEN_LOSS_WORKSPACE: of every row 16 bytes of terms, 8 each of (m, s) as parts, whole, and of weight and advantage, 4 each of
+// slope and the token's logit;
 // of every sequence 16 (a pair's terms) and 4; the constant part for more parts than rows
 RowArgs row_args(const sr_token_rows *x, const RowPlan &plan, void *workspace) {
     RowArgs a{};
@@ -820,6 +844,7 @@ RowArgs row_args(const sr_token_rows *x, const RowPlan &plan, void *workspace) {
     a.whole = (float2 *)take(8 * rows);
     a.info = (float2 *)take(8 * rows);
     a.slope = (float *)take(4 * rows);
+    a.chosen = (float *)take(4 * rows);
     a.count = (int32_t *)take(4 * ((size_t)x->n_seq + 2));
     a.splits = plan.parts;
     a.split_elems = plan.elems;
@@ -909,11 +934,11 @@ int policy_loss(const sr_token_rows *x, const PolicyArgs &p, void *workspace, hi
             if (a.grad && plan.resident) return launch_resident<T>(a, p, plan.waves, plan.resident, stream);
             SR_TRY(launch_row_stats<T>(a, plan.waves, stream));
             if (small) {
-                policy_small_kernel<T><<<dim3(1), dim3(kSumThreads), 0, stream>>>(a, p);
+                policy_small_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(a, p);
                 SR_HIP(hipGetLastError());
             } else {
                 SR_TRY(launch_row_info(a, p, stream));
-                policy_rows_kernel<T><<<dim3(ceil_div(a.n_rows, kTermThreads)), dim3(kTermThreads), 0, stream>>>(a, p);
+                policy_rows_kernel<<<dim3(ceil_div(a.n_rows, kTermThreads)), dim3(kTermThreads), 0, stream>>>(a, p);
                 SR_HIP(hipGetLastError());
             }
             return a.grad ? launch_logit_grad<T>(a, PairArgs{}, plan.grad_waves, stream) : SR_OK;
@@ -938,8 +963,8 @@ int preference_loss(const sr_token_rows *x, const PairArgs &p, void *workspace, 
         typedef std::remove_pointer_t<decltype(t)> T;
         if (a.n_rows > 0) SR_TRY(launch_row_stats<T>(a, plan.waves, stream));
         const bool small = a.n_rows <= kMostPairRows && a.n_seq <= kMostPairSeqs;
-        if (small) pair_small_kernel<T><<<dim3(1), dim3(kSumThreads), 0, stream>>>(a, p);
-        else pair_kernel<T><<<dim3(a.n_seq / 2), dim3(kTermThreads), 0, stream>>>(a, p);
+        if (small) pair_small_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(a, p);
+        else pair_kernel<<<dim3(a.n_seq / 2), dim3(kTermThreads), 0, stream>>>(a, p);
         SR_HIP(hipGetLastError());
         if (a.n_rows > 0 && a.grad) return launch_logit_grad<T>(a, small ? PairArgs{} : p, plan.grad_waves, stream);
         if (small) return SR_OK;
