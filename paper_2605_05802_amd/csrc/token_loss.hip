@@ -26,7 +26,6 @@ constexpr int kMostSummedRows = 16384, kShares = 256;      // rows whose terms o
 constexpr int kMostInline = 1024;      // sequences of a small call
 constexpr int kMostTableRows = 4096;   // its rows
 constexpr int kMostSmallRows = 2048;   // rows whose slopes and terms one workgroup computes
-constexpr int kMostTableBlocks = 512;  // workgroups that look the weights up for themselves
 constexpr int kMostPairRows = 512, kMostPairSeqs = 32;     // of a small call of the preference loss
 constexpr int kParts = 8192;           // parts of rows that the workspace holds
 
@@ -135,8 +134,15 @@ __device__ __forceinline__ int sequence_of(const int32_t *seq_start, int n_seq, 
     }
     return lo >= 0 && row < seq_start[lo + 1] ? lo : -1;
 }
+// A uniform row's mask, by a scalar load of the word that holds it where all of that word is the mask's
+__device__ __forceinline__ bool masked_in(const RowArgs &a, int row) {
+    if (!a.mask) return true;
+    const uintptr_t from = (uintptr_t)a.mask, at = from + row, word = at & ~(uintptr_t)3;
+    if (word < from || word + 4 > from + a.n_rows) return a.mask[row] != 0;
+    return (read_uniform((const uint32_t *)word) >> (8 * (at & 3)) & 255u) != 0;
+}
 __device__ __forceinline__ bool row_counts(const RowArgs &a, int row) {
-    return (!a.mask || a.mask[row]) && row >= read_uniform(a.seq_start) && row < read_uniform(a.seq_start + a.n_seq);
+    return row >= read_uniform(a.seq_start) && row < read_uniform(a.seq_start + a.n_seq) && masked_in(a, row);
 }
 
 template <typename T>
@@ -306,9 +312,11 @@ __device__ __forceinline__ unsigned set_bytes(unsigned w) {
     return ((top >> 7) * 0x10204080u) >> 28;                 // bits 0, 8, 16, 24 to 28 .. 31, the other products apart from each other
 }
 // ... and for sixteen bytes of a mask
-__device__ __forceinline__ unsigned set_bytes_16(const uint8_t *p) {
+__device__ __forceinline__ raw16 load_bytes(const uint8_t *p) {
     typedef uint32_t raw16_bytes __attribute__((ext_vector_type(4), aligned(1)));
-    const raw16 m = *(const raw16_bytes *)p;
+    return *(const raw16_bytes *)p;
+}
+__device__ __forceinline__ unsigned set_bytes_16(raw16 m) {
     return set_bytes(m[0]) | set_bytes(m[1]) << 4 | set_bytes(m[2]) << 8 | set_bytes(m[3]) << 12;
 }
 // Sums of two whole numbers over the wavefronts of a workgroup, into LDS
@@ -337,7 +345,7 @@ __global__ __launch_bounds__(kTermThreads) void seq_count_kernel(RowArgs a) {
     __syncthreads();
     int n = 0;
     for (int r = from + 16 * t; r < to; r += 16 * kTermThreads) {
-        if (r + 16 <= to) n += __popc(set_bytes_16(a.mask + r));
+        if (r + 16 <= to) n += __popc(set_bytes_16(load_bytes(a.mask + r)));
         else
             for (int i = r; i < to; ++i) n += a.mask[i] != 0;
     }
@@ -378,22 +386,38 @@ struct SeqTable {
 
     __device__ __forceinline__ int rank(int row) const { return before[row >> 4] + __popc(bits[row >> 4] & ((1u << (row & 15)) - 1u)); }
 
+    // What fill() reads, asked for ahead of it: loads return in order, and those of a row in between would be waited for
+    struct Ahead {
+        int start;
+        raw16 mask;
+    };
+    static __device__ __forceinline__ Ahead ahead(const RowArgs &a) {
+        Ahead x = {};
+        const int t = threadIdx.x;
+        if (t <= a.n_seq) x.start = a.seq_start[t];
+        // the last word's rows are the end of the mask's last sixteen bytes
+        if (a.mask && 16 * t < a.n_rows && a.n_rows >= 16) x.mask = load_bytes(a.mask + min(16 * t, a.n_rows - 16));
+        return x;
+    }
+
     // by the whole workgroup; barriers inside and behind
     template <int THREADS>
-    __device__ __forceinline__ void fill(const RowArgs &a) {
+    __device__ __forceinline__ void fill(const RowArgs &a, const Ahead &x) {
         static_assert(kMostTableRows / 16 == 256 && THREADS >= 256, "a word a thread");
         const int t = threadIdx.x;
-        for (int i = t; i <= a.n_seq; i += THREADS) start[i] = a.seq_start[i];
+        if (t <= a.n_seq) start[t] = x.start;
+        for (int i = t + THREADS; i <= a.n_seq; i += THREADS) start[i] = a.seq_start[i];
         if (t == 0) rows = used = 0;
         if (a.mask) {
             unsigned mine = 0;
             int ahead = 0;
             if (t < 256) {
                 const int n = a.n_rows - 16 * t;
-                if (n >= 16) {
-                    mine = set_bytes_16(a.mask + 16 * t);
-                } else {
+                if (a.n_rows < 16) {
                     for (int i = 0; i < n; ++i) mine |= (unsigned)(a.mask[16 * t + i] != 0) << i;
+                } else if (n > 0) {
+                    mine = set_bytes_16(x.mask);
+                    if (n < 16) mine >>= 16 - n;
                 }
                 const int own = __popc(mine);
                 ahead = own;
@@ -429,7 +453,7 @@ struct SeqTable {
         __syncthreads();
     }
     __device__ __forceinline__ float2 info(const RowArgs &a, const PolicyArgs &p, int row) const {
-        const int seq = !a.mask || a.mask[row] ? sequence_of(start, a.n_seq, row) : -1;
+        const int seq = !a.mask || bits[row >> 4] >> (row & 15) & 1 ? sequence_of(start, a.n_seq, row) : -1;
         return seq < 0 ? make_float2(0.f, 0.f) : row_info(p, seq, count[seq], rows, used);
     }
 };
@@ -443,7 +467,7 @@ __global__ __launch_bounds__(kTermThreads) void row_info_kernel(RowArgs a, Polic
 // The same three by one workgroup
 __global__ __launch_bounds__(kSumThreads) void row_info_small_kernel(RowArgs a, PolicyArgs p) {
     __shared__ SeqTable table;
-    table.fill<kSumThreads>(a);
+    table.fill<kSumThreads>(a, SeqTable::ahead(a));
     for (int row = threadIdx.x; row < a.n_rows; row += kSumThreads) a.info[row] = table.info(a, p, row);
 }
 
@@ -571,11 +595,12 @@ __global__ __launch_bounds__(kSumThreads) void policy_small_kernel(RowArgs a, Po
     __shared__ double s[3 * kSumThreads / 64];
     __shared__ SeqTable table;
     constexpr int EACH = kMostSmallRows / kSumThreads;
+    const SeqTable::Ahead ahead = SeqTable::ahead(a);
     RowInput in[EACH];                                       // asked for before the table is made
 #pragma unroll
     for (int k = 0; k < EACH; ++k)
         if ((int)threadIdx.x + k * kSumThreads < a.n_rows) in[k] = row_input(a, p, threadIdx.x + k * kSumThreads);
-    table.fill<kSumThreads>(a);
+    table.fill<kSumThreads>(a, ahead);
     PolicySums sums;
 #pragma unroll
     for (int k = 0; k < EACH; ++k) {
@@ -643,6 +668,8 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
         info = read_uniform(a.info + row);
         if (info.x == 0.f) return zeros(row);
     }
+    SeqTable::Ahead ahead;
+    if constexpr (TABLE) ahead = SeqTable::ahead(a);
     const T *x = (const T *)a.logits + row * a.ld_logits;
     if (mine) {
 #pragma unroll
@@ -657,7 +684,7 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
     }
     if constexpr (TABLE) {
         __shared__ SeqTable table;
-        table.template fill<row_block(WAVES)>(a);
+        table.template fill<row_block(WAVES)>(a, ahead);
         if (!mine) return;
         info = table.info(a, p, row);
     }
@@ -907,7 +934,7 @@ int launch_resident(const RowArgs &a, const PolicyArgs &p, int vecs, hipStream_t
         policy_resident_kernel<T, WAVES, NV, true, false><<<dim3(a.n_rows < 256 ? a.n_rows : 256), dim3(row_block(WAVES)), 0, stream>>>(a, p);
     } else {
         const int blocks = WAVES == 1 ? ceil_div(a.n_rows, 4) : a.n_rows;
-        if (blocks <= kMostTableBlocks && a.n_seq <= kMostInline && a.n_rows <= kMostTableRows) {
+        if (a.n_seq <= kMostInline && a.n_rows <= kMostTableRows) {
             policy_resident_kernel<T, WAVES, NV, false, true><<<dim3(blocks), dim3(row_block(WAVES)), 0, stream>>>(a, p);
         } else {
             SR_TRY(launch_row_info(a, p, stream));
