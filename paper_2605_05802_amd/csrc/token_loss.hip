@@ -145,11 +145,6 @@ __device__ __forceinline__ bool row_counts(const RowArgs &a, int row) {
     return row >= read_uniform(a.seq_start) && row < read_uniform(a.seq_start + a.n_seq) && masked_in(a, row);
 }
 
-template <typename T>
-__device__ __forceinline__ float logit_of(const RowArgs &a, int row, int v) {
-    return v >= 0 && v < a.vocab ? (float)((const T *)a.logits)[row * a.ld_logits + v] : NAN;
-}
-
 // ---------------------------------------------------------------------------------------------
 // streaming: (m, s) in one kernel, the gradient in another
 // ---------------------------------------------------------------------------------------------
@@ -370,11 +365,11 @@ __global__ __launch_bounds__(kSumThreads) void seq_total_kernel(RowArgs a) {
 
 // Weight and advantage of a counting row.  count: its sequence's counting rows; rows, used: those of all sequences, and the sequences
 // that have any
-__device__ __forceinline__ float2 row_info(const PolicyArgs &p, int seq, int count, int rows, int used) {
+__device__ __forceinline__ float2 row_info(const PolicyArgs &p, float advantage, int count, int rows, int used) {
     const float w = p.reduce == SR_MEAN_TOKENS      ? 1.f / (float)rows
                     : p.reduce == SR_MEAN_SEQUENCES ? 1.f / ((float)used * (float)count)
                                                     : 1.f / (float)used;
-    return make_float2(w, p.advantages[seq]);
+    return make_float2(w, advantage);
 }
 
 // The sequences of a small call in LDS.  Counting rows in front of a row: sixteen rows of the mask are a word of bits, with the number
@@ -452,9 +447,17 @@ struct SeqTable {
         add_up(n, some, &rows, &used);
         __syncthreads();
     }
+    __device__ __forceinline__ int sequence(const RowArgs &a, int row) const {
+        return !a.mask || bits[row >> 4] >> (row & 15) & 1 ? sequence_of(start, a.n_seq, row) : -1;
+    }
     __device__ __forceinline__ float2 info(const RowArgs &a, const PolicyArgs &p, int row) const {
-        const int seq = !a.mask || bits[row >> 4] >> (row & 15) & 1 ? sequence_of(start, a.n_seq, row) : -1;
-        return seq < 0 ? make_float2(0.f, 0.f) : row_info(p, seq, count[seq], rows, used);
+        const int seq = sequence(a, row);
+        return seq < 0 ? make_float2(0.f, 0.f) : row_info(p, p.advantages[seq], count[seq], rows, used);
+    }
+    // of a uniform row
+    __device__ __forceinline__ float2 info_of_wave(const RowArgs &a, const PolicyArgs &p, int row) const {
+        const int seq = __builtin_amdgcn_readfirstlane(sequence(a, row));
+        return seq < 0 ? make_float2(0.f, 0.f) : row_info(p, read_uniform(p.advantages + seq), count[seq], rows, used);
     }
 };
 
@@ -462,7 +465,7 @@ __global__ __launch_bounds__(kTermThreads) void row_info_kernel(RowArgs a, Polic
     const int row = blockIdx.x * kTermThreads + threadIdx.x;
     if (row >= a.n_rows) return;
     const int seq = !a.mask || a.mask[row] ? sequence_of(a.seq_start, a.n_seq, row) : -1;
-    a.info[row] = seq < 0 ? make_float2(0.f, 0.f) : row_info(p, seq, a.count[seq], a.count[a.n_seq], a.count[a.n_seq + 1]);
+    a.info[row] = seq < 0 ? make_float2(0.f, 0.f) : row_info(p, p.advantages[seq], a.count[seq], a.count[a.n_seq], a.count[a.n_seq + 1]);
 }
 // The same three by one workgroup
 __global__ __launch_bounds__(kSumThreads) void row_info_small_kernel(RowArgs a, PolicyArgs p) {
@@ -626,7 +629,11 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
     int row = WAVES == 1 ? __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)) : blockIdx.x;
     const int full = a.vocab / N * N, tail = full + t;
     raw16 raw[NV];
-    T last;                                                  // lanes behind the last whole vector: an element of the rest
+    // Loaded unconditionally, from a place in the row, and looked at later: a load under a condition is waited for at its end, and
+    // everything before it with it.
+    T last, chosen;                                          // lanes behind the last whole vector: an element of the rest; the token's
+    const int last_at = min(tail, a.vocab - 1);
+    auto token_at = [&](int target) __attribute__((always_inline)) { return min(max(target, 0), a.vocab - 1); };
     int at = t * N;                                          // the thread's element of the row's first LANES vectors
     auto fetch = [&](int j, const T *x) __attribute__((always_inline)) {
         raw[j] = raw16(Elem<T>::kMinusInf);
@@ -654,43 +661,47 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
         return row;
     };
     float2 info;
-    bool mine = row < a.n_rows;                              // false for a wavefront of a small call that has no counting row
+    bool mine = row < a.n_rows;                              // false for a wavefront beside others that has no counting row
+    SeqTable::Ahead ahead;
     if constexpr (LOOP) {
         row = counting(row, &info);
         if (row >= a.n_rows) return;
     } else if (TABLE) {
+        ahead = SeqTable::ahead(a);
         if (mine && !row_counts(a, row)) {
             zeros(row);
             mine = false;
+        }
+        if (WAVES > 1) {                                     // one row: done, and where the row's loads are not conditional their number is known
+            if (!mine) return;
+            mine = true;
         }
     } else {
         if (!mine) return;
         info = read_uniform(a.info + row);
         if (info.x == 0.f) return zeros(row);
     }
-    SeqTable::Ahead ahead;
-    if constexpr (TABLE) ahead = SeqTable::ahead(a);
     const T *x = (const T *)a.logits + row * a.ld_logits;
     if (mine) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) fetch(j, x);
-        if (tail < a.vocab) last = x[tail];
+        last = x[last_at];
     }
     RowScalars scalars;
-    float chosen;
     if (mine) {
         scalars = row_scalars(a, p, row);
-        chosen = logit_of<T>(a, row, scalars.target);
+        chosen = x[token_at(scalars.target)];
     }
     if constexpr (TABLE) {
         __shared__ SeqTable table;
         table.template fill<row_block(WAVES)>(a, ahead);
         if (!mine) return;
-        info = table.info(a, p, row);
+        info = table.info_of_wave(a, p, row);
     }
     RowSum r = {-FLT_MAX, 0.f};
     if (tail < a.vocab) r = one_element((float)last);
     add_vectors<T, NV>(r, raw);
+    if (LOOP) asm volatile("" ::"v"((float)chosen));         // waited for here, so that in the loop nothing but a row's own loads is
     for (int turn = 0;; turn ^= 1) {
         asm volatile("" : "+v"(at));                         // or the loop keeps every vector's address and index in registers
         T *g = (T *)a.grad + row * a.ld_grad;
@@ -701,7 +712,8 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
         r = merge_lanes<64>(r);
         // the half of s_part that the row before used may still be read by wavefronts behind this barrier, but not the other
         if (WAVES > 1) r = merge_waves<WAVES>(r, s_part[turn]);
-        const float logprob = (chosen - r.m) - logf(r.s), m = r.m;
+        const float logit = token_at(scalars.target) == scalars.target ? (float)chosen : NAN;
+        const float logprob = (logit - r.m) - logf(r.s), m = r.m;
         float4 term;
         const float slope = policy_row(p, info, logprob, scalars.old_logprob, scalars.ref_logprob, &term) * a.grad_scale;
         const float factor = -slope / r.s;
@@ -723,8 +735,8 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
         // for AHEAD vectors earlier are added up, so that neither the memory nor the arithmetic waits for the other.
         constexpr int AHEAD = NV / 2 / kGroup * kGroup;
         x = (const T *)a.logits + next * a.ld_logits;
-        if (tail < a.vocab) last = x[tail];
-        chosen = logit_of<T>(a, next, next_scalars.target);
+        last = x[last_at];
+        chosen = x[token_at(next_scalars.target)];
         r = RowSum{-FLT_MAX, 0.f};
 #pragma unroll
         for (int k = 0; k < NV; k += kGroup) {
