@@ -13,6 +13,9 @@
  *     d_K < d_L (Eq. 2); a cut group stops generating and leaves the batch (Section 3.2,
  *     paragraph "The gate"; Appendix C.1).
  *
+ * Behind the rollout it has the losses over the kept trajectories' logits with their gradients, and
+ * the clipping of a list of gradients (sr_policy_loss, sr_preference_loss, sr_clip_grad_norm).
+ *
  * Conventions
  *   - Every function returns SR_OK (0) or a negative sr_status; nothing throws or exits.
  *   - "device" pointers are HIP device memory of the current device; "host" pointers are

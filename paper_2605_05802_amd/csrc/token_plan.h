@@ -11,6 +11,7 @@ struct RowPlan {
     int grad_waves, grad_parts, grad_elems;    // the same of the gradient
 };
 constexpr int kMostResident = 20, kMostOneWave = 8;
+// Many small parts in the order of the memory: 2400 rows of 152064 bf16 take 244 us in parts of 101 KB, 231 of 32 KB, 214 of 16 KB, 220 of 9 KB.
 constexpr int kGradPartBytes = 16384;
 
 // A row of `vecs` vectors in at most `parts` equal ones
@@ -21,7 +22,9 @@ inline void split_row(int vecs, int per_vec, int parts, int *n, int *elems) {
     *elems = each * per_vec;
 }
 
-// Rows that are read twice
+// Rows that are read twice.  Few rows: parts for about 1024 workgroups (128 rows of 152064 fp32 in 8 parts 15 + 22 us for maximum and
+// gradient; in 16, 32 and 64 the kernel between them, which merges the parts, takes 1, 4 and 9 us longer).  Many: 8192 parts even out the end
+// (2400 rows of 152064 bf16 in 3 parts each 129 us, in one 136; 1701 rows of 50021 in 4, 30 us, 34).
 inline RowPlan plan_streamed_rows(int n_rows, int vocab, int elem_bytes) {
     const int per_vec = 16 / elem_bytes, vecs = ceil_div(vocab, per_vec);
     int parts = n_rows > 0 ? (n_rows < 1024 ? 1024 : 8192) / n_rows : 1;
