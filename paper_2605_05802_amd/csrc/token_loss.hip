@@ -11,7 +11,7 @@
 // Everything else goes through the logits twice:
 //   row_stats_kernel     (m, s) of a row, or of a part of one
 //   policy_small_kernel, or row_info_*, policy_rows_kernel and policy_sum_kernel    the slopes of the rows and the loss
-//   pair_small_kernel, or pair_kernel    log ratios of a pair's sequences, the margin, the slopes of the pair's rows
+//   pair_kernel          log ratios of a pair's sequences, the margin, the slopes of the pair's rows
 //   logit_grad_kernel    the gradient, from the row, (m, s) and the slope; in passing the pairs added up (pair_sum_kernel without one)
 //
 // Memory bounds all of them but the smallest calls, which are bound by their two or three launches.  4096 rows of 152064 bf16 (2.49 GB
@@ -35,7 +35,6 @@ constexpr int kMostSummedRows = 16384, kShares = 256;      // rows whose terms o
 constexpr int kMostInline = 1024;      // sequences of a small call
 constexpr int kMostTableRows = 4096;   // its rows
 constexpr int kMostSmallRows = 2048;   // rows whose slopes and terms one workgroup computes
-constexpr int kMostPairRows = 512, kMostPairSeqs = 32;     // of a small call of the preference loss
 constexpr int kParts = 8192;           // parts of rows that the workspace holds
 
 // exp(x) for x <= 0 by the exponential instruction; results below 2^-126 are 0.
@@ -769,14 +768,14 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
 // ---------------------------------------------------------------------------------------------
 // preference loss
 // ---------------------------------------------------------------------------------------------
-// A pair, by LANES threads of which this is number t: log ratios, margin, slopes.  sum(x): over the LANES threads, in all of them.
-// Returns the pair's terms of the loss.  Rows outside every sequence are left to the first and the last pair.
-template <int LANES, typename F>
-__device__ __forceinline__ float4 finish_pair(const RowArgs &a, const PairArgs &p, int pair, int t, F &&sum) {
-    const int pairs = a.n_seq / 2;
+// A workgroup a pair: log ratios, margin, slopes and the pair's terms of the loss.  Rows outside every sequence are left to the first and
+// the last pair.
+__global__ __launch_bounds__(kTermThreads) void pair_kernel(RowArgs a, PairArgs p) {
+    __shared__ double s[kTermThreads / 64], s_ratio[2];
+    const int pairs = a.n_seq / 2, pair = blockIdx.x, t = threadIdx.x;
     const int start = max(a.seq_start[2 * pair], 0), mid = a.seq_start[2 * pair + 1], end = min(a.seq_start[2 * pair + 2], a.n_rows);
     double ratio[2] = {};
-    for (int row = start + t; row < end; row += LANES) {
+    for (int row = start + t; row < end; row += kTermThreads) {
         const float chosen = a.chosen[row];
         const double ref = p.ref_logprob ? (double)p.ref_logprob[row] : 0.0;
         const RowSum r = whole_row(a, row);
@@ -790,8 +789,14 @@ __device__ __forceinline__ float4 finish_pair(const RowArgs &a, const PairArgs &
         a.whole[row] = make_float2(r.m, r.s);
         if (a.token_logprob) a.token_logprob[row] = (float)logprob;
     }
-    ratio[0] = sum(ratio[0]);
-    ratio[1] = sum(ratio[1]);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const double sum = block_sum<kTermThreads / 64>(ratio[k], s);
+        if (t == 0) s_ratio[k] = sum;
+    }
+    __syncthreads();
+    ratio[0] = s_ratio[0];
+    ratio[1] = s_ratio[1];
     const double reward0 = (double)p.beta * ratio[0], reward1 = (double)p.beta * ratio[1];
     // The margin is a difference of sums in double; what becomes of it is good to single precision from there on.
     const float m = (float)(reward0 - reward1), e = expf(-fabsf(m)), tail = log1pf(e), sm = p.smoothing;
@@ -799,52 +804,27 @@ __device__ __forceinline__ float4 finish_pair(const RowArgs &a, const PairArgs &
     const float loss = (sm < 1.f ? (1.f - sm) * (fmaxf(-m, 0.f) + tail) : 0.f) + (sm > 0.f ? sm * (fmaxf(m, 0.f) + tail) : 0.f);
     const float small = e / (1.f + e), large = 1.f / (1.f + e);      // sigmoid(-|m|), sigmoid(|m|)
     const float slope = p.beta / (float)pairs * (sm * (m >= 0.f ? large : small) - (1.f - sm) * (m >= 0.f ? small : large)) * a.grad_scale;
-    if (t == 0 && p.log_ratio) {
-        p.log_ratio[2 * pair] = (float)ratio[0];
-        p.log_ratio[2 * pair + 1] = (float)ratio[1];
+    if (t == 0) {
+        a.terms[pair] = make_float4(loss, m > 0.f ? 1.f : 0.f, (float)reward0, (float)reward1);
+        if (p.log_ratio) {
+            p.log_ratio[2 * pair] = (float)ratio[0];
+            p.log_ratio[2 * pair + 1] = (float)ratio[1];
+        }
     }
-    for (int row = start + t; row < end; row += LANES) a.slope[row] = row < mid ? slope : -slope;
+    for (int row = start + t; row < end; row += kTermThreads) a.slope[row] = row < mid ? slope : -slope;
     auto outside = [&](int row) {
         a.whole[row] = make_float2(0.f, kNoRow);
         if (a.token_logprob) a.token_logprob[row] = 0.f;
     };
     if (pair == 0)
-        for (int row = t; row < min(start, a.n_rows); row += LANES) outside(row);
+        for (int row = t; row < min(start, a.n_rows); row += kTermThreads) outside(row);
     if (pair == pairs - 1)
-        for (int row = max(a.seq_start[a.n_seq], 0) + t; row < a.n_rows; row += LANES) outside(row);
-    return make_float4(loss, m > 0.f ? 1.f : 0.f, (float)reward0, (float)reward1);
-}
-
-__global__ __launch_bounds__(kTermThreads) void pair_kernel(RowArgs a, PairArgs p) {
-    __shared__ double s[kTermThreads / 64 + 1];
-    const float4 term = finish_pair<kTermThreads>(a, p, blockIdx.x, threadIdx.x, [&](double x) {
-        x = block_sum<kTermThreads / 64>(x, s);
-        if (threadIdx.x == 0) s[kTermThreads / 64] = x;
-        __syncthreads();
-        return s[kTermThreads / 64];
-    });
-    if (threadIdx.x == 0) a.terms[blockIdx.x] = term;
+        for (int row = max(a.seq_start[a.n_seq], 0) + t; row < a.n_rows; row += kTermThreads) outside(row);
 }
 
 __global__ __launch_bounds__(kTermThreads) void pair_sum_kernel(RowArgs a, PairArgs p) {
     __shared__ double s[kTermThreads / 64];
     sum_pairs<kTermThreads>(a, p, s);
-}
-
-// Both by one workgroup, a wavefront a pair: few pairs of few rows
-__global__ __launch_bounds__(kSumThreads) void pair_small_kernel(RowArgs a, PairArgs p) {
-    __shared__ double s[kSumThreads / 64];
-    const int lane = threadIdx.x & 63;
-    for (int pair = threadIdx.x >> 6; pair < a.n_seq / 2; pair += kSumThreads / 64) {
-        const float4 term = finish_pair<64>(a, p, pair, lane, [](double x) {
-#pragma unroll
-            for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off, 64);
-            return x;
-        });
-        if (lane == 0) a.terms[pair] = term;
-    }
-    __syncthreads();
-    sum_pairs<kSumThreads>(a, p, s);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -1010,12 +990,9 @@ int preference_loss(const sr_token_rows *x, const PairArgs &p, void *workspace, 
     return with_type(x->dtype, [&](auto *t) -> int {
         typedef std::remove_pointer_t<decltype(t)> T;
         if (a.n_rows > 0) SR_TRY(launch_row_stats<T>(a, plan.waves, stream));
-        const bool small = a.n_rows <= kMostPairRows && a.n_seq <= kMostPairSeqs;
-        if (small) pair_small_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(a, p);
-        else pair_kernel<<<dim3(a.n_seq / 2), dim3(kTermThreads), 0, stream>>>(a, p);
+        pair_kernel<<<dim3(a.n_seq / 2), dim3(kTermThreads), 0, stream>>>(a, p);
         SR_HIP(hipGetLastError());
-        if (a.n_rows > 0 && a.grad) return launch_logit_grad<T>(a, small ? PairArgs{} : p, plan.grad_waves, stream);
-        if (small) return SR_OK;
+        if (a.n_rows > 0 && a.grad) return launch_logit_grad<T>(a, p, plan.grad_waves, stream);
         pair_sum_kernel<<<dim3(1), dim3(kTermThreads), 0, stream>>>(a, p);
         SR_HIP(hipGetLastError());
         return SR_OK;
