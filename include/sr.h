@@ -294,7 +294,7 @@ int sr_grpo_loss_static(const double *logprob, const float *rewards, int n_group
  * receive log-probability 0 and a gradient of exactly 0.  An entry of -infinity is a token that cannot occur; a row whose
  * entries are all -infinity, or that holds NaN or +infinity, has log-probability NaN, and so has a counting row whose target
  * lies outside the vocabulary.  seq_start must not decrease; other values give unspecified results, but no access outside
- * the buffers.
+ * the buffers.  A token of probability 0 has log-probability -infinity and, with a reference that allows it, an infinite kl.
  *
  * Arithmetic: the logits are widened to single precision; maximum, sum of exponentials, loss and slopes are single
  * precision, sums over tokens double, added in a fixed order (the results are the same bit for bit from call to call); the

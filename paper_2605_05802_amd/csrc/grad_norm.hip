@@ -254,7 +254,7 @@ int take(const sr_tensor *tensors, int n_tensors, int at, TensorList *l) {
 
 int norm_and_clip(const sr_tensor *tensors, int n_tensors, float scale, float max_norm, bool clip, float *norm, void *workspace,
                   size_t workspace_bytes, hipStream_t stream) {
-    if (n_tensors < 0 || (n_tensors > 0 && !tensors) || !norm || !workspace || (uintptr_t)workspace % 16 ||
+    if (n_tensors < 0 || (n_tensors > 0 && !tensors) || !norm || (uintptr_t)norm % 4 || !workspace || (uintptr_t)workspace % 16 ||
         workspace_bytes < SR_GRAD_NORM_WORKSPACE || !std::isfinite(scale) || !std::isfinite(max_norm) || max_norm < 0.f)
         return SR_E_ARG;
     int64_t bytes = 0;                                   // of what the next launches read

@@ -132,6 +132,8 @@ template <typename V> __device__ __forceinline__ V read_uniform(const V *p) {
     typedef std::conditional_t<sizeof(V) == 8, uint64_t, uint32_t> bits;
     return __builtin_bit_cast(V, *(const __attribute__((address_space(4))) bits *)p);
 }
+// An entry of seq_start as an end of a range of rows, whatever it holds
+__device__ __forceinline__ int row_bound(const RowArgs &a, int row) { return min(max(row, 0), a.n_rows); }
 // the sequence of a row, or -1: the last one that begins at or before it
 __device__ __forceinline__ int sequence_of(const int32_t *seq_start, int n_seq, int row) {
     int lo = -1, hi = n_seq;
@@ -339,7 +341,7 @@ __device__ __forceinline__ void add_up(int n, int some, int *rows, int *used) {
 __global__ __launch_bounds__(kTermThreads) void seq_count_kernel(RowArgs a) {
     __shared__ int s_n, s_unused;
     const int seq = blockIdx.x, t = threadIdx.x;
-    const int from = max(a.seq_start[seq], 0), to = min(a.seq_start[seq + 1], a.n_rows);
+    const int from = row_bound(a, a.seq_start[seq]), to = row_bound(a, a.seq_start[seq + 1]);
     if (!a.mask) {
         if (t == 0) a.count[seq] = max(to - from, 0);
         return;
@@ -446,7 +448,7 @@ struct SeqTable {
         __syncthreads();
         int n = 0, some = 0;
         for (int i = t; i < a.n_seq; i += THREADS) {
-            const int from = max(start[i], 0), to = min(start[i + 1], a.n_rows);
+            const int from = row_bound(a, start[i]), to = row_bound(a, start[i + 1]);
             const int c = from >= to ? 0 : a.mask ? rank(to) - rank(from) : to - from;
             count[i] = c;
             n += c;
@@ -492,7 +494,7 @@ __device__ __forceinline__ float policy_row(const PolicyArgs &p, float2 info, fl
     *term = make_float4(out ? clipped : plain, 0.f, out ? 1.f : 0.f, info.x);
     if (p.ref_logprob) {
         const float d = ref_logprob - logprob, e = expm1f(d);
-        term->y = e - d;
+        term->y = e <= FLT_MAX ? e - d : e;                  // a token that the policy has given up: infinite, and no difference of infinities
         if (p.kl_coef != 0.f) slope = fmaf(-p.kl_coef, e, slope);
     }
     return slope * info.x;
@@ -680,7 +682,7 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
             zeros(row);
             mine = false;
         }
-        if (WAVES > 1) {                                     // one row: done, and where the row's loads are not conditional their number is known
+        if (WAVES > 1) {                                     // the workgroup's only row; behind this the number of loads under way is known
             if (!mine) return;
             mine = true;
         }
@@ -773,7 +775,7 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
 __global__ __launch_bounds__(kTermThreads) void pair_kernel(RowArgs a, PairArgs p) {
     __shared__ double s[kTermThreads / 64], s_ratio[2];
     const int pairs = a.n_seq / 2, pair = blockIdx.x, t = threadIdx.x;
-    const int start = max(a.seq_start[2 * pair], 0), mid = a.seq_start[2 * pair + 1], end = min(a.seq_start[2 * pair + 2], a.n_rows);
+    const int start = row_bound(a, a.seq_start[2 * pair]), end = row_bound(a, a.seq_start[2 * pair + 2]), mid = a.seq_start[2 * pair + 1];
     double ratio[2] = {};
     for (int row = start + t; row < end; row += kTermThreads) {
         const float chosen = a.chosen[row];
@@ -817,9 +819,9 @@ __global__ __launch_bounds__(kTermThreads) void pair_kernel(RowArgs a, PairArgs 
         if (a.token_logprob) a.token_logprob[row] = 0.f;
     };
     if (pair == 0)
-        for (int row = t; row < min(start, a.n_rows); row += kTermThreads) outside(row);
+        for (int row = t; row < start; row += kTermThreads) outside(row);
     if (pair == pairs - 1)
-        for (int row = max(a.seq_start[a.n_seq], 0) + t; row < a.n_rows; row += kTermThreads) outside(row);
+        for (int row = end + t; row < a.n_rows; row += kTermThreads) outside(row);
 }
 
 __global__ __launch_bounds__(kTermThreads) void pair_sum_kernel(RowArgs a, PairArgs p) {
@@ -830,10 +832,18 @@ __global__ __launch_bounds__(kTermThreads) void pair_sum_kernel(RowArgs a, PairA
 // ---------------------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------------------
+// Scalar loads drop the low bits of an address
+bool whole_words(std::initializer_list<const void *> pointers) {
+    for (const void *p : pointers)
+        if ((uintptr_t)p % 4) return false;
+    return true;
+}
+
 int check_rows(const sr_token_rows *x, const void *workspace, size_t bytes) {
     if (!x || !workspace || (uintptr_t)workspace % 16) return SR_E_ARG;
     if (x->dtype < SR_F32 || x->dtype > SR_F16 || x->n_rows < 0 || x->vocab < 1 || x->n_seq < 1) return SR_E_ARG;
     if (x->vocab > 1 << 30 || !x->seq_start || !std::isfinite(x->grad_scale)) return SR_E_ARG;
+    if (!whole_words({x->targets, x->seq_start, x->token_logprob})) return SR_E_ARG;
     if (x->n_rows > 1 << 26 || x->n_seq > 1 << 23) return SR_E_LIMIT;     // threads of a launch
     if (bytes < SR_TOKEN_LOSS_WORKSPACE(x->n_rows, x->n_seq)) return SR_E_ARG;
     if (x->n_rows == 0) return SR_OK;
@@ -1009,6 +1019,7 @@ extern "C" int sr_policy_loss(const sr_token_rows *rows, const float *old_logpro
     if (!(opt->clip_low >= 0.f && opt->clip_low <= 1.f) || !(opt->clip_high >= 0.f) || !std::isfinite(opt->clip_high)) return SR_E_ARG;
     if (!std::isfinite(opt->kl_coef) || (opt->kl_coef != 0.f && !ref_logprob && rows->n_rows > 0)) return SR_E_ARG;
     if (opt->reduce < SR_MEAN_TOKENS || opt->reduce > SR_MEAN_SUMS) return SR_E_ARG;
+    if (!sr::whole_words({old_logprob, ref_logprob, advantages, stats})) return SR_E_ARG;
     const sr::PolicyArgs p = {old_logprob, ref_logprob, advantages, opt->clip_low, opt->clip_high, opt->kl_coef, opt->reduce, stats};
     return sr::policy_loss(rows, p, workspace, (hipStream_t)stream);
 }
@@ -1016,6 +1027,7 @@ extern "C" int sr_policy_loss(const sr_token_rows *rows, const float *old_logpro
 extern "C" int sr_preference_loss(const sr_token_rows *rows, const float *ref_logprob, float beta, float label_smoothing,
                                   float *log_ratio, float *stats, void *workspace, size_t workspace_bytes, void *stream) {
     SR_TRY(sr::check_rows(rows, workspace, workspace_bytes));
+    if (!sr::whole_words({ref_logprob, log_ratio, stats})) return SR_E_ARG;
     if (!stats || rows->n_seq % 2 || !std::isfinite(beta) || !(label_smoothing >= 0.f && label_smoothing <= 1.f)) return SR_E_ARG;
     const sr::PairArgs p = {ref_logprob, beta, label_smoothing, log_ratio, stats};
     return sr::preference_loss(rows, p, workspace, (hipStream_t)stream);

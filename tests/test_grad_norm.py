@@ -200,7 +200,7 @@ def test_refusals():
     one = lambda data=4096, out=None, n=5, dtype=0, out_dtype=0: (sr.Tensor * 1)(sr.Tensor(data, out, n, dtype, out_dtype))
     clip = lambda a=one(), n=1, scale=1.0, limit=1.0, norm=fake, ws=fake, size=sr.GRAD_NORM_WORKSPACE: L.sr_clip_grad_norm(
         a, n, scale, limit, norm, ws, size, None)
-    for r in (clip(a=None), clip(n=-1), clip(scale=math.nan), clip(limit=math.inf), clip(limit=-1.0), clip(norm=None), clip(ws=None),
+    for r in (clip(a=None), clip(n=-1), clip(scale=math.nan), clip(limit=math.inf), clip(limit=-1.0), clip(norm=None), clip(norm=ctypes.c_void_p(4098)), clip(ws=None),
               clip(ws=ctypes.c_void_p(4100)), clip(size=sr.GRAD_NORM_WORKSPACE - 1), clip(a=one(data=None)), clip(a=one(data=4098)),
               clip(a=one(n=-1)), clip(a=one(n=1 << 50)), clip(a=one(n=(1 << 36) + 1)), clip(a=one(dtype=3)), clip(a=one(dtype=1, out=8192, out_dtype=2)),
               clip(a=one(out=8192, out_dtype=1)), clip(a=one(dtype=1, out=8193, out_dtype=1)), clip(a=one(dtype=1, out=4096, out_dtype=0))):

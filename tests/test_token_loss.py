@@ -239,6 +239,38 @@ def test_rows_without_a_distribution_say_nan(rows, vocab):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,vocab", [(9, 800), (9, 33003), (200, 60001), (9, 152064)])
+def test_a_token_that_cannot_occur(rows, vocab):
+    """Log-probability -infinity, ratio 0: no gradient without a KL term whatever the advantage, an infinite KL term with one."""
+    x = make(rows, 2, vocab, torch.bfloat16, 6)
+    x["logits"][2, int(x["targets"][2])] = float("-inf")
+    x["advantages"].copy_(torch.tensor([1.5, -0.5], device="cuda"))
+    stats, lp, g = run_policy(x, "tokens", 0.0, use_ref=True)
+    assert lp[2].item() == float("-inf") and bool(torch.isfinite(lp[3:]).all())
+    assert bool((g[2] == 0).all()) and bool(torch.isfinite(g).all())
+    assert bool(torch.isfinite(stats[:2]).all()) and stats[2].item() == float("inf")
+    stats, _, g = run_policy(x, "tokens", 0.04)
+    assert stats[0].item() == float("inf") and bool(torch.isfinite(g[3:]).all()) and bool(torch.isfinite(g[:2]).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,vocab,n_seq", [(300, 500, 6), (40, 9000, 2), (5000, 64, 1500), (260, 50001, 4)])
+def test_starts_that_make_no_sense_stay_inside_the_buffers(rows, vocab, n_seq):
+    """Decreasing, negative and huge sequence starts: unspecified results, nothing else written."""
+    x = make(rows, n_seq, vocab, torch.bfloat16, 6, masked=0.3)
+    rng = np.random.default_rng(1)
+    top = 2 ** 31 - 1
+    for starts in ([top] * (n_seq + 1), [-top - 1] * (n_seq + 1), rng.integers(-5, rows + 5, n_seq + 1).tolist(),
+                   [rows] + [0] * (n_seq - 1) + [top], [-3] + [top] * (n_seq - 1) + [rows // 2], [top] + [5] * n_seq):
+        y = dict(x, seq_start=torch.tensor(starts, dtype=torch.int64, device="cuda").to(torch.int32))
+        for run in (lambda: run_policy(y, "sequences", 0.04), lambda: run_policy(y, "sequences", 0.04, grad=False), lambda: run_pairs(y, 0.1, 0.0)):
+            before = [x["logits"].clone(), x["targets"].clone(), x["old_logprob"].clone()]
+            run()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(before, (x["logits"], x["targets"], x["old_logprob"])))
+
+
+@pytest.mark.gpu
 def test_nothing_counts():
     for rows, vocab in ((5, 50), (5, 20000), (300, 9000)):
         x = make(rows, 2, vocab, torch.bfloat16, 1, masked=0.5)
@@ -510,7 +542,8 @@ def _rows(**kw):
 
 @pytest.mark.parametrize("bad", [dict(logits=None), dict(targets=None), dict(seq_start=None), dict(dtype=3), dict(dtype=-1), dict(n_rows=-1), dict(vocab=0),
                                  dict(n_seq=0), dict(ld_logits=99), dict(ld_grad=99), dict(logits=4097), dict(grad=8193), dict(grad_scale=math.nan),
-                                 dict(dtype=0, logits=4098), dict(grad=4096, ld_grad=104), dict(vocab=(1 << 30) + 1, ld_logits=1 << 31, ld_grad=1 << 31)])
+                                 dict(dtype=0, logits=4098), dict(grad=4096, ld_grad=104), dict(vocab=(1 << 30) + 1, ld_logits=1 << 31, ld_grad=1 << 31),
+                                 dict(targets=4097), dict(seq_start=4098), dict(token_logprob=4099)])
 def test_refusals_of_rows(bad):
     L, fake = sr.lib(), ctypes.c_void_p(4096)                      # never dereferenced: validation fails first
     big = 1 << 20
@@ -530,6 +563,8 @@ def test_refusals_of_options_and_workspaces():
               sr.PolicyOptions(0.2, 0.2, 0.0, 3), sr.PolicyOptions(0.2, 0.2, 0.0, -1), sr.PolicyOptions(0.2, 0.2, 0.1, 0)):
         assert p(o) == sr.SR_E_ARG
     assert p(good, old=None) == p(good, adv=None) == p(good, stats=None) == p(good, ws=None) == sr.SR_E_ARG
+    odd = ctypes.c_void_p(4098)
+    assert p(good, old=odd) == p(good, ref=odd) == p(good, adv=odd) == p(good, stats=odd) == sr.SR_E_ARG
     assert p(good, ws=ctypes.c_void_p(4104)) == p(good, n=need - 1) == sr.SR_E_ARG
     assert L.sr_policy_loss(None, fake, None, fake, ctypes.byref(good), fake, fake, big, None) == sr.SR_E_ARG
     assert L.sr_policy_loss(rows, fake, None, fake, None, fake, fake, big, None) == sr.SR_E_ARG
