@@ -390,6 +390,24 @@ int sr_clip_grad_norm(const sr_tensor *host_tensors, int n_tensors, float scale,
                       size_t workspace_bytes, void *stream);
 
 /*
+ * The same for a list that stays: sr_plan_tensors copies it to `table` (device memory of the caller, 16-byte aligned,
+ * SR_TENSOR_TABLE_BYTES(n_tensors) bytes, kept as long as the plan is used), waits for the stream, and fills *host_plan.  The planned
+ * calls then take any number of tensors in one launch a pass, on any stream.  A plan names addresses: it has to be made again when
+ * a tensor moves.  Results are those of the calls above but for the order in which the squares are added.
+ * SR_E_ARG as above; SR_E_LIMIT: more than 2^31 pieces of 8192 elements; SR_E_NOMEM, SR_E_HIP.
+ */
+#define SR_TENSOR_TABLE_BYTES(n_tensors) ((size_t)64 + (size_t)24 * (size_t)(n_tensors))
+typedef struct {
+    const void *table;
+    int64_t chunks, keep;      /* the library's */
+    int32_t n_tensors, reserved;
+} sr_tensor_plan;
+int sr_plan_tensors(const sr_tensor *host_tensors, int n_tensors, void *table, size_t table_bytes, sr_tensor_plan *host_plan, void *stream);
+int sr_planned_grad_norm(const sr_tensor_plan *host_plan, float scale, float *norm, void *workspace, size_t workspace_bytes, void *stream);
+int sr_planned_clip_grad_norm(const sr_tensor_plan *host_plan, float scale, float max_norm, float *norm, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/*
  * The in-group divergence signals of Appendix B at step K, and the gates of Eq. 2 and of
  * Appendix E (Eq. 3), for groups whose members may have finished early (no context needed).
  *

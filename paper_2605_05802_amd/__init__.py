@@ -21,7 +21,8 @@ EXPORTS = ("sr_init", "sr_destroy", "sr_load_weights", "sr_prefill_chunk", "sr_d
            "sr_get_live_map", "sr_stats", "sr_strerror", "sr_profile", "sr_profile_read", "sr_signals_batch",
            "sr_score_chunk", "sr_get_logprob", "sr_grpo_loss", "sr_finish_sequences", "sr_grpo_loss_static",
            "sr_probe_hbm", "sr_probe_mfma_bf16", "sr_probe_mfma_under_loads", "sr_gate_batch_antidiag",
-           "sr_probe_decode_attention", "sr_policy_loss", "sr_preference_loss", "sr_grad_norm", "sr_clip_grad_norm")
+           "sr_probe_decode_attention", "sr_policy_loss", "sr_preference_loss", "sr_grad_norm", "sr_clip_grad_norm",
+           "sr_plan_tensors", "sr_planned_grad_norm", "sr_planned_clip_grad_norm")
 
 # ways to take the mean (sr_reduce)
 REDUCE = {"tokens": 0, "sequences": 1, "sums": 2}
@@ -79,6 +80,11 @@ class Tensor(ctypes.Structure):
                 ("out_dtype", ctypes.c_int32)]
 
 
+class TensorPlan(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("chunks", ctypes.c_int64), ("keep", ctypes.c_int64), ("n_tensors", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
 class KernelTime(ctypes.Structure):
     _fields_ = [("launches", ctypes.c_int64), ("total_ms", ctypes.c_double)]
 
@@ -130,6 +136,10 @@ def lib():
                                          ctypes.c_size_t, vp]
         L.sr_grad_norm.argtypes = [vp, ci, ctypes.c_float, vp, vp, ctypes.c_size_t, vp]
         L.sr_clip_grad_norm.argtypes = [vp, ci, ctypes.c_float, ctypes.c_float, vp, vp, ctypes.c_size_t, vp]
+        plan = ctypes.POINTER(TensorPlan)
+        L.sr_plan_tensors.argtypes = [vp, ci, vp, ctypes.c_size_t, plan, vp]
+        L.sr_planned_grad_norm.argtypes = [plan, ctypes.c_float, vp, vp, ctypes.c_size_t, vp]
+        L.sr_planned_clip_grad_norm.argtypes = [plan, ctypes.c_float, ctypes.c_float, vp, vp, ctypes.c_size_t, vp]
         L.sr_finish_sequences.argtypes = [vp, vp, ctypes.POINTER(ci), vp]
         L.sr_set_actions.argtypes = [vp, ci, vp, vp]
         L.sr_get_actions.argtypes = [vp, vp, vp]
@@ -248,6 +258,12 @@ def _of_type(t, kind: str, n: int, what: str):
     return t.data_ptr()
 
 
+def _on_device(where, *tensors):
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            raise SrError(SR_E_ARG, f"{where}: device tensors expected")
+
+
 def _token_rows(where, logits, targets, seq_start, mask, grad, token_logprob, grad_scale):
     dtype = _dtypes().get(logits.dtype)
     if dtype is None or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
@@ -275,9 +291,10 @@ def sr_policy_loss(logits, targets, seq_start, old_logprob, advantages, stats, w
     workspace: device bytes, token_loss_workspace(rows, sequences) of them; reduce: "tokens", "sequences" or "sums"."""
     rows, n, n_seq = _token_rows("sr_policy_loss", logits, targets, seq_start, mask, grad, token_logprob, grad_scale)
     opt = PolicyOptions(clip_low, clip_high, kl_coef, REDUCE[reduce])
-    _check(lib().sr_policy_loss(rows, _of_type(old_logprob, "f4", n, "old_logprob"), _of_type(ref_logprob, "f4", n, "ref_logprob"),
-                                _of_type(advantages, "f4", n_seq, "advantages"), opt, _of_type(stats, "f4", 4, "stats"),
-                                workspace.data_ptr(), workspace.nbytes, _stream(stream)), "sr_policy_loss")
+    old, ref = _of_type(old_logprob, "f4", n, "old_logprob"), _of_type(ref_logprob, "f4", n, "ref_logprob")
+    adv, to = _of_type(advantages, "f4", n_seq, "advantages"), _of_type(stats, "f4", 4, "stats")
+    _on_device("sr_policy_loss", logits, targets, seq_start, mask, grad, token_logprob, old_logprob, ref_logprob, advantages, stats, workspace)
+    _check(lib().sr_policy_loss(rows, old, ref, adv, opt, to, workspace.data_ptr(), workspace.nbytes, _stream(stream)), "sr_policy_loss")
 
 
 def sr_preference_loss(logits, targets, seq_start, stats, workspace, *, mask=None, ref_logprob=None, grad=None,
@@ -286,15 +303,18 @@ def sr_preference_loss(logits, targets, seq_start, stats, workspace, *, mask=Non
     sr_policy_loss.  stats float32 [4] receives loss, fraction of pairs in the right order, mean reward of the preferred
     and of the other sequences; log_ratio float32 [sequences]."""
     rows, n, n_seq = _token_rows("sr_preference_loss", logits, targets, seq_start, mask, grad, token_logprob, grad_scale)
-    _check(lib().sr_preference_loss(rows, _of_type(ref_logprob, "f4", n, "ref_logprob"), beta, label_smoothing,
-                                    _of_type(log_ratio, "f4", n_seq, "log_ratio"), _of_type(stats, "f4", 4, "stats"),
-                                    workspace.data_ptr(), workspace.nbytes, _stream(stream)), "sr_preference_loss")
+    ref, ratio, to = _of_type(ref_logprob, "f4", n, "ref_logprob"), _of_type(log_ratio, "f4", n_seq, "log_ratio"), _of_type(stats, "f4", 4, "stats")
+    _on_device("sr_preference_loss", logits, targets, seq_start, mask, grad, token_logprob, ref_logprob, log_ratio, stats, workspace)
+    _check(lib().sr_preference_loss(rows, ref, beta, label_smoothing, ratio, to, workspace.data_ptr(), workspace.nbytes, _stream(stream)),
+           "sr_preference_loss")
 
 
 class TensorList:
-    """The tensors of a norm, as the C boundary takes them; keeps them alive.  To be built again when one of them is replaced."""
+    """The tensors of a norm, as the C boundary takes them; keeps them alive.  To be built again when one of them is replaced.
+    plan: copied to the device as well (waits for the current stream); the list is then kept until the last call with it has
+    finished, where that runs on another stream."""
 
-    def __init__(self, tensors, out=None):
+    def __init__(self, tensors, out=None, plan=False):
         self.tensors, self.out = list(tensors), None if out is None else list(out)
         if self.out is not None and len(self.out) != len(self.tensors):
             raise SrError(SR_E_ARG, "tensor_list: one output per tensor expected")
@@ -304,34 +324,47 @@ class TensorList:
             o = t if self.out is None else self.out[i]
             if t.dtype not in types or o.dtype not in types or not t.is_contiguous() or not o.is_contiguous() or o.numel() != t.numel():
                 raise SrError(SR_E_ARG, f"tensor_list: contiguous float32, bfloat16 or float16 tensors expected ({i})")
+            if not (t.is_cuda and o.is_cuda):
+                raise SrError(SR_E_ARG, f"tensor_list: device tensors expected ({i})")
             rows.append((t.data_ptr(), o.data_ptr(), t.numel(), types[t.dtype], types[o.dtype]))
         self.array = (Tensor * len(rows))(*rows)
+        self.plan = None
+        if plan and rows:
+            import torch
+            self.table = torch.empty(64 + 24 * len(rows), dtype=torch.uint8, device=self.tensors[0].device)
+            self.plan = TensorPlan()
+            _check(lib().sr_plan_tensors(self.array, len(rows), self.table.data_ptr(), self.table.nbytes, self.plan, _stream(None)),
+                   "sr_plan_tensors")
 
 
 def tensor_list(tensors, out=None) -> TensorList:
-    """tensors: contiguous float32, bfloat16 or float16 device tensors; out: where the scaled tensors go (same type, or
-    float32), None = in place."""
-    return TensorList(tensors, out)
+    """A list to be kept: tensors: contiguous float32, bfloat16 or float16 device tensors; out: where the scaled tensors go
+    (same type, or float32), None = in place.  Not to be made while a graph is captured; to be used there it is made before."""
+    return TensorList(tensors, out, plan=True)
 
 
-def _norm_args(tensors, norm, workspace):
+def _norm_call(tensors, name, numbers, norm, workspace, stream):
     if not isinstance(tensors, TensorList):
         tensors = TensorList(tensors)
     _dtypes()
-    return (tensors.array, len(tensors.array)), (_of_type(norm, "f4", 1, "norm"), workspace.data_ptr(), workspace.nbytes)
+    to = _of_type(norm, "f4", 1, "norm")
+    _on_device(name, norm, workspace)
+    tail = to, workspace.data_ptr(), workspace.nbytes, _stream(stream)
+    if tensors.plan is not None:
+        _check(getattr(lib(), "sr_planned_" + name)(tensors.plan, *numbers, *tail), "sr_" + name)
+    else:
+        _check(getattr(lib(), "sr_" + name)(tensors.array, len(tensors.array), *numbers, *tail), "sr_" + name)
 
 
 def sr_grad_norm(tensors, norm, workspace, *, scale=1.0, stream=None):
     """norm (device float32 [1]) = |scale| * the 2-norm over all tensors (a tensor_list, or a list of tensors);
     workspace: GRAD_NORM_WORKSPACE device bytes."""
-    head, tail = _norm_args(tensors, norm, workspace)
-    _check(lib().sr_grad_norm(*head, scale, *tail, _stream(stream)), "sr_grad_norm")
+    _norm_call(tensors, "grad_norm", (scale,), norm, workspace, stream)
 
 
 def sr_clip_grad_norm(tensors, max_norm: float, norm, workspace, *, scale=1.0, stream=None):
     """sr_grad_norm, and the tensors times scale * min(1, max_norm / norm), in place or to the list's outputs."""
-    head, tail = _norm_args(tensors, norm, workspace)
-    _check(lib().sr_clip_grad_norm(*head, scale, max_norm, *tail, _stream(stream)), "sr_clip_grad_norm")
+    _norm_call(tensors, "clip_grad_norm", (scale, max_norm), norm, workspace, stream)
 
 
 def sr_probe_hbm(src, dst, mode: int, iters: int = 10, stream=None) -> float:

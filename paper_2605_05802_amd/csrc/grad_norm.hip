@@ -7,10 +7,12 @@
 // behind (the second pass over 0.47 GB of bf16 into fp32 took 265 us where all had been read so, and 233 where none had).
 // 2 GB of bf16 into bf16: 290 + 648 us (6.2 TB/s) of 956; the list of a small model: two launches, which cost more than their work.
 //
-// The list travels in the kernel arguments, kListTensors tensors a launch: no copy to the device, nothing kept between calls, and a
-// captured launch holds its own list.  A chunk of kChunk elements is a workgroup's step; its tensor is found by comparing 64 first
-// chunks at a time.
+// A list travels in the kernel arguments, kListTensors tensors a launch: no copy to the device, nothing kept between calls, and a
+// captured launch holds its own list.  A planned list lies on the device, of any length, for one launch a pass: 339 tensors of 20 000
+// elements on average take 17 us, 24 in the arguments of two.  A chunk of kChunk elements is a workgroup's step; its tensor is found by
+// comparing 64 first chunks at a time.
 #include <cmath>
+#include <cstdlib>
 
 #include "row_vectors.h"
 
@@ -18,6 +20,7 @@ namespace sr {
 namespace {
 
 constexpr int kListTensors = 184;      // with the hidden ones 4 KB of kernel arguments
+constexpr int kLdsTensors = 512;       // of a list that square_sum_kernel copies to LDS
 constexpr int kChunk = 8192;           // elements
 constexpr int kNormThreads = 256;
 constexpr int kMostBlocks = 1024;      // workgroups of a launch
@@ -38,6 +41,13 @@ struct TensorList {
 };
 static_assert(sizeof(TensorList) + 32 + 256 <= 4096, "kernel arguments");
 
+// The same on the device
+struct TensorTable {
+    const uint64_t *data, *out;
+    const uint32_t *first;
+    int32_t tensors;
+};
+
 struct Chunk {
     char *data, *out;                  // of the chunk's first element
     int n, type, out_type;
@@ -57,21 +67,20 @@ __device__ __forceinline__ Chunk chunk_of(uint64_t data, uint64_t out, uint32_t 
     return c;
 }
 
-// The workgroup's copy of the list
+// The workgroup's copy of a list of at most kLdsTensors
 struct ListInLds {
-    uint64_t data[kListTensors];
-    uint32_t first[256];               // behind the tensors: no chunk
+    uint64_t data[kLdsTensors];
+    uint32_t first[kLdsTensors + 64];  // behind the tensors: no chunk
 
-    __device__ __forceinline__ void fill(const TensorList &l) {
-        const int i = threadIdx.x;
-        if (i < l.tensors) data[i] = l.data[i];
-        first[i] = i <= l.tensors ? l.first[i] : 0xffffffffu;
+    template <typename List>
+    __device__ __forceinline__ void fill(const List &l) {
+        for (int i = threadIdx.x; i < l.tensors; i += kNormThreads) data[i] = l.data[i];
+        for (int i = threadIdx.x; i < (l.tensors & ~63) + 64; i += kNormThreads) first[i] = i <= l.tensors ? l.first[i] : 0xffffffffu;
     }
     // Every wavefront for itself: tensors that begin at or before the chunk, 64 compared at a time
-    __device__ __forceinline__ Chunk find(uint32_t chunk) const {
+    __device__ __forceinline__ Chunk find(int tensors, uint32_t chunk) const {
         int t = -1;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) t += __popcll(__ballot(first[64 * k + (threadIdx.x & 63)] <= chunk));
+        for (int k = 0; k <= tensors; k += 64) t += __popcll(__ballot(first[k + (threadIdx.x & 63)] <= chunk));
         return chunk_of(data[t], 0, first[t], first[t + 1], chunk);
     }
 };
@@ -85,7 +94,19 @@ __device__ __forceinline__ Chunk find_chunk(const TensorList &l, uint32_t chunk)
     t = __builtin_amdgcn_readfirstlane(t);
     return chunk_of(l.data[t], l.out[t], l.first[t], l.first[t + 1], chunk);
 }
-static_assert(kNormThreads == 256 && kListTensors < 256, "one entry a thread");
+// ... and from a table: the one of 64 shares of what is left that the chunk lies in, until that is one tensor
+__device__ __forceinline__ Chunk find_chunk(const TensorTable &l, uint32_t chunk) {
+    int t = 0;
+    for (int n = l.tensors; n > 1;) {
+        const int step = (n + 63) / 64, i = (int)(threadIdx.x & 63) * step;
+        const int past = __popcll(__ballot(i < n && l.first[t + i] <= chunk)) - 1;     // the first one is
+        t += past * step;
+        n = min(step, n - past * step);
+    }
+    t = __builtin_amdgcn_readfirstlane(t);
+    return chunk_of(read_uniform(l.data + t), read_uniform(l.out + t), read_uniform(l.first + t), read_uniform(l.first + t + 1), chunk);
+}
+static_assert(kListTensors <= kLdsTensors && kLdsTensors % 64 == 0, "capacity");
 
 // f(vector j of the thread, its element) for the chunk's whole vectors of N elements, j known to the compiler; WHOLE: all are there
 template <int N, bool WHOLE, typename F>
@@ -126,15 +147,17 @@ __device__ __forceinline__ double squares(const T *p, int n, bool keep) {
 }
 
 // add: the slots hold the sums of an earlier launch of the same call; keep: chunks from here on are read again by scale_kernel
-__global__ __launch_bounds__(kNormThreads) void square_sum_kernel(TensorList l, double *__restrict__ slots, int add, uint32_t keep) {
+template <typename List>
+__global__ __launch_bounds__(kNormThreads) void square_sum_kernel(List l, double *__restrict__ slots, int add, uint32_t keep) {
     __shared__ ListInLds list;
     __shared__ double s[kNormThreads / 64];
-    list.fill(l);
+    const bool in_lds = l.tensors <= kLdsTensors;
+    if (in_lds) list.fill(l);
     __syncthreads();
-    const uint32_t chunks = list.first[l.tensors];
+    const uint32_t chunks = l.first[l.tensors];
     double acc = 0.0;
     for (uint32_t k = blockIdx.x; k < chunks; k += gridDim.x) {
-        const Chunk c = list.find(k);
+        const Chunk c = in_lds ? list.find(l.tensors, k) : find_chunk(l, k);
         acc += c.type == SR_F32    ? squares((const float *)c.data, c.n, k >= keep)
                : c.type == SR_BF16 ? squares((const __bf16 *)c.data, c.n, k >= keep)
                                    : squares((const f16_t *)c.data, c.n, k >= keep);
@@ -199,10 +222,12 @@ __device__ __forceinline__ void scale_chunk(const Chunk &k, F &&factor) {
 }
 
 // One chunk a workgroup, in the order of the list: 2 GB of bf16 in 657 us, 732 with 1024 workgroups that take chunks in turn
-__global__ __launch_bounds__(kNormThreads) void scale_kernel(TensorList l, const double *__restrict__ slots, int used, float scale,
+// chunk0: that of the launch's first workgroup
+template <typename List>
+__global__ __launch_bounds__(kNormThreads) void scale_kernel(List l, uint32_t chunk0, const double *__restrict__ slots, int used, float scale,
                                                              float max_norm, float *__restrict__ norm_out) {
     __shared__ double s[kNormThreads / 64 + 1];
-    const Chunk k = find_chunk(l, blockIdx.x);
+    const Chunk k = find_chunk(l, chunk0 + blockIdx.x);
     auto factor = [&]() __attribute__((always_inline)) {     // holds barriers: once, by the whole workgroup
         const double norm = fabs((double)scale) * sqrt(sum_slots(slots, used, s));
         if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
@@ -233,6 +258,12 @@ int check_tensor(const sr_tensor &t, bool clip) {
     return t.out == t.data && t.out_dtype != t.dtype ? SR_E_ARG : SR_OK;
 }
 
+uint64_t packed_data(const sr_tensor &t) {
+    return (uint64_t)(uintptr_t)t.data | (uint64_t)(t.n % kChunk) << kAddressBits | (uint64_t)t.dtype << kTypeShift;
+}
+uint64_t packed_out(const sr_tensor &t) {
+    return (uint64_t)(uintptr_t)(t.out ? t.out : t.data) | (uint64_t)(t.out ? t.out_dtype : t.dtype) << kTypeShift;
+}
 int64_t tensor_bytes(const sr_tensor &t) { return t.n * (t.dtype == SR_F32 ? 4 : 2); }
 
 // A launch's share of the list: tensors from `at` on; returns where the next share begins.  A launch has at most kMostChunks chunks.
@@ -245,18 +276,24 @@ int take(const sr_tensor *tensors, int n_tensors, int at, TensorList *l) {
         const int64_t chunks = (t.n + kChunk - 1) / kChunk + l->first[l->tensors];
         if (chunks > kMostChunks) break;
         const int i = l->tensors++;
-        l->data[i] = (uint64_t)(uintptr_t)t.data | (uint64_t)(t.n % kChunk) << kAddressBits | (uint64_t)t.dtype << kTypeShift;
-        l->out[i] = (uint64_t)(uintptr_t)(t.out ? t.out : t.data) | (uint64_t)(t.out ? t.out_dtype : t.dtype) << kTypeShift;
+        l->data[i] = packed_data(t);
+        l->out[i] = packed_out(t);
         l->first[i + 1] = (uint32_t)chunks;
     }
     return at;
 }
 
+int check_norm(float scale, float max_norm, const float *norm, const void *workspace, size_t workspace_bytes) {
+    return norm && (uintptr_t)norm % 4 == 0 && workspace && (uintptr_t)workspace % 16 == 0 && workspace_bytes >= SR_GRAD_NORM_WORKSPACE &&
+                   std::isfinite(scale) && std::isfinite(max_norm) && max_norm >= 0.f
+               ? SR_OK
+               : SR_E_ARG;
+}
+
 int norm_and_clip(const sr_tensor *tensors, int n_tensors, float scale, float max_norm, bool clip, float *norm, void *workspace,
                   size_t workspace_bytes, hipStream_t stream) {
-    if (n_tensors < 0 || (n_tensors > 0 && !tensors) || !norm || (uintptr_t)norm % 4 || !workspace || (uintptr_t)workspace % 16 ||
-        workspace_bytes < SR_GRAD_NORM_WORKSPACE || !std::isfinite(scale) || !std::isfinite(max_norm) || max_norm < 0.f)
-        return SR_E_ARG;
+    if (n_tensors < 0 || (n_tensors > 0 && !tensors)) return SR_E_ARG;
+    SR_TRY(check_norm(scale, max_norm, norm, workspace, workspace_bytes));
     int64_t bytes = 0;                                   // of what the next launches read
     for (int i = 0; i < n_tensors; ++i) {
         SR_TRY(check_tensor(tensors[i], clip));
@@ -295,7 +332,80 @@ int norm_and_clip(const sr_tensor *tensors, int n_tensors, float scale, float ma
     for (int at = 0; clip && at < n_tensors;) {
         at = take(tensors, n_tensors, at, &l);
         if (!l.tensors) continue;
-        scale_kernel<<<dim3(l.first[l.tensors]), dim3(kNormThreads), 0, stream>>>(l, slots, used, scale, max_norm, out);
+        scale_kernel<<<dim3(l.first[l.tensors]), dim3(kNormThreads), 0, stream>>>(l, 0u, slots, used, scale, max_norm, out);
+        SR_HIP(hipGetLastError());
+        out = nullptr;
+    }
+    return SR_OK;
+}
+
+// A planned list's table: packed data, packed outputs, first chunks
+TensorTable table_of(const sr_tensor_plan &p) {
+    const uint64_t *t = (const uint64_t *)p.table;
+    return TensorTable{t, t + p.n_tensors, (const uint32_t *)(t + 2 * (size_t)p.n_tensors), p.n_tensors};
+}
+
+int plan_tensors(const sr_tensor *tensors, int n_tensors, void *table, size_t table_bytes, sr_tensor_plan *plan, hipStream_t stream) {
+    if (n_tensors < 0 || (n_tensors > 0 && !tensors) || !table || (uintptr_t)table % 16 || !plan) return SR_E_ARG;
+    if (table_bytes < SR_TENSOR_TABLE_BYTES(n_tensors)) return SR_E_ARG;
+    int64_t bytes = 0, chunks = 0, keep = 0;
+    int used = 0;
+    for (int i = 0; i < n_tensors; ++i) {
+        SR_TRY(check_tensor(tensors[i], true));
+        if (tensors[i].n == 0) continue;
+        bytes += tensor_bytes(tensors[i]);
+        chunks += (tensors[i].n + kChunk - 1) / kChunk;
+        ++used;
+    }
+    if (chunks > INT32_MAX) return SR_E_LIMIT;
+    const size_t size = (size_t)20 * used + 4;
+    char *host = (char *)malloc(size);
+    if (!host) return SR_E_NOMEM;
+    uint64_t *data = (uint64_t *)host, *out = data + used;
+    uint32_t *first = (uint32_t *)(out + used);
+    int at = 0;
+    first[0] = 0;
+    for (int i = 0; i < n_tensors; ++i) {
+        const sr_tensor &t = tensors[i];
+        if (t.n == 0) continue;
+        data[at] = packed_data(t);
+        out[at] = packed_out(t);
+        first[at + 1] = first[at] + (uint32_t)((t.n + kChunk - 1) / kChunk);
+        const int64_t n = tensor_bytes(t), before = bytes - kKeepBytes;
+        if (before > 0) keep += ((before < n ? before : n) / (t.dtype == SR_F32 ? 4 : 2) + kChunk - 1) / kChunk;
+        bytes -= n;
+        ++at;
+    }
+    hipError_t e = hipMemcpyAsync(table, host, size, hipMemcpyHostToDevice, stream);
+    if (e == hipSuccess) e = hipStreamSynchronize(stream);
+    free(host);
+    SR_HIP(e);
+    *plan = sr_tensor_plan{table, chunks, keep, used, 0};
+    return SR_OK;
+}
+
+int planned_norm_and_clip(const sr_tensor_plan *plan, float scale, float max_norm, bool clip, float *norm, void *workspace,
+                          size_t workspace_bytes, hipStream_t stream) {
+    if (!plan || !plan->table || plan->n_tensors < 0 || plan->chunks < plan->n_tensors || plan->chunks > INT32_MAX) return SR_E_ARG;
+    SR_TRY(check_norm(scale, max_norm, norm, workspace, workspace_bytes));
+    double *slots = (double *)workspace;
+    const TensorTable l = table_of(*plan);
+    const int64_t chunks = l.tensors ? plan->chunks : 0;
+    int used = chunks < kMostBlocks ? (int)chunks : kMostBlocks;
+    if (used) {
+        square_sum_kernel<<<dim3(used), dim3(kNormThreads), 0, stream>>>(l, slots, 0, clip ? (uint32_t)plan->keep : UINT32_MAX);
+        SR_HIP(hipGetLastError());
+    }
+    const bool alone = !clip || used == 0 || chunks > kMostSummed;
+    if (alone) {
+        norm_kernel<<<dim3(1), dim3(kNormThreads), 0, stream>>>(slots, used, scale, norm);
+        SR_HIP(hipGetLastError());
+        used = 1;
+    }
+    float *out = alone ? nullptr : norm;
+    for (int64_t at = 0; clip && at < chunks; at += kMostChunks) {
+        const int64_t n = chunks - at < kMostChunks ? chunks - at : kMostChunks;
+        scale_kernel<<<dim3((unsigned)n), dim3(kNormThreads), 0, stream>>>(l, (uint32_t)at, slots, used, scale, max_norm, out);
         SR_HIP(hipGetLastError());
         out = nullptr;
     }
@@ -313,4 +423,19 @@ extern "C" int sr_grad_norm(const sr_tensor *host_tensors, int n_tensors, float 
 extern "C" int sr_clip_grad_norm(const sr_tensor *host_tensors, int n_tensors, float scale, float max_norm, float *norm,
                                  void *workspace, size_t workspace_bytes, void *stream) {
     return sr::norm_and_clip(host_tensors, n_tensors, scale, max_norm, true, norm, workspace, workspace_bytes, (hipStream_t)stream);
+}
+
+extern "C" int sr_plan_tensors(const sr_tensor *host_tensors, int n_tensors, void *table, size_t table_bytes, sr_tensor_plan *host_plan,
+                               void *stream) {
+    return sr::plan_tensors(host_tensors, n_tensors, table, table_bytes, host_plan, (hipStream_t)stream);
+}
+
+extern "C" int sr_planned_grad_norm(const sr_tensor_plan *host_plan, float scale, float *norm, void *workspace, size_t workspace_bytes,
+                                    void *stream) {
+    return sr::planned_norm_and_clip(host_plan, scale, 0.f, false, norm, workspace, workspace_bytes, (hipStream_t)stream);
+}
+
+extern "C" int sr_planned_clip_grad_norm(const sr_tensor_plan *host_plan, float scale, float max_norm, float *norm, void *workspace,
+                                         size_t workspace_bytes, void *stream) {
+    return sr::planned_norm_and_clip(host_plan, scale, max_norm, true, norm, workspace, workspace_bytes, (hipStream_t)stream);
 }

@@ -94,6 +94,12 @@ __device__ __forceinline__ float reduce_64(float x, F &&f) {
     return row_reduce(reduce_16(x, f), f);
 }
 
+// A uniform address by a scalar load: it does not queue behind vector loads and stores.  Nothing that the kernel itself writes.
+template <typename V> __device__ __forceinline__ V read_uniform(const V *p) {
+    typedef std::conditional_t<sizeof(V) == 8, uint64_t, uint32_t> bits;
+    return __builtin_bit_cast(V, *(const __attribute__((address_space(4))) bits *)p);
+}
+
 // Sum over the workgroup, in an order that depends on the thread number alone; valid in thread 0.  s: WAVES doubles of LDS,
 // free to be overwritten.
 template <int WAVES>

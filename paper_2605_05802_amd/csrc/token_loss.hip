@@ -127,11 +127,6 @@ constexpr int64_t kKeepBytes = 384 << 20;
 // s of a row that does not count
 constexpr float kNoRow = -1.f;
 
-// A uniform address by a scalar load: it does not queue behind vector loads and stores.  Nothing that the kernel itself writes.
-template <typename V> __device__ __forceinline__ V read_uniform(const V *p) {
-    typedef std::conditional_t<sizeof(V) == 8, uint64_t, uint32_t> bits;
-    return __builtin_bit_cast(V, *(const __attribute__((address_space(4))) bits *)p);
-}
 // An entry of seq_start as an end of a range of rows, whatever it holds
 __device__ __forceinline__ int row_bound(const RowArgs &a, int row) { return min(max(row, 0), a.n_rows); }
 // the sequence of a row, or -1: the last one that begins at or before it

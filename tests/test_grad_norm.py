@@ -214,3 +214,58 @@ def test_refusals():
         sr.tensor_list([torch.zeros(3)], [torch.zeros(4)])
     with pytest.raises(sr.SrError):
         sr.tensor_list([torch.zeros(3)], [])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("count", [1, 64, 511, 512, 513, 4096, 4097, 9000])
+def test_planned_lists_of_any_length(count):
+    """One table on the device: up to 512 tensors are copied to LDS, more are searched, 64 at a time.  Empty tensors, several
+    chunks in some of them and all three types among them."""
+    sizes = [(i * 7919) % 23 if i % 97 else 8192 * (i % 5) + i % 3 for i in range(count)]
+    sizes[0] = 40000
+    ts = tensors_of(sizes, [F32, BF16, F16], 11)
+    check(ts, 0.3 * norm_of(ts))
+    listed, (norm, ws) = sr.tensor_list(ts), work()
+    sr.sr_grad_norm(listed, norm, ws, scale=-0.5)
+    assert norm.item() == pytest.approx(0.5 * norm_of(ts), rel=4 * U)
+
+
+@pytest.mark.gpu
+def test_a_plan_writes_its_table_and_nothing_else():
+    ts = tensors_of([0, 5, 10000, 0, 7], [F32], 12)
+    rows = (sr.Tensor * 5)(*[sr.Tensor(t.data_ptr(), None, t.numel(), 0, 0) for t in ts])
+    table = torch.full((64 + 24 * 5 + 64,), 99, dtype=torch.uint8, device="cuda")
+    plan = sr.TensorPlan()
+    assert sr.lib().sr_plan_tensors(rows, 5, table.data_ptr(), 64 + 24 * 5, plan, None) == sr.SR_OK
+    assert bool((table[-64:] == 99).all()) and plan.n_tensors == 3 and plan.chunks == 4
+    assert sr.lib().sr_plan_tensors(rows, 0, table.data_ptr(), 64, plan, None) == sr.SR_OK
+    norm, ws = work()
+    assert sr.lib().sr_planned_clip_grad_norm(plan, 1.0, 1.0, norm.data_ptr(), ws.data_ptr(), ws.nbytes, None) == sr.SR_OK
+    torch.cuda.synchronize()
+    assert norm.item() == 0.0
+
+
+def test_refusals_of_plans():
+    L, fake = sr.lib(), ctypes.c_void_p(4096)                      # never dereferenced: validation fails first
+    one = (sr.Tensor * 1)(sr.Tensor(4096, None, 5, 0, 0))
+    plan = sr.TensorPlan()
+    make = lambda a=one, n=1, table=fake, size=88, to=plan: L.sr_plan_tensors(a, n, table, size, to, None)
+    for r in (make(a=None), make(n=-1), make(table=None), make(table=ctypes.c_void_p(4104)), make(size=87), make(to=None),
+              make(a=(sr.Tensor * 1)(sr.Tensor(None, None, 5, 0, 0))), make(a=(sr.Tensor * 1)(sr.Tensor(4096, 4096, 5, 1, 0)))):
+        assert r == sr.SR_E_ARG
+    many = (sr.Tensor * 256)(*[sr.Tensor(4096, None, 1 << 36, 1, 0)] * 256)
+    assert make(a=many, n=256, size=64 + 24 * 256) == sr.SR_E_LIMIT
+    good = dict(table=4096, chunks=3, keep=0, n_tensors=2, reserved=0)
+    clip = lambda scale=1.0, limit=1.0, norm=fake, ws=fake, size=sr.GRAD_NORM_WORKSPACE, **k: L.sr_planned_clip_grad_norm(
+        sr.TensorPlan(**{**good, **k}), scale, limit, norm, ws, size, None)
+    for r in (clip(scale=math.nan), clip(limit=-1.0), clip(norm=None), clip(ws=None), clip(size=100), clip(table=None),
+              clip(n_tensors=-1), clip(chunks=1), clip(chunks=1 << 31)):
+        assert r == sr.SR_E_ARG
+    assert L.sr_planned_clip_grad_norm(None, 1.0, 1.0, fake, fake, sr.GRAD_NORM_WORKSPACE, None) == sr.SR_E_ARG
+    assert L.sr_planned_grad_norm(None, 1.0, fake, fake, sr.GRAD_NORM_WORKSPACE, None) == sr.SR_E_ARG
+
+
+def test_host_tensors_are_refused():
+    for make in (lambda t: sr.TensorList([t]), lambda t: sr.tensor_list([t]), lambda t: sr.sr_grad_norm([], t, t)):
+        with pytest.raises(sr.SrError, match="device tensors expected"):
+            make(torch.zeros(1))

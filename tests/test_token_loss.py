@@ -631,3 +631,13 @@ def test_the_binding_refuses_wrong_tensors():
         with pytest.raises(sr.SrError) as e:
             sr.sr_policy_loss(**{**good, **bad}, stream=0)
         assert e.value.status == sr.SR_E_ARG
+
+
+def test_host_tensors_are_refused():
+    i32 = torch.int32
+    rows = dict(logits=torch.zeros(4, 10), targets=torch.zeros(4, dtype=i32), seq_start=torch.zeros(3, dtype=i32), stats=torch.zeros(4),
+                workspace=torch.zeros(sr.token_loss_workspace(4, 2), dtype=torch.uint8))
+    with pytest.raises(sr.SrError, match="device tensors expected"):
+        sr.sr_policy_loss(old_logprob=torch.zeros(4), advantages=torch.zeros(2), **rows)
+    with pytest.raises(sr.SrError, match="device tensors expected"):
+        sr.sr_preference_loss(**rows)
