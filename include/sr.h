@@ -338,7 +338,8 @@ typedef struct {
  * old_logprob, ref_logprob: device float [n_rows], as sr_score_chunk writes them; ref_logprob may be NULL if kl_coef == 0.
  * advantages: device float [n_seq].
  * SR_E_ARG: null pointers, a bad dtype, shape, stride or option, a workspace that is too small or not 16-byte aligned;
- * SR_E_LIMIT: more than 2^26 rows or 2^23 sequences.  n_rows may be 0.
+ * SR_E_LIMIT: more than 2^26 - 4 rows or 2^23 sequences, or more threads than a launch may have (2^32 - 1; a row of more than
+ * 8 KiB takes 256, and so does every 16 KiB of a preference loss's gradient).  n_rows may be 0.
  */
 typedef enum { SR_MEAN_TOKENS = 0, SR_MEAN_SEQUENCES = 1, SR_MEAN_SUMS = 2 } sr_reduce;
 typedef struct {

@@ -959,6 +959,7 @@ int launch_resident(const RowArgs &a, const PolicyArgs &p, int waves, int vecs, 
 
 int policy_loss(const sr_token_rows *x, const PolicyArgs &p, void *workspace, hipStream_t stream) {
     const RowPlan plan = plan_policy_rows(x->n_rows, x->vocab, x->dtype == SR_F32 ? 4 : 2);
+    if (!launches_fit(plan, x->n_rows, x->grad != nullptr)) return SR_E_LIMIT;
     const RowArgs a = row_args(x, plan, workspace);
     const bool small = a.n_rows <= kMostSmallRows && a.n_seq <= kMostInline && !(a.grad && plan.resident);
     if (a.n_rows > 0)
@@ -991,6 +992,7 @@ int policy_loss(const sr_token_rows *x, const PolicyArgs &p, void *workspace, hi
 
 int preference_loss(const sr_token_rows *x, const PairArgs &p, void *workspace, hipStream_t stream) {
     const RowPlan plan = plan_streamed_rows(x->n_rows, x->vocab, x->dtype == SR_F32 ? 4 : 2);
+    if (!launches_fit(plan, x->n_rows, x->grad != nullptr)) return SR_E_LIMIT;
     const RowArgs a = row_args(x, plan, workspace);
     return with_type(x->dtype, [&](auto *t) -> int {
         typedef std::remove_pointer_t<decltype(t)> T;

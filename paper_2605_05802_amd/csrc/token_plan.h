@@ -1,5 +1,7 @@
 // Which kernels the losses over token rows run on, in plain C++ so that the rules can be evaluated without a GPU.
 #pragma once
+#include <cstdint>
+
 #include "plan.h"
 
 namespace sr {
@@ -52,6 +54,14 @@ inline RowPlan plan_policy_rows(int n_rows, int vocab, int elem_bytes) {
     RowPlan p{waves, each > 0 ? each : 1};
     split_row(ceil_div(vocab, per_vec), per_vec, 1, &p.parts, &p.elems);
     return p;
+}
+
+// A launch has at most 2^32 - 1 threads
+inline bool launches_fit(const RowPlan &p, int n_rows, bool grad) {
+    auto threads = [](int64_t units, int waves) { return waves == 1 ? (units + 3) / 4 * 256 : units * 64 * waves; };
+    if (p.resident && grad) return p.waves == 16 || threads(n_rows, p.waves) <= UINT32_MAX;
+    return threads((int64_t)n_rows * p.parts, p.waves) <= UINT32_MAX &&
+           (!grad || threads((int64_t)n_rows * p.grad_parts, p.grad_waves) <= UINT32_MAX);
 }
 
 }  // namespace sr

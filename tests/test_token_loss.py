@@ -641,3 +641,14 @@ def test_host_tensors_are_refused():
         sr.sr_policy_loss(old_logprob=torch.zeros(4), advantages=torch.zeros(2), **rows)
     with pytest.raises(sr.SrError, match="device tensors expected"):
         sr.sr_preference_loss(**rows)
+
+
+def test_more_threads_than_a_launch_has():
+    L, fake = sr.lib(), ctypes.c_void_p(4096)
+    opt = sr.PolicyOptions(0.2, 0.2, 0.0, 0)
+    for n_rows, vocab in (((1 << 26) - 3, 4), (1 << 24, 5000), (1 << 26, 3000)):
+        rows = ctypes.byref(_rows(n_rows=n_rows, vocab=vocab, ld_logits=vocab, ld_grad=vocab, grad=4096))
+        assert L.sr_policy_loss(rows, fake, None, fake, ctypes.byref(opt), fake, fake, 1 << 40, None) == sr.SR_E_LIMIT
+        assert L.sr_preference_loss(rows, fake, 0.1, 0.0, None, fake, fake, 1 << 40, None) == sr.SR_E_LIMIT
+    rows = ctypes.byref(_rows(n_rows=1 << 23, vocab=50000, ld_logits=50000, ld_grad=50000, grad=4096))
+    assert L.sr_preference_loss(rows, fake, 0.1, 0.0, None, fake, fake, 1 << 40, None) == sr.SR_E_LIMIT
