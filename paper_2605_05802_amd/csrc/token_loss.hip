@@ -10,7 +10,8 @@
 //   policy_sum_kernel    the rows' terms of the loss added up
 // Everything else goes through the logits twice:
 //   row_stats_kernel     (m, s) of a row, or of a part of one
-//   policy_small_kernel, or row_info_*, policy_rows_kernel and policy_sum_kernel    the slopes of the rows and the loss
+//   policy_grad_kernel   few rows: the gradient and the loss; without a gradient policy_small_kernel
+//   row_info_*, policy_rows_kernel and policy_sum_kernel    the slopes of the rows and the loss
 //   pair_kernel          log ratios of a pair's sequences, the margin, the slopes of the pair's rows
 //   logit_grad_kernel    the gradient, from the row, (m, s) and the slope; in passing the pairs added up (pair_sum_kernel without one)
 //
@@ -35,6 +36,8 @@ constexpr int kMostSummedRows = 16384, kShares = 256;      // rows whose terms o
 constexpr int kMostInline = 1024;      // sequences of a small call
 constexpr int kMostTableRows = 4096;   // its rows
 constexpr int kMostSmallRows = 2048;   // rows whose slopes and terms one workgroup computes
+constexpr int kMostAtOnce = 1024;      // workgroups of policy_grad_kernel, all of which run at once (2048 rows of 100000 fp32 in parts of 16 KB: 423 us, with a
+                                       // kernel in between 395)
 constexpr int kParts = 8192;           // parts of rows that the workspace holds
 
 // exp(x) for x <= 0 by the exponential instruction; results below 2^-126 are 0.
@@ -51,11 +54,6 @@ __device__ __forceinline__ float exp_neg_of_16(float x, int i) { return __builti
 struct RowSum {
     float m, s;
 };
-__device__ __forceinline__ void merge(RowSum &a, float m2, float s2) {
-    const float mn = fmaxf(a.m, m2);
-    a.s = fmaf(a.s, expf(a.m - mn), s2 * expf(m2 - mn));
-    a.m = mn;
-}
 __device__ __forceinline__ RowSum one_element(float x) {
     const float m = fmaxf(x, -FLT_MAX);
     return RowSum{m, exp_neg(x - m)};
@@ -212,9 +210,19 @@ __global__ __launch_bounds__(row_block(WAVES)) void row_stats_kernel(RowArgs a) 
 // (m, s) of a row from its parts, in their order
 __device__ __forceinline__ RowSum whole_row(const RowArgs &a, int row) {
     const float2 *p = a.part + (size_t)row * a.splits;
-    RowSum r = {p[0].x, p[0].y};
-    if (r.s == kNoRow) return r;
-    for (int k = 1; k < a.splits; ++k) merge(r, p[k].x, p[k].y);
+    if (a.splits == 1 || p[0].y == kNoRow) return RowSum{p[0].x, p[0].y};
+    RowSum r = {p[0].x, 0.f};
+    for (int k = 1; k < a.splits; ++k) r.m = fmaxf(r.m, p[k].x);
+    for (int k = 0; k < a.splits; ++k) r.s = fmaf(p[k].y, expf(p[k].x - r.m), r.s);
+    return r;
+}
+// ... a uniform row's, from at most 64 parts that lie in the lanes, the last one in all lanes behind them
+__device__ __forceinline__ RowSum whole_row_of_wave(float2 part, int splits) {
+    auto lane = [](float x, int k) __attribute__((always_inline)) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), k)); };
+    if (splits == 1 || lane(part.y, 0) == kNoRow) return RowSum{lane(part.x, 0), lane(part.y, 0)};
+    RowSum r = {reduce_64(part.x, [](float x, float y) { return fmaxf(x, y); }), 0.f};
+    const float e = expf(part.x - r.m);
+    for (int k = 0; k < splits; ++k) r.s = fmaf(lane(part.y, k), lane(e, k), r.s);
     return r;
 }
 
@@ -232,6 +240,28 @@ __device__ __forceinline__ raw16 gradient(raw16 raw, int hot, float m, float fac
         for (int i = 0; i < N; ++i)
             if (hot == i) v[i] += slope;
     return Elem<T>::narrow(v);
+}
+
+// The whole vectors of a part, every LANES-th from e on for this thread
+constexpr int kGradDepth = 4;
+template <typename T, int LANES>
+__device__ __forceinline__ void write_gradient(const T *x, T *g, int e, int full, int target, float m, float factor, float slope) {
+    constexpr int N = Elem<T>::kPerVec;
+    raw16 raw[kGradDepth];
+    for (; e + (kGradDepth - 1) * LANES * N < full; e += kGradDepth * LANES * N) {
+#pragma unroll
+        for (int j = 0; j < kGradDepth; ++j) raw[j] = load_vec_once(x + e + j * LANES * N);
+#pragma unroll
+        for (int j = 0; j < kGradDepth; ++j)
+            store_vec_once(g + e + j * LANES * N, gradient<T>(raw[j], target - e - j * LANES * N, m, factor, slope));
+    }
+    for (; e < full; e += LANES * N) store_vec_once(g + e, gradient<T>(load_vec_once(x + e), target - e, m, factor, slope));
+}
+// ... and element `rest` behind them, if there is one
+template <typename T, int LANES>
+__device__ __forceinline__ void write_zeros(T *g, int e, int full, int rest, int to) {
+    for (; e < full; e += LANES * Elem<T>::kPerVec) store_vec_once(g + e, raw16(0));
+    if (rest < to) g[rest] = (T)0.f;
 }
 
 // The preference loss
@@ -262,7 +292,7 @@ __device__ __forceinline__ void sum_pairs(const RowArgs &a, const PairArgs &p, d
 // WAVES wavefronts per (row, part).  In place: a thread reads what it then writes.  p.stats: the first workgroup adds the pairs up.
 template <typename T, int WAVES>
 __global__ __launch_bounds__(row_block(WAVES)) void logit_grad_kernel(RowArgs a, PairArgs p) {
-    constexpr int N = Elem<T>::kPerVec, LANES = 64 * WAVES, DEPTH = 4;
+    constexpr int N = Elem<T>::kPerVec, LANES = 64 * WAVES;
     __shared__ double s[row_block(WAVES) / 64];
     if (p.stats && blockIdx.x == 0) sum_pairs<row_block(WAVES)>(a, p, s);
     const int unit = WAVES == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
@@ -273,27 +303,14 @@ __global__ __launch_bounds__(row_block(WAVES)) void logit_grad_kernel(RowArgs a,
     T *g = (T *)a.grad + row * a.ld_grad;
     const int from = part * a.grad_elems, to = min(from + a.grad_elems, a.vocab), full = from + (to - from) / N * N;
     const float2 whole = a.whole[row];
-    if (whole.y == kNoRow) {
-        for (int e = from + t * N; e < full; e += LANES * N) store_vec_once(g + e, raw16(0));
-        if (full + t < to) g[full + t] = (T)0.f;
-        return;
-    }
+    if (whole.y == kNoRow) return write_zeros<T, LANES>(g, from + t * N, full, full + t, to);
     const float m = whole.x, slope = a.slope[row], factor = -slope / whole.y;
     const int target = a.targets[row];
     if (full + t < to) {
         const float v = factor * exp_neg((float)x[full + t] - m);
         g[full + t] = (T)(target == full + t ? v + slope : v);
     }
-    raw16 raw[DEPTH];
-    int e = from + t * N;
-    for (; e + (DEPTH - 1) * LANES * N < full; e += DEPTH * LANES * N) {
-#pragma unroll
-        for (int j = 0; j < DEPTH; ++j) raw[j] = load_vec_once(x + e + j * LANES * N);
-#pragma unroll
-        for (int j = 0; j < DEPTH; ++j)
-            store_vec_once(g + e + j * LANES * N, gradient<T>(raw[j], target - e - j * LANES * N, m, factor, slope));
-    }
-    for (; e < full; e += LANES * N) store_vec_once(g + e, gradient<T>(load_vec_once(x + e), target - e, m, factor, slope));
+    write_gradient<T, LANES>(x, g, from + t * N, full, target, m, factor, slope);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -513,8 +530,8 @@ struct PolicySums {
         kl += (double)t.w * (double)t.y;
         out += (double)t.w * (double)t.z;
     }
-    // over the workgroup, valid in thread 0; s: 3 * kSumThreads / 64 doubles of LDS
-    __device__ __forceinline__ void gather(double *s) {
+    // over a wavefront, into its places in s, 3 * kSumThreads / 64 doubles of LDS
+    __device__ __forceinline__ void fold(double *s, int wave) {
         constexpr int WAVES = kSumThreads / 64;
 #pragma unroll
         for (int off = 32; off >= 1; off >>= 1) {
@@ -523,11 +540,15 @@ struct PolicySums {
             out += __shfl_xor(out, off, 64);
         }
         if ((threadIdx.x & 63) == 0) {
-            double *mine = s + threadIdx.x / 64;
+            double *mine = s + wave;
             mine[0] = surrogate;
             mine[WAVES] = kl;
             mine[2 * WAVES] = out;
         }
+    }
+    // over the wavefronts, valid in thread 0
+    __device__ __forceinline__ void unfold(const double *s) {
+        constexpr int WAVES = kSumThreads / 64;
         __syncthreads();
         if (threadIdx.x >= 64) return;
         const int k = threadIdx.x & (WAVES - 1);             // the first 16 lanes have all they need
@@ -541,8 +562,15 @@ struct PolicySums {
             out += __shfl_xor(out, off, 64);
         }
     }
+    __device__ __forceinline__ void gather(double *s) {
+        fold(s, threadIdx.x / 64);
+        unfold(s);
+    }
     __device__ __forceinline__ void finish(const PolicyArgs &p, double *s) {
         gather(s);
+        write(p);
+    }
+    __device__ __forceinline__ void write(const PolicyArgs &p) const {
         if (threadIdx.x != 0) return;
         p.stats[0] = (float)((p.kl_coef != 0.f ? (double)p.kl_coef * kl : 0.0) - surrogate);
         p.stats[1] = (float)surrogate;
@@ -559,13 +587,18 @@ struct RowInput {
 __device__ __forceinline__ RowInput row_input(const RowArgs &a, const PolicyArgs &p, int row) {
     return RowInput{whole_row(a, row), a.chosen[row], p.old_logprob[row], p.ref_logprob ? p.ref_logprob[row] : 0.f};
 }
+// Its terms of the loss and its log-probability; returns the slope
+__device__ __forceinline__ float row_outcome(const RowArgs &a, const PolicyArgs &p, float2 info, const RowInput &in, float4 *term, float *logprob) {
+    *logprob = 0.f;
+    *term = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (info.x == 0.f) return 0.f;
+    *logprob = (in.chosen - in.r.m) - logf(in.r.s);
+    return policy_row(p, info, *logprob, in.old_logprob, in.ref_logprob, term) * a.grad_scale;
+}
 __device__ __forceinline__ float4 finish_row(const RowArgs &a, const PolicyArgs &p, int row, float2 info, const RowInput &in) {
-    float logprob = 0.f, slope = 0.f;
-    float4 term = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (info.x != 0.f) {
-        logprob = (in.chosen - in.r.m) - logf(in.r.s);
-        slope = policy_row(p, info, logprob, in.old_logprob, in.ref_logprob, &term) * a.grad_scale;
-    }
+    float logprob;
+    float4 term;
+    const float slope = row_outcome(a, p, info, in, &term, &logprob);
     if (a.token_logprob) a.token_logprob[row] = logprob;
     a.slope[row] = slope;
     a.whole[row] = make_float2(in.r.m, in.r.s);
@@ -598,7 +631,7 @@ __global__ __launch_bounds__(kSumThreads) void policy_shares_kernel(PolicyArgs p
     sums.finish(p, s);
 }
 
-// The kernels between row_stats_kernel and logit_grad_kernel, and policy_sum_kernel, by one workgroup: few rows
+// row_info_*, policy_rows_kernel and policy_sum_kernel by one workgroup: few rows, no gradient
 __global__ __launch_bounds__(kSumThreads) void policy_small_kernel(RowArgs a, PolicyArgs p) {
     __shared__ double s[3 * kSumThreads / 64];
     __shared__ SeqTable table;
@@ -616,6 +649,71 @@ __global__ __launch_bounds__(kSumThreads) void policy_small_kernel(RowArgs a, Po
         if (row < a.n_rows) sums.add(finish_row(a, p, row, table.info(a, p, row), in[k]));
     }
     sums.finish(p, s);
+}
+
+// The gradient of few rows straight from their parts' (m, s): every workgroup works out its row's weight and slope while its first EARLY
+// vectors a thread are on their way, and one workgroup more, the first, the loss.  Kernels for 128 rows of 152064 fp32: 16 + 24 us, with a
+// kernel in between 16 + 6 + 22; 16 rows of 50021 f16 11 us instead of 14 a call.  Four vectors on their way: 2 us more, eight: 1.
+template <typename T, int WAVES>
+__global__ __launch_bounds__(row_block(WAVES)) void policy_grad_kernel(RowArgs a, PolicyArgs p) {
+    constexpr int THREADS = row_block(WAVES), N = Elem<T>::kPerVec, LANES = 64 * WAVES, EARLY = 12;
+    __shared__ SeqTable table;
+    const SeqTable::Ahead ahead = SeqTable::ahead(a);
+    if (blockIdx.x == 0) {
+        // as kSumThreads threads would add them up
+        __shared__ double s[3 * kSumThreads / 64];
+        table.template fill<THREADS>(a, ahead);
+        PolicySums sums;
+#pragma unroll 1
+        for (int k = 0; k < kSumThreads; k += THREADS) {
+            sums = PolicySums();
+            for (int row = threadIdx.x + k; row < a.n_rows; row += kSumThreads) {
+                float logprob;
+                float4 term;
+                row_outcome(a, p, table.info(a, p, row), row_input(a, p, row), &term, &logprob);
+                sums.add(term);
+                if (a.token_logprob) a.token_logprob[row] = logprob;
+            }
+            sums.fold(s, (threadIdx.x + k) / 64);
+        }
+        sums.unfold(s);
+        sums.write(p);
+        return;
+    }
+    const int unit = WAVES == 1 ? __builtin_amdgcn_readfirstlane((blockIdx.x - 1) * 4 + (threadIdx.x >> 6)) : blockIdx.x - 1;
+    const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const bool mine = unit < a.n_rows * a.grad_splits;       // false for a wavefront beside others that has nothing left
+    const int row = mine ? unit / a.grad_splits : 0, part = mine ? unit - row * a.grad_splits : 0;
+    const T *x = (const T *)a.logits + row * a.ld_logits;
+    T *g = (T *)a.grad + row * a.ld_grad;
+    const int from = part * a.grad_elems, to = min(from + a.grad_elems, a.vocab), full = from + (to - from) / N * N;
+    const float2 parts = a.part[(size_t)row * a.splits + min((int)threadIdx.x & 63, a.splits - 1)];
+    RowInput in = {{}, read_uniform(a.chosen + row), read_uniform(p.old_logprob + row), p.ref_logprob ? read_uniform(p.ref_logprob + row) : 0.f};
+    const int target = read_uniform(a.targets + row);
+    int e = from + t * N;
+    raw16 raw[EARLY];
+#pragma unroll
+    for (int j = 0; j < EARLY; ++j)
+        if (mine && from + j * LANES * N < full) raw[j] = load_vec_once(x + min(e + j * LANES * N, full - N));    // whole wavefronts
+    table.template fill<THREADS>(a, ahead);
+    if (!mine) return;
+    asm volatile("" : "+v"(e));                              // not a path of its own for every number of vectors
+    const float2 info = table.info_of_wave(a, p, row);
+    in.r = whole_row_of_wave(parts, a.splits);
+    if (info.x == 0.f || in.r.s == kNoRow) return write_zeros<T, LANES>(g, e, full, full + t, to);
+    float logprob;
+    float4 term;
+    const float slope = row_outcome(a, p, info, in, &term, &logprob), m = in.r.m, factor = -slope / in.r.s;
+    if (full + t < to) {
+        const float v = factor * exp_neg((float)x[full + t] - m);
+        g[full + t] = (T)(target == full + t ? v + slope : v);
+    }
+#pragma unroll
+    for (int j = 0; j < EARLY; ++j) {
+        if (e + j * LANES * N < full) store_vec_once(g + e + j * LANES * N, gradient<T>(raw[j], target - e - j * LANES * N, m, factor, slope));
+        __builtin_amdgcn_sched_barrier(0);                   // one vector's widened values at a time
+    }
+    write_gradient<T, LANES>(x, g, e + EARLY * LANES * N, full, target, m, factor, slope);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -914,6 +1012,15 @@ int launch_logit_grad(const RowArgs &a, const PairArgs &p, int waves, hipStream_
     return SR_OK;
 }
 
+template <typename T>
+int launch_policy_grad(const RowArgs &a, const PolicyArgs &p, int waves, hipStream_t stream) {
+    const int units = a.n_rows * a.grad_splits;
+    if (waves == 1) policy_grad_kernel<T, 1><<<dim3(ceil_div(units, 4) + 1), dim3(row_block(1)), 0, stream>>>(a, p);
+    else policy_grad_kernel<T, 4><<<dim3(units + 1), dim3(row_block(4)), 0, stream>>>(a, p);
+    SR_HIP(hipGetLastError());
+    return SR_OK;
+}
+
 int launch_row_info(const RowArgs &a, const PolicyArgs &p, hipStream_t stream) {
     if (a.n_seq <= kMostInline && a.n_rows <= kMostTableRows) {
         row_info_small_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(a, p);
@@ -967,6 +1074,7 @@ int policy_loss(const sr_token_rows *x, const PolicyArgs &p, void *workspace, hi
             typedef std::remove_pointer_t<decltype(t)> T;
             if (a.grad && plan.resident) return launch_resident<T>(a, p, plan.waves, plan.resident, stream);
             SR_TRY(launch_row_stats<T>(a, plan.waves, stream));
+            if (small && a.grad && a.n_rows * a.grad_splits <= kMostAtOnce) return launch_policy_grad<T>(a, p, plan.grad_waves, stream);
             if (small) {
                 policy_small_kernel<<<dim3(1), dim3(kSumThreads), 0, stream>>>(a, p);
                 SR_HIP(hipGetLastError());

@@ -24,8 +24,8 @@ inline void split_row(int vecs, int per_vec, int parts, int *n, int *elems) {
     *elems = each * per_vec;
 }
 
-// Rows that are read twice.  Few rows: parts for about 1024 workgroups (128 rows of 152064 fp32 in 8 parts 15 + 22 us for maximum and
-// gradient; in 16, 32 and 64 the kernel between them, which merges the parts, takes 1, 4 and 9 us longer).  Many: 8192 parts even out the end
+// Rows that are read twice.  Few rows: parts for about 1024 workgroups (128 rows of 152064 fp32 in 8 parts 16 + 24 us for maximum and
+// gradient, in 16 parts 16 + 27; where a kernel between them merges the parts, 16, 32 and 64 of them take it 1, 4 and 9 us longer).  Many: 8192 parts even out the end
 // (2400 rows of 152064 bf16 in 3 parts each 129 us, in one 136; 1701 rows of 50021 in 4, 30 us, 34).
 inline RowPlan plan_streamed_rows(int n_rows, int vocab, int elem_bytes) {
     const int per_vec = 16 / elem_bytes, vecs = ceil_div(vocab, per_vec);
@@ -43,13 +43,13 @@ inline RowPlan plan_streamed_rows(int n_rows, int vocab, int elem_bytes) {
 }
 
 // Rows of the policy loss: held in registers between maximum and gradient where they fit.  Rows of sixteen wavefronts are one to a
-// compute unit: below 112 of them too few compute units work (64 rows of 152064 bf16: 28 us, streamed 21; 128: 28 and 28; 192: 30 and 39),
-// and a few more than 256 wait for a second round (300 rows of 152064 bf16: 57 us, streamed 52; of 50000: 30 and 24; 384: 58 and 63;
-// of 64000 fp32, which take longer in either way, 42 and 47).
+// compute unit: with few of them too few compute units work (rows of 152064 bf16: 64 take 27 us, streamed 18; 128, 28 and 24; 160, 28 and 29;
+// 192, 31 and 35; of 75000 fp32: 112 take 23 and 21; 128, 24 and 25; 192, 29 and 34), and a few more than 256 wait for a second round
+// (152064 bf16: 288 rows take 58 us, streamed 46; 352, 59 and 54; 448, 60 and 66; 75000 fp32: 51 and 46, 57 and 56, 61 and 71).
 inline RowPlan plan_policy_rows(int n_rows, int vocab, int elem_bytes) {
     const int per_vec = 16 / elem_bytes, vecs = vocab / per_vec;
     const int waves = vecs <= 64 * kMostOneWave ? 1 : vecs <= 256 * kMostResident ? 4 : 16, each = ceil_div(vecs, 64 * waves);
-    const bool uneven = n_rows < 112 || (elem_bytes == 2 && n_rows > 256 && n_rows <= 320);
+    const bool uneven = n_rows < (elem_bytes == 2 ? 160 : 128) || (n_rows > 256 && n_rows <= 352);
     if (each > kMostResident || (waves == 16 && uneven)) return plan_streamed_rows(n_rows, vocab, elem_bytes);
     RowPlan p{waves, each > 0 ? each : 1};
     split_row(ceil_div(vocab, per_vec), per_vec, 1, &p.parts, &p.elems);

@@ -652,3 +652,21 @@ def test_more_threads_than_a_launch_has():
         assert L.sr_preference_loss(rows, fake, 0.1, 0.0, None, fake, fake, 1 << 40, None) == sr.SR_E_LIMIT
     rows = ctypes.byref(_rows(n_rows=1 << 23, vocab=50000, ld_logits=50000, ld_grad=50000, grad=4096))
     assert L.sr_preference_loss(rows, fake, 0.1, 0.0, None, fake, fake, 1 << 40, None) == sr.SR_E_LIMIT
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n_seq,vocab,pad,shift", [
+    (7, 3, 45056, 0, 0),        # parts of one wavefront, bf16
+    (50, 60, 22528, 0, 0),      # ... fp32; more sequences than rows
+    (120, 1024, 43001, 7, 1), (121, 1025, 43001, 0, 0), (159, 9, 60000, 0, 3), (160, 9, 41000, 0, 0), (127, 5, 21003, 1, 2),
+    (257, 300, 41001, 0, 1), (352, 8, 41000, 8, 0), (353, 8, 41000, 0, 0), (2, 2, 400001, 0, 5), (1023, 40, 164001, 0, 0), (1024, 40, 164001, 0, 0)])
+def test_few_rows_in_parts(dtype, rows, n_seq, vocab, pad, shift):
+    x = make(rows, n_seq, vocab, dtype, rows + vocab, pad=pad, shift=shift, masked=0.25 if rows > 7 else 0.0, lead=min(rows // 9, 5), tail=min(rows // 7, 3))
+    scale = 4096.0 if dtype == torch.float16 else 1.0
+    for reduce in ("tokens", "sequences", "sums") if rows < 200 else ("sequences",):
+        stats, lp, g = check_policy(x, reduce, 0.04, scale=scale)
+    s1, l1, none = run_policy(x, reduce, 0.04, grad=False, scale=scale)
+    assert torch.equal(s1, stats) and torch.equal(l1, lp)
+    s2, l2, g2 = run_policy(x, reduce, 0.04, in_place=True, scale=scale)
+    assert torch.equal(s2, stats) and torch.equal(l2, lp) and torch.equal(g2, g)
