@@ -154,6 +154,25 @@ __device__ __forceinline__ bool row_counts(const RowArgs &a, int row) {
 // The threads and wavefronts of a workgroup for rows of WAVES wavefronts: four rows of one each
 constexpr int row_block(int waves) { return waves == 1 ? 256 : 64 * waves; }
 
+// 1 for a row of 16-bit elements that begins inside a word: its vectors begin behind its first element, at a word
+template <typename T> __device__ __forceinline__ int inside_word(const T *x) { return sizeof(T) == 2 ? (int)((uintptr_t)x >> 1 & 1) : 0; }
+// A part of a row x: whole vectors in [from, full), then single elements to `to`; in front of the first part's one more if the row
+// begins inside a word (1701 rows of 50021 bf16 in pairs, a third masked: 77 us, 84 with half of the rows' vectors cutting words).
+template <typename T>
+struct Part {
+    static constexpr int N = Elem<T>::kPerVec;
+    int begin, from, full, to;
+    __device__ __forceinline__ Part(const T *x, int part, int elems, int vocab) {
+        const int first = part * elems, odd = inside_word(x);
+        from = first + odd;
+        to = min(from + elems, vocab);
+        full = from + (to - from) / N * N;
+        begin = part ? from : 0;
+    }
+    // lane t's single element, if that is in front of `to`: those behind the vectors, and one lane more for the first
+    __device__ __forceinline__ int single(int t) const { return t == N && begin != from ? begin : full + t; }
+};
+
 // The whole vectors of [from, full) of a row, every LANES-th for this thread, four in flight.  ONCE: with the non-temporal hint.
 template <typename T, int LANES, bool ONCE>
 __device__ __forceinline__ void add_part(RowSum &r, const T *x, int e, int full) {
@@ -189,14 +208,14 @@ __global__ __launch_bounds__(row_block(WAVES)) void row_stats_kernel(RowArgs a) 
         return;
     }
     const T *x = (const T *)a.logits + row * a.ld_logits;
-    const int from = part * a.split_elems, to = min(from + a.split_elems, a.vocab), full = from + (to - from) / N * N;
-    const int target = read_uniform(a.targets + row);
+    const Part<T> q(x, part, a.split_elems, a.vocab);
+    const int target = read_uniform(a.targets + row), single = q.single(t);
     RowSum r = {-FLT_MAX, 0.f};
-    if (full + t < to) r = one_element((float)x[full + t]);
-    if (unit < a.once_units) add_part<T, LANES, true>(r, x, from + t * N, full);
-    else add_part<T, LANES, false>(r, x, from + t * N, full);
+    if (single < q.to) r = one_element((float)x[single]);
+    if (unit < a.once_units) add_part<T, LANES, true>(r, x, q.from + t * N, q.full);
+    else add_part<T, LANES, false>(r, x, q.from + t * N, q.full);
     // The token's logit for the kernel behind this one: there it would be a cache line and an address translation per row, cold
-    const bool holds = target >= from && target < to, none = part == 0 && (target < 0 || target >= a.vocab);
+    const bool holds = target >= q.begin && target < q.to, none = part == 0 && (target < 0 || target >= a.vocab);
     float chosen = NAN;
     if (holds) chosen = (float)x[target];
     r = merge_lanes<64>(r);
@@ -257,11 +276,19 @@ __device__ __forceinline__ void write_gradient(const T *x, T *g, int e, int full
     }
     for (; e < full; e += LANES * N) store_vec_once(g + e, gradient<T>(load_vec_once(x + e), target - e, m, factor, slope));
 }
-// ... and element `rest` behind them, if there is one
+// ... and its single elements
 template <typename T, int LANES>
-__device__ __forceinline__ void write_zeros(T *g, int e, int full, int rest, int to) {
-    for (; e < full; e += LANES * Elem<T>::kPerVec) store_vec_once(g + e, raw16(0));
-    if (rest < to) g[rest] = (T)0.f;
+__device__ __forceinline__ void write_zeros(T *g, const Part<T> &q, int t) {
+    for (int e = q.from + t * Elem<T>::kPerVec; e < q.full; e += LANES * Elem<T>::kPerVec) store_vec_once(g + e, raw16(0));
+    const int single = q.single(t);
+    if (single < q.to) g[single] = (T)0.f;
+}
+template <typename T>
+__device__ __forceinline__ void write_single(const T *x, T *g, const Part<T> &q, int t, int target, float m, float factor, float slope) {
+    const int single = q.single(t);
+    if (single >= q.to) return;
+    const float v = factor * exp_neg((float)x[single] - m);
+    g[single] = (T)(target == single ? v + slope : v);
 }
 
 // The preference loss
@@ -301,16 +328,13 @@ __global__ __launch_bounds__(row_block(WAVES)) void logit_grad_kernel(RowArgs a,
     const int row = unit / a.grad_splits, part = unit - row * a.grad_splits;
     const T *x = (const T *)a.logits + row * a.ld_logits;
     T *g = (T *)a.grad + row * a.ld_grad;
-    const int from = part * a.grad_elems, to = min(from + a.grad_elems, a.vocab), full = from + (to - from) / N * N;
+    const Part<T> q(x, part, a.grad_elems, a.vocab);
     const float2 whole = a.whole[row];
-    if (whole.y == kNoRow) return write_zeros<T, LANES>(g, from + t * N, full, full + t, to);
+    if (whole.y == kNoRow) return write_zeros<T, LANES>(g, q, t);
     const float m = whole.x, slope = a.slope[row], factor = -slope / whole.y;
     const int target = a.targets[row];
-    if (full + t < to) {
-        const float v = factor * exp_neg((float)x[full + t] - m);
-        g[full + t] = (T)(target == full + t ? v + slope : v);
-    }
-    write_gradient<T, LANES>(x, g, from + t * N, full, target, m, factor, slope);
+    write_single<T>(x, g, q, t, target, m, factor, slope);
+    write_gradient<T, LANES>(x, g, q.from + t * N, q.full, target, m, factor, slope);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -686,34 +710,31 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_grad_kernel(RowArgs a
     const int row = mine ? unit / a.grad_splits : 0, part = mine ? unit - row * a.grad_splits : 0;
     const T *x = (const T *)a.logits + row * a.ld_logits;
     T *g = (T *)a.grad + row * a.ld_grad;
-    const int from = part * a.grad_elems, to = min(from + a.grad_elems, a.vocab), full = from + (to - from) / N * N;
+    const Part<T> q(x, part, a.grad_elems, a.vocab);
     const float2 parts = a.part[(size_t)row * a.splits + min((int)threadIdx.x & 63, a.splits - 1)];
     RowInput in = {{}, read_uniform(a.chosen + row), read_uniform(p.old_logprob + row), p.ref_logprob ? read_uniform(p.ref_logprob + row) : 0.f};
     const int target = read_uniform(a.targets + row);
-    int e = from + t * N;
+    int e = q.from + t * N;
     raw16 raw[EARLY];
 #pragma unroll
     for (int j = 0; j < EARLY; ++j)
-        if (mine && from + j * LANES * N < full) raw[j] = load_vec_once(x + min(e + j * LANES * N, full - N));    // whole wavefronts
+        if (mine && q.from + j * LANES * N < q.full) raw[j] = load_vec_once(x + min(e + j * LANES * N, q.full - N));    // whole wavefronts
     table.template fill<THREADS>(a, ahead);
     if (!mine) return;
     asm volatile("" : "+v"(e));                              // not a path of its own for every number of vectors
     const float2 info = table.info_of_wave(a, p, row);
     in.r = whole_row_of_wave(parts, a.splits);
-    if (info.x == 0.f || in.r.s == kNoRow) return write_zeros<T, LANES>(g, e, full, full + t, to);
+    if (info.x == 0.f || in.r.s == kNoRow) return write_zeros<T, LANES>(g, q, t);
     float logprob;
     float4 term;
     const float slope = row_outcome(a, p, info, in, &term, &logprob), m = in.r.m, factor = -slope / in.r.s;
-    if (full + t < to) {
-        const float v = factor * exp_neg((float)x[full + t] - m);
-        g[full + t] = (T)(target == full + t ? v + slope : v);
-    }
+    write_single<T>(x, g, q, t, target, m, factor, slope);
 #pragma unroll
     for (int j = 0; j < EARLY; ++j) {
-        if (e + j * LANES * N < full) store_vec_once(g + e + j * LANES * N, gradient<T>(raw[j], target - e - j * LANES * N, m, factor, slope));
+        if (e + j * LANES * N < q.full) store_vec_once(g + e + j * LANES * N, gradient<T>(raw[j], target - e - j * LANES * N, m, factor, slope));
         __builtin_amdgcn_sched_barrier(0);                   // one vector's widened values at a time
     }
-    write_gradient<T, LANES>(x, g, e + EARLY * LANES * N, full, target, m, factor, slope);
+    write_gradient<T, LANES>(x, g, e + EARLY * LANES * N, q.full, target, m, factor, slope);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -730,25 +751,25 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
     __shared__ RowSum s_part[2][16];
     const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
     int row = WAVES == 1 ? __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)) : blockIdx.x;
-    const int full = a.vocab / N * N, tail = full + t;
     raw16 raw[NV];
     // Loaded unconditionally, from a place in the row, and looked at later: a load under a condition is waited for at its end, and
     // everything before it with it.
-    T last, chosen;                                          // lanes behind the last whole vector: an element of the rest; the token's
-    const int last_at = min(tail, a.vocab - 1);
+    T last, chosen;                                          // a lane's single element, if it has one; the token's
     auto token_at = [&](int target) __attribute__((always_inline)) { return min(max(target, 0), a.vocab - 1); };
+    auto part_of = [&](int row) __attribute__((always_inline)) { return Part<T>((const T *)a.logits + row * a.ld_logits, 0, a.vocab, a.vocab); };
     int at = t * N;                                          // the thread's element of the row's first LANES vectors
-    auto fetch = [&](int j, const T *x) __attribute__((always_inline)) {
+    auto fetch = [&](int j, const T *x, const Part<T> &q) __attribute__((always_inline)) {
         raw[j] = raw16(Elem<T>::kMinusInf);
-        if (j < SURE || at + j * LANES * N < full) raw[j] = load_vec_once(x + j * LANES * N + (unsigned)at);
+        if (j < SURE || at + j * LANES * N < q.full - q.from) raw[j] = load_vec_once(x + q.from + j * LANES * N + (unsigned)at);
     };
-    auto put = [&](int j, T *g, raw16 v) __attribute__((always_inline)) {
-        if (j < SURE || at + j * LANES * N < full) store_vec_once(g + j * LANES * N + (unsigned)at, v);
+    auto put = [&](int j, T *g, const Part<T> &q, raw16 v) __attribute__((always_inline)) {
+        if (j < SURE || at + j * LANES * N < q.full - q.from) store_vec_once(g + q.from + j * LANES * N + (unsigned)at, v);
     };
     auto zeros = [&](int row) __attribute__((always_inline)) {
         T *g = (T *)a.grad + row * a.ld_grad;
-        for (int j = 0; j < NV; ++j) put(j, g, raw16(0));
-        if (tail < a.vocab) g[tail] = (T)0.f;
+        const Part<T> q = part_of(row);
+        for (int j = 0; j < NV; ++j) put(j, g, q, raw16(0));
+        if (q.single(t) < a.vocab) g[q.single(t)] = (T)0.f;
         if (t == 0) {
             if (a.token_logprob) a.token_logprob[row] = 0.f;
             a.terms[row] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -785,10 +806,11 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
         if (info.x == 0.f) return zeros(row);
     }
     const T *x = (const T *)a.logits + row * a.ld_logits;
+    Part<T> q = part_of(row);
     if (mine) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) fetch(j, x);
-        last = x[last_at];
+        for (int j = 0; j < NV; ++j) fetch(j, x, q);
+        last = x[min(q.single(t), a.vocab - 1)];
     }
     RowScalars scalars;
     if (mine) {
@@ -802,7 +824,7 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
         info = table.info_of_wave(a, p, row);
     }
     RowSum r = {-FLT_MAX, 0.f};
-    if (tail < a.vocab) r = one_element((float)last);
+    if (q.single(t) < a.vocab) r = one_element((float)last);
     add_vectors<T, NV>(r, raw);
     if (LOOP) asm volatile("" ::"v"((float)chosen));         // waited for here, so that in the loop nothing but a row's own loads is
     for (int turn = 0;; turn ^= 1) {
@@ -825,36 +847,40 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
             if (a.token_logprob) a.token_logprob[row] = logprob;
             a.terms[row] = term;
         }
-        if (tail < a.vocab) {
+        const int single = q.single(t);
+        if (single < a.vocab) {
             const float v = factor * exp_neg((float)last - m);
-            g[tail] = (T)(target == tail ? v + slope : v);
+            g[single] = (T)(target == single ? v + slope : v);
         }
+        const int hot = target - q.from;
         if (next >= a.n_rows) {                              // the same for every wavefront of the row
 #pragma unroll
-            for (int j = 0; j < NV; ++j) put(j, g, gradient<T>(raw[j], target - at - j * LANES * N, m, factor, slope));
+            for (int j = 0; j < NV; ++j) put(j, g, q, gradient<T>(raw[j], hot - at - j * LANES * N, m, factor, slope));
             return;
         }
         // A group of vectors at a time: this row's gradient leaves, the next row's vectors are asked for, and those that were asked
         // for AHEAD vectors earlier are added up, so that neither the memory nor the arithmetic waits for the other.
         constexpr int AHEAD = NV / 2 / kGroup * kGroup;
         x = (const T *)a.logits + next * a.ld_logits;
-        last = x[last_at];
+        const Part<T> next_q = part_of(next);
+        last = x[min(next_q.single(t), a.vocab - 1)];
         chosen = x[token_at(next_scalars.target)];
         r = RowSum{-FLT_MAX, 0.f};
 #pragma unroll
         for (int k = 0; k < NV; k += kGroup) {
 #pragma unroll
             for (int j = k; j < k + kGroup; ++j) {
-                put(j, g, gradient<T>(raw[j], target - at - j * LANES * N, m, factor, slope));
-                fetch(j, x);
+                put(j, g, q, gradient<T>(raw[j], hot - at - j * LANES * N, m, factor, slope));
+                fetch(j, x, next_q);
                 __builtin_amdgcn_sched_barrier(0);           // one vector's widened values at a time
             }
-            if (k == AHEAD && tail < a.vocab) r = one_element((float)last);
+            if (k == AHEAD && next_q.single(t) < a.vocab) r = one_element((float)last);
             if (k >= AHEAD) add_vectors<T, kGroup>(r, raw + k - AHEAD);
             __builtin_amdgcn_sched_barrier(0);
         }
         add_vectors<T, AHEAD>(r, raw + NV - AHEAD);
         row = next;
+        q = next_q;
         info = next_info;
         scalars = next_scalars;
     }

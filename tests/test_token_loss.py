@@ -670,3 +670,28 @@ def test_few_rows_in_parts(dtype, rows, n_seq, vocab, pad, shift):
     assert torch.equal(s1, stats) and torch.equal(l1, lp)
     s2, l2, g2 = run_policy(x, reduce, 0.04, in_place=True, scale=scale)
     assert torch.equal(s2, stats) and torch.equal(l2, lp) and torch.equal(g2, g)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n_seq,vocab,pad,shift", [
+    (520, 30, 41001, 0, 1), (769, 7, 45056, 1, 0), (400, 3, 81921, 0, 0), (513, 600, 100000, 3, 1), (600, 40, 152064, 0, 1)])
+def test_workgroups_of_several_rows(dtype, rows, n_seq, vocab, pad, shift):
+    """Rows held in registers, two or more a workgroup, which begin at and inside words."""
+    x = make(rows, n_seq, vocab, dtype, rows, pad=pad, shift=shift, masked=0.3, lead=5, tail=7)
+    scale = 4096.0 if dtype == torch.float16 else 1.0
+    stats, lp, g = check_policy(x, "sequences", 0.04, scale=scale)
+    s2, l2, g2 = run_policy(x, "sequences", 0.04, in_place=True, scale=scale)
+    assert torch.equal(s2, stats) and torch.equal(l2, lp) and torch.equal(g2, g)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows", [3, 70, 1030])
+@pytest.mark.parametrize("vocab", [1, 2, 8, 9, 15, 16, 17, 512, 4096, 4097, 16384])
+def test_rows_that_begin_inside_words(dtype, rows, vocab):
+    """Gradient and logits apart by a word, by half of one, and every row differently."""
+    for shift, pad in ((1, 0), (1, 1), (0, 1), (3, 2)):
+        x = make(rows, 2, vocab, dtype, vocab, pad=pad, shift=shift)
+        check_policy(x, "tokens", 0.04, scale=4096.0 if dtype == torch.float16 else 1.0)
+        check_pairs(x, 0.2, 0.1, scale=4096.0 if dtype == torch.float16 else 1.0)
