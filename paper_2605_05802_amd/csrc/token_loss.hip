@@ -12,6 +12,7 @@
 //   row_stats_kernel     (m, s) of a row, or of a part of one
 //   policy_grad_kernel   few rows: the gradient and the loss; without a gradient policy_small_kernel
 //   row_info_*, policy_rows_kernel and policy_sum_kernel    the slopes of the rows and the loss
+//   pair_grad_kernel     few rows: the gradient and the loss
 //   pair_kernel          log ratios of a pair's sequences, the margin, the slopes of the pair's rows
 //   logit_grad_kernel    the gradient, from the row, (m, s) and the slope; in passing the pairs added up (pair_sum_kernel without one)
 //
@@ -36,6 +37,10 @@ constexpr int kMostSummedRows = 16384, kShares = 256;      // rows whose terms o
 constexpr int kMostInline = 1024;      // sequences of a small call
 constexpr int kMostTableRows = 4096;   // its rows
 constexpr int kMostSmallRows = 2048;   // rows whose slopes and terms one workgroup computes
+// Pairs, and workgroups, of a call for pair_grad_kernel.  Its wavefronts each go through a pair's rows: 256 rows of 4000 fp32 in 8 pairs
+// 10.7 us instead of 12.4, but 64 of 50021 f16, in 12 parts, 16.4 instead of 14.7, and 400 of 1024 fp32 in 16 pairs 13.7 instead of 13.
+constexpr int kMostSmallPairs = 8, kMostPairUnits = 256;
+static_assert(kMostPairUnits <= kTermThreads, "rows of a pair");
 constexpr int kMostAtOnce = 1024;      // workgroups of policy_grad_kernel, all of which run at once (2048 rows of 100000 fp32 in parts of 16 KB: 423 us, with a
                                        // kernel in between 395)
 constexpr int kParts = 8192;           // parts of rows that the workspace holds
@@ -300,11 +305,10 @@ struct PairArgs {
 
 // The mean over pairs of their terms, by a workgroup; s: THREADS / 64 doubles of LDS
 template <int THREADS>
-__device__ __forceinline__ void sum_pairs(const RowArgs &a, const PairArgs &p, double *s) {
-    const int pairs = a.n_seq / 2;
+__device__ __forceinline__ void sum_pairs(const float4 *terms, int pairs, const PairArgs &p, double *s) {
     double x[4] = {};
     for (int i = threadIdx.x; i < pairs; i += THREADS) {
-        const float4 t = a.terms[i];
+        const float4 t = terms[i];
         x[0] += t.x;
         x[1] += t.y;
         x[2] += t.z;
@@ -321,7 +325,7 @@ template <typename T, int WAVES>
 __global__ __launch_bounds__(row_block(WAVES)) void logit_grad_kernel(RowArgs a, PairArgs p) {
     constexpr int N = Elem<T>::kPerVec, LANES = 64 * WAVES;
     __shared__ double s[row_block(WAVES) / 64];
-    if (p.stats && blockIdx.x == 0) sum_pairs<row_block(WAVES)>(a, p, s);
+    if (p.stats && blockIdx.x == 0) sum_pairs<row_block(WAVES)>(a.terms, a.n_seq / 2, p, s);
     const int unit = WAVES == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
     const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
     if (unit >= a.n_rows * a.grad_splits) return;
@@ -675,12 +679,36 @@ __global__ __launch_bounds__(kSumThreads) void policy_small_kernel(RowArgs a, Po
     sums.finish(p, s);
 }
 
-// The gradient of few rows straight from their parts' (m, s): every workgroup works out its row's weight and slope while its first EARLY
-// vectors a thread are on their way, and one workgroup more, the first, the loss.  Kernels for 128 rows of 152064 fp32: 16 + 24 us, with a
-// kernel in between 16 + 6 + 22; 16 rows of 50021 f16 11 us instead of 14 a call.  Four vectors on their way: 2 us more, eight: 1.
+// The first vectors of a part, asked for while what their gradient takes is worked out
+template <typename T, int LANES>
+struct EarlyPart {
+    static constexpr int N = Elem<T>::kPerVec, COUNT = 12;
+    raw16 raw[COUNT];
+    __device__ __forceinline__ void load(const T *x, const Part<T> &q, int t) {
+#pragma unroll
+        for (int j = 0; j < COUNT; ++j)
+            if (q.from + j * LANES * N < q.full) raw[j] = load_vec_once(x + min(q.from + (j * LANES + t) * N, q.full - N));    // whole wavefronts
+    }
+    // the gradient of the whole part
+    __device__ __forceinline__ void write(const T *x, T *g, const Part<T> &q, int t, int target, float m, float factor, float slope) {
+        int e = q.from + t * N;
+        asm volatile("" : "+v"(e));                          // not a path of its own for every number of vectors
+        write_single<T>(x, g, q, t, target, m, factor, slope);
+#pragma unroll
+        for (int j = 0; j < COUNT; ++j) {
+            if (e + j * LANES * N < q.full) store_vec_once(g + e + j * LANES * N, gradient<T>(raw[j], target - e - j * LANES * N, m, factor, slope));
+            __builtin_amdgcn_sched_barrier(0);               // one vector's widened values at a time
+        }
+        write_gradient<T, LANES>(x, g, e + COUNT * LANES * N, q.full, target, m, factor, slope);
+    }
+};
+
+// The gradient of few rows straight from their parts' (m, s): every workgroup works out its row's weight and slope while its first
+// vectors are on their way, and one workgroup more, the first, the loss.  Kernels for 128 rows of 152064 fp32: 16 + 24 us, with a
+// kernel in between 16 + 6 + 22; 16 rows of 50021 f16 11 us instead of 14 a call.  Four of them a thread instead of twelve: 2 us more, eight: 1.
 template <typename T, int WAVES>
 __global__ __launch_bounds__(row_block(WAVES)) void policy_grad_kernel(RowArgs a, PolicyArgs p) {
-    constexpr int THREADS = row_block(WAVES), N = Elem<T>::kPerVec, LANES = 64 * WAVES, EARLY = 12;
+    constexpr int THREADS = row_block(WAVES), N = Elem<T>::kPerVec, LANES = 64 * WAVES;
     __shared__ SeqTable table;
     const SeqTable::Ahead ahead = SeqTable::ahead(a);
     if (blockIdx.x == 0) {
@@ -714,27 +742,17 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_grad_kernel(RowArgs a
     const float2 parts = a.part[(size_t)row * a.splits + min((int)threadIdx.x & 63, a.splits - 1)];
     RowInput in = {{}, read_uniform(a.chosen + row), read_uniform(p.old_logprob + row), p.ref_logprob ? read_uniform(p.ref_logprob + row) : 0.f};
     const int target = read_uniform(a.targets + row);
-    int e = q.from + t * N;
-    raw16 raw[EARLY];
-#pragma unroll
-    for (int j = 0; j < EARLY; ++j)
-        if (mine && q.from + j * LANES * N < q.full) raw[j] = load_vec_once(x + min(e + j * LANES * N, q.full - N));    // whole wavefronts
+    EarlyPart<T, LANES> early;
+    if (mine) early.load(x, q, t);
     table.template fill<THREADS>(a, ahead);
     if (!mine) return;
-    asm volatile("" : "+v"(e));                              // not a path of its own for every number of vectors
     const float2 info = table.info_of_wave(a, p, row);
     in.r = whole_row_of_wave(parts, a.splits);
     if (info.x == 0.f || in.r.s == kNoRow) return write_zeros<T, LANES>(g, q, t);
     float logprob;
     float4 term;
-    const float slope = row_outcome(a, p, info, in, &term, &logprob), m = in.r.m, factor = -slope / in.r.s;
-    write_single<T>(x, g, q, t, target, m, factor, slope);
-#pragma unroll
-    for (int j = 0; j < EARLY; ++j) {
-        if (e + j * LANES * N < q.full) store_vec_once(g + e + j * LANES * N, gradient<T>(raw[j], target - e - j * LANES * N, m, factor, slope));
-        __builtin_amdgcn_sched_barrier(0);                   // one vector's widened values at a time
-    }
-    write_gradient<T, LANES>(x, g, e + EARLY * LANES * N, q.full, target, m, factor, slope);
+    const float slope = row_outcome(a, p, info, in, &term, &logprob);
+    early.write(x, g, q, t, target, in.r.m, -slope / in.r.s, slope);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -889,6 +907,33 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_resident_kernel(RowAr
 // ---------------------------------------------------------------------------------------------
 // preference loss
 // ---------------------------------------------------------------------------------------------
+// A row's log ratio, and its log-probability; both 0 for one that does not count.  In double: a pair adds hundreds of them, and rounds
+// to single precision once.
+struct RowRatio {
+    double ratio, logprob;
+};
+__device__ __forceinline__ RowRatio row_ratio(const RowArgs &a, const PairArgs &p, int row, const RowSum &r, float chosen) {
+    const double ref = p.ref_logprob ? (double)p.ref_logprob[row] : 0.0;
+    if (r.s == kNoRow) return RowRatio{0.0, 0.0};
+    const double logprob = (double)(chosen - r.m) - log((double)r.s);
+    return RowRatio{logprob - ref, logprob};
+}
+// A pair's terms of the loss from its sequences' log ratios, and the slope of the preferred one's rows; the other's have its negative
+struct PairOutcome {
+    float4 term;
+    float slope;
+};
+__device__ __forceinline__ PairOutcome pair_outcome(const RowArgs &a, const PairArgs &p, double ratio0, double ratio1) {
+    const double reward0 = (double)p.beta * ratio0, reward1 = (double)p.beta * ratio1;
+    // The margin is a difference of sums in double; what becomes of it is good to single precision from there on.
+    const float m = (float)(reward0 - reward1), e = expf(-fabsf(m)), tail = log1pf(e), sm = p.smoothing;
+    // a term with weight 0 is left out: it may be infinite
+    const float loss = (sm < 1.f ? (1.f - sm) * (fmaxf(-m, 0.f) + tail) : 0.f) + (sm > 0.f ? sm * (fmaxf(m, 0.f) + tail) : 0.f);
+    const float small = e / (1.f + e), large = 1.f / (1.f + e);      // sigmoid(-|m|), sigmoid(|m|)
+    return PairOutcome{make_float4(loss, m > 0.f ? 1.f : 0.f, (float)reward0, (float)reward1),
+                       p.beta / (float)(a.n_seq / 2) * (sm * (m >= 0.f ? large : small) - (1.f - sm) * (m >= 0.f ? small : large)) * a.grad_scale};
+}
+
 // A workgroup a pair: log ratios, margin, slopes and the pair's terms of the loss.  Rows outside every sequence are left to the first and
 // the last pair.
 __global__ __launch_bounds__(kTermThreads) void pair_kernel(RowArgs a, PairArgs p) {
@@ -898,17 +943,12 @@ __global__ __launch_bounds__(kTermThreads) void pair_kernel(RowArgs a, PairArgs 
     double ratio[2] = {};
     for (int row = start + t; row < end; row += kTermThreads) {
         const float chosen = a.chosen[row];
-        const double ref = p.ref_logprob ? (double)p.ref_logprob[row] : 0.0;
         const RowSum r = whole_row(a, row);
-        double logprob = 0.0;
-        if (r.s != kNoRow) {
-            // l in double: a pair adds hundreds of them, and rounds to single precision once
-            logprob = (double)(chosen - r.m) - log((double)r.s);
-            if (row < mid) ratio[0] += logprob - ref;
-            else ratio[1] += logprob - ref;
-        }
+        const RowRatio x = row_ratio(a, p, row, r, chosen);
+        if (row < mid) ratio[0] += x.ratio;
+        else ratio[1] += x.ratio;
         a.whole[row] = make_float2(r.m, r.s);
-        if (a.token_logprob) a.token_logprob[row] = (float)logprob;
+        if (a.token_logprob) a.token_logprob[row] = (float)x.logprob;
     }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -918,21 +958,15 @@ __global__ __launch_bounds__(kTermThreads) void pair_kernel(RowArgs a, PairArgs 
     __syncthreads();
     ratio[0] = s_ratio[0];
     ratio[1] = s_ratio[1];
-    const double reward0 = (double)p.beta * ratio[0], reward1 = (double)p.beta * ratio[1];
-    // The margin is a difference of sums in double; what becomes of it is good to single precision from there on.
-    const float m = (float)(reward0 - reward1), e = expf(-fabsf(m)), tail = log1pf(e), sm = p.smoothing;
-    // a term with weight 0 is left out: it may be infinite
-    const float loss = (sm < 1.f ? (1.f - sm) * (fmaxf(-m, 0.f) + tail) : 0.f) + (sm > 0.f ? sm * (fmaxf(m, 0.f) + tail) : 0.f);
-    const float small = e / (1.f + e), large = 1.f / (1.f + e);      // sigmoid(-|m|), sigmoid(|m|)
-    const float slope = p.beta / (float)pairs * (sm * (m >= 0.f ? large : small) - (1.f - sm) * (m >= 0.f ? small : large)) * a.grad_scale;
+    const PairOutcome o = pair_outcome(a, p, ratio[0], ratio[1]);
     if (t == 0) {
-        a.terms[pair] = make_float4(loss, m > 0.f ? 1.f : 0.f, (float)reward0, (float)reward1);
+        a.terms[pair] = o.term;
         if (p.log_ratio) {
             p.log_ratio[2 * pair] = (float)ratio[0];
             p.log_ratio[2 * pair + 1] = (float)ratio[1];
         }
     }
-    for (int row = start + t; row < end; row += kTermThreads) a.slope[row] = row < mid ? slope : -slope;
+    for (int row = start + t; row < end; row += kTermThreads) a.slope[row] = row < mid ? o.slope : -o.slope;
     auto outside = [&](int row) {
         a.whole[row] = make_float2(0.f, kNoRow);
         if (a.token_logprob) a.token_logprob[row] = 0.f;
@@ -943,9 +977,94 @@ __global__ __launch_bounds__(kTermThreads) void pair_kernel(RowArgs a, PairArgs 
         for (int row = end + t; row < a.n_rows; row += kTermThreads) outside(row);
 }
 
+// A pair's rows, at most kTermThreads, and their log ratios by one wavefront, added up as pair_kernel's four would.  WRITE: the rows'
+// log-probabilities too.
+struct PairRows {
+    int start, mid, end;
+    double ratio[2];
+    // starts: seq_start, an entry a lane
+    __device__ __forceinline__ PairRows(const RowArgs &a, int starts, int pair)
+        : start(row_bound(a, __builtin_amdgcn_readlane(starts, 2 * pair))), mid(__builtin_amdgcn_readlane(starts, 2 * pair + 1)),
+          end(row_bound(a, __builtin_amdgcn_readlane(starts, 2 * pair + 2))) {}
+    template <bool WRITE>
+    __device__ __forceinline__ void add(const RowArgs &a, const PairArgs &p) {
+        constexpr int WAVES = kTermThreads / 64;
+        double x[WAVES][2] = {};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const int row = start + 64 * w + (int)(threadIdx.x & 63);
+            if (row >= end) continue;
+            const RowRatio one = row_ratio(a, p, row, whole_row(a, row), a.chosen[row]);
+            x[w][row < mid ? 0 : 1] = one.ratio;
+            if (WRITE && a.token_logprob) a.token_logprob[row] = (float)one.logprob;
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            ratio[k] = 0.0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                if (start + 64 * w >= end) continue;         // nothing but zeros
+#pragma unroll
+                for (int off = 32; off >= 1; off >>= 1) x[w][k] += __shfl_xor(x[w][k], off, 64);
+                ratio[k] += x[w][k];
+            }
+        }
+    }
+};
+
+// What pair_kernel, logit_grad_kernel and pair_sum_kernel do, for few rows: every wavefront works out the slope of its row's pair while
+// the row's first vectors are on their way, and one workgroup more, the first, the loss.  203 rows of 1024 fp32 in 8 pairs: 15 us
+// a call with a kernel in between, 12 without; the kernels 3.1 + 7.0 instead of 3.2 + 4.6 + 3.7.
+template <typename T, int WAVES>
+__global__ __launch_bounds__(row_block(WAVES)) void pair_grad_kernel(RowArgs a, PairArgs p) {
+    constexpr int THREADS = row_block(WAVES), LANES = 64 * WAVES;
+    const int pairs = a.n_seq / 2, lane = threadIdx.x & 63, starts = a.seq_start[min(lane, a.n_seq)];
+    if (blockIdx.x == 0) {
+        __shared__ double s[THREADS / 64];
+        __shared__ float4 terms[kMostSmallPairs];
+        for (int pair = threadIdx.x >> 6; pair < pairs; pair += THREADS / 64) {
+            PairRows rows(a, starts, __builtin_amdgcn_readfirstlane(pair));
+            rows.template add<true>(a, p);
+            if (lane == 0) {
+                terms[pair] = pair_outcome(a, p, rows.ratio[0], rows.ratio[1]).term;
+                if (p.log_ratio) {
+                    p.log_ratio[2 * pair] = (float)rows.ratio[0];
+                    p.log_ratio[2 * pair + 1] = (float)rows.ratio[1];
+                }
+            }
+        }
+        if (a.token_logprob) {                               // rows outside every sequence
+            const int first = row_bound(a, __builtin_amdgcn_readlane(starts, 0)), end = row_bound(a, __builtin_amdgcn_readlane(starts, a.n_seq));
+            for (int row = threadIdx.x; row < first; row += THREADS) a.token_logprob[row] = 0.f;
+            for (int row = end + threadIdx.x; row < a.n_rows; row += THREADS) a.token_logprob[row] = 0.f;
+        }
+        __syncthreads();
+        sum_pairs<THREADS>(terms, pairs, p, s);
+        return;
+    }
+    const int unit = WAVES == 1 ? __builtin_amdgcn_readfirstlane((blockIdx.x - 1) * 4 + (threadIdx.x >> 6)) : blockIdx.x - 1;
+    const int t = WAVES == 1 ? lane : threadIdx.x;
+    if (unit >= a.n_rows * a.grad_splits) return;
+    const int row = unit / a.grad_splits, part = unit - row * a.grad_splits;
+    const T *x = (const T *)a.logits + row * a.ld_logits;
+    T *g = (T *)a.grad + row * a.ld_grad;
+    const Part<T> q(x, part, a.grad_elems, a.vocab);
+    const float2 parts = a.part[(size_t)row * a.splits + min(lane, a.splits - 1)];
+    const int target = read_uniform(a.targets + row);
+    EarlyPart<T, LANES> early;
+    early.load(x, q, t);
+    const RowSum r = whole_row_of_wave(parts, a.splits);
+    const int seq = __popcll(__ballot(lane < a.n_seq && starts <= row)) - 1;
+    if (r.s == kNoRow || seq < 0) return write_zeros<T, LANES>(g, q, t);
+    PairRows rows(a, starts, seq >> 1);
+    rows.template add<false>(a, p);
+    const float of_preferred = pair_outcome(a, p, rows.ratio[0], rows.ratio[1]).slope, slope = row < rows.mid ? of_preferred : -of_preferred;
+    early.write(x, g, q, t, target, r.m, -slope / r.s, slope);
+}
+
 __global__ __launch_bounds__(kTermThreads) void pair_sum_kernel(RowArgs a, PairArgs p) {
     __shared__ double s[kTermThreads / 64];
-    sum_pairs<kTermThreads>(a, p, s);
+    sum_pairs<kTermThreads>(a.terms, a.n_seq / 2, p, s);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -1039,6 +1158,14 @@ int launch_logit_grad(const RowArgs &a, const PairArgs &p, int waves, hipStream_
 }
 
 template <typename T>
+int launch_pair_grad(const RowArgs &a, const PairArgs &p, int waves, hipStream_t stream) {
+    const int units = a.n_rows * a.grad_splits;
+    if (waves == 1) pair_grad_kernel<T, 1><<<dim3(ceil_div(units, 4) + 1), dim3(row_block(1)), 0, stream>>>(a, p);
+    else pair_grad_kernel<T, 4><<<dim3(units + 1), dim3(row_block(4)), 0, stream>>>(a, p);
+    SR_HIP(hipGetLastError());
+    return SR_OK;
+}
+template <typename T>
 int launch_policy_grad(const RowArgs &a, const PolicyArgs &p, int waves, hipStream_t stream) {
     const int units = a.n_rows * a.grad_splits;
     if (waves == 1) policy_grad_kernel<T, 1><<<dim3(ceil_div(units, 4) + 1), dim3(row_block(1)), 0, stream>>>(a, p);
@@ -1131,6 +1258,8 @@ int preference_loss(const sr_token_rows *x, const PairArgs &p, void *workspace, 
     return with_type(x->dtype, [&](auto *t) -> int {
         typedef std::remove_pointer_t<decltype(t)> T;
         if (a.n_rows > 0) SR_TRY(launch_row_stats<T>(a, plan.waves, stream));
+        if (a.grad && a.n_rows > 0 && a.n_seq <= 2 * kMostSmallPairs && a.n_rows * a.grad_splits <= kMostPairUnits)
+            return launch_pair_grad<T>(a, p, plan.grad_waves, stream);
         pair_kernel<<<dim3(a.n_seq / 2), dim3(kTermThreads), 0, stream>>>(a, p);
         SR_HIP(hipGetLastError());
         if (a.n_rows > 0 && a.grad) return launch_logit_grad<T>(a, p, plan.grad_waves, stream);

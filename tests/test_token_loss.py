@@ -695,3 +695,21 @@ def test_rows_that_begin_inside_words(dtype, rows, vocab):
         x = make(rows, 2, vocab, dtype, vocab, pad=pad, shift=shift)
         check_policy(x, "tokens", 0.04, scale=4096.0 if dtype == torch.float16 else 1.0)
         check_pairs(x, 0.2, 0.1, scale=4096.0 if dtype == torch.float16 else 1.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,pairs,vocab,pad,shift", [
+    (2, 1, 3, 0, 1), (256, 1, 515, 0, 0), (257, 1, 515, 0, 0), (256, 8, 2001, 0, 1), (256, 9, 2001, 1, 0), (255, 2, 3500, 0, 3), (10, 4, 50021, 0, 0),
+    (300, 1, 515, 0, 0), (512, 16, 2001, 0, 1), (513, 16, 2001, 0, 1), (512, 17, 2001, 1, 0), (500, 2, 7000, 0, 3), (65, 13, 50021, 0, 0),
+    (130, 1, 12288, 0, 0), (7, 3, 45056, 0, 0), (31, 16, 152064, 0, 1)])
+def test_few_pairs(dtype, rows, pairs, vocab, pad, shift):
+    """Either side of the sizes up to which the loss has two kernels; the sums are the same with and without a gradient."""
+    scale = 4096.0 if dtype == torch.float16 else 1.0
+    for masked, lead, tail in ((0.0, 0, 0), (0.3, rows // 9, rows // 7)):
+        x = make(rows, 2 * pairs, vocab, dtype, rows + vocab, pad=pad, shift=shift, masked=masked, lead=lead, tail=tail)
+        stats, lr, lp, g = check_pairs(x, 0.1, 0.2, scale=scale)
+        s1, r1, l1, none = run_pairs(x, 0.1, 0.2, grad=False, scale=scale)
+        assert torch.equal(s1, stats) and torch.equal(r1, lr) and torch.equal(l1, lp)
+        s2, r2, l2, g2 = run_pairs(x, 0.1, 0.2, in_place=True, scale=scale)
+        assert torch.equal(s2, stats) and torch.equal(r2, lr) and torch.equal(l2, lp) and torch.equal(g2, g)
