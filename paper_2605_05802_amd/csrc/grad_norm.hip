@@ -230,9 +230,10 @@ __global__ __launch_bounds__(kNormThreads) void scale_kernel(List l, uint32_t ch
     const Chunk k = find_chunk(l, chunk0 + blockIdx.x);
     auto factor = [&]() __attribute__((always_inline)) {     // holds barriers: once, by the whole workgroup
         const double norm = fabs((double)scale) * sqrt(sum_slots(slots, used, s));
-        if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
+        const float written = (float)norm;                   // the caller knows this one: infinite beyond FLT_MAX, and then nothing is scaled
+        if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = written;
         // a quotient of doubles, rounded once; false for NaN
-        return norm > (double)max_norm && norm <= DBL_MAX ? (float)((double)scale * ((double)max_norm / norm)) : scale;
+        return norm > (double)max_norm && written <= FLT_MAX ? (float)((double)scale * ((double)max_norm / norm)) : scale;
     };
     auto scale_by = [&](auto &&f) __attribute__((always_inline)) {
         switch (k.type * 4 + k.out_type) {

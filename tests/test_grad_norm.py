@@ -269,3 +269,21 @@ def test_host_tensors_are_refused():
     for make in (lambda t: sr.TensorList([t]), lambda t: sr.tensor_list([t]), lambda t: sr.sr_grad_norm([], t, t)):
         with pytest.raises(sr.SrError, match="device tensors expected"):
             make(torch.zeros(1))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("plan", [False, True])
+@pytest.mark.parametrize("value,scale", [(1e38, 1.0), (1e30, 1e9), (3e38, -2.0)])
+def test_a_norm_beyond_single_precision_scales_nothing(plan, value, scale):
+    """A hundred elements whose norm is finite in 64 bits and infinite as it is written: the factor is 1, in place and not."""
+    ts = [torch.full((n,), value, device="cuda") for n in (93, 7)]
+    assert norm_of(ts, scale) > torch.finfo(F32).max
+    before, outs = [t.clone() for t in ts], [torch.empty_like(t) for t in ts]
+    norm, ws = work()
+    sr.sr_grad_norm(ts, norm, ws, scale=scale)
+    assert norm.item() == math.inf
+    sr.sr_clip_grad_norm(sr.TensorList(ts, outs, plan=plan), 0.1, norm.fill_(7.0), ws, scale=scale)
+    assert norm.item() == math.inf
+    assert all(torch.equal(o, b * scale) for o, b in zip(outs, before)) and all(torch.equal(a, b) for a, b in zip(ts, before))
+    sr.sr_clip_grad_norm(sr.TensorList(ts, plan=plan), 0.1, norm.fill_(7.0), ws, scale=scale)
+    assert norm.item() == math.inf and all(torch.equal(a, b * scale) for a, b in zip(ts, before))
