@@ -187,6 +187,16 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(double *slots, int u
     *norm = (float)(fabs((double)scale) * sqrt(sum));
 }
 
+// What to multiply by, in two steps: where the whole of it is below the smallest normal number, 2^100 times it, which has all its bits, and
+// 2^-100.  Else the second is 1 and changes nothing (one product more an element of a kernel that waits for memory).
+struct Factor {
+    float first, second;
+};
+__device__ __forceinline__ Factor factor_of(double x) {
+    if (fabs(x) < (double)FLT_MIN) return Factor{(float)(x * 0x1p100), 0x1p-100f};
+    return Factor{(float)x, 1.f};
+}
+
 // Four elements a thread and step where 16-bit data become single precision, so that whole lines are written at once.
 // factor(): what to multiply by, asked for when the loads are under way.
 template <typename T, typename U, bool WHOLE, typename F>
@@ -205,13 +215,13 @@ __device__ __forceinline__ void scale_some(const T *p, U *q, int n, F &&factor) 
     const int rest = n / N * N + (int)threadIdx.x;
     float last = 0.f;
     if (!WHOLE && rest < n) last = (float)p[rest];
-    const float c = factor();
-    if (!WHOLE && rest < n) q[rest] = (U)(last * c);
+    const Factor c = factor();
+    if (!WHOLE && rest < n) q[rest] = (U)(last * c.first * c.second);
     each_vector<N, WHOLE>(n, [&](int j, int e) __attribute__((always_inline)) {
         float x[Elem<T>::kPerVec];
         Elem<T>::widen(raw[j], x);
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] *= c;
+        for (int i = 0; i < N; ++i) x[i] = x[i] * c.first * c.second;
         store_vec_once(q + e, Elem<U>::narrow(x));
     });
 }
@@ -233,7 +243,7 @@ __global__ __launch_bounds__(kNormThreads) void scale_kernel(List l, uint32_t ch
         const float written = (float)norm;                   // the caller knows this one: infinite beyond FLT_MAX, and then nothing is scaled
         if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = written;
         // a quotient of doubles, rounded once; false for NaN
-        return norm > (double)max_norm && written <= FLT_MAX ? (float)((double)scale * ((double)max_norm / norm)) : scale;
+        return norm > (double)max_norm && written <= FLT_MAX ? factor_of((double)scale * ((double)max_norm / norm)) : Factor{scale, 1.f};
     };
     auto scale_by = [&](auto &&f) __attribute__((always_inline)) {
         switch (k.type * 4 + k.out_type) {
@@ -245,8 +255,8 @@ __global__ __launch_bounds__(kNormThreads) void scale_kernel(List l, uint32_t ch
         }
     };
     if (k.data != k.out) return scale_by(factor);
-    const float c = factor();                                // in place: nothing is read where nothing changes
-    if (c != 1.f) scale_by([&]() { return c; });
+    const Factor c = factor();                               // in place: nothing is read where nothing changes
+    if (c.first != 1.f) scale_by([&]() { return c; });
 }
 
 int check_tensor(const sr_tensor &t, bool clip) {

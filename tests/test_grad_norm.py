@@ -287,3 +287,25 @@ def test_a_norm_beyond_single_precision_scales_nothing(plan, value, scale):
     assert all(torch.equal(o, b * scale) for o, b in zip(outs, before)) and all(torch.equal(a, b) for a, b in zip(ts, before))
     sr.sr_clip_grad_norm(sr.TensorList(ts, plan=plan), 0.1, norm.fill_(7.0), ws, scale=scale)
     assert norm.item() == math.inf and all(torch.equal(a, b * scale) for a, b in zip(ts, before))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,out,std,limit", [
+    (F32, F32, 1e30, 1e-10), (F32, F32, 1e30, 1e-25), (F32, F32, 1e36, 0.3), (BF16, F32, 1e30, 1e-10), (BF16, BF16, 1e30, 1e-25),
+    (F16, F32, 1e3, 1e-36), (F32, F32, 1.0, 1e-36), (BF16, BF16, 1e36, 0.3)])
+def test_factors_below_the_normal_numbers(dtype, out, std, limit):
+    """limit / norm is subnormal or 0 in single precision, the products are not."""
+    sizes = [5000, 77, 8192, 20001]
+    ts = tensors_of(sizes, [dtype], 13, std=std)
+    for scale in (1.0, -0.25):
+        assert limit / norm_of(ts) < 2.0 ** -126
+        check(ts, limit, scale=scale, out_dtype=out)
+    if out == dtype:
+        check(ts, limit, in_place=True)
+
+
+@pytest.mark.gpu
+def test_the_largest_norm_that_single_precision_holds_is_scaled():
+    top = torch.finfo(F32).max
+    check([torch.full((1,), top, device="cuda")], 1.0)
+    check([torch.full((1,), top, device="cuda")], 1.0, in_place=True)
