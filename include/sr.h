@@ -299,6 +299,9 @@ int sr_grpo_loss_static(const double *logprob, const float *rewards, int n_group
  * Arithmetic: the logits are widened to single precision; maximum, sum of exponentials, loss and slopes are single
  * precision, sums over tokens double, added in a fixed order (the results are the same bit for bit from call to call); the
  * gradient is rounded once, to the type of the logits.
+ *
+ * Outputs overlap neither each other, nor the workspace, nor an input; the gradient alone may lie in the place of the logits.
+ * That token_logprob shares nothing with old_logprob and ref_logprob is checked: different workgroups would read and write it.
  */
 typedef enum { SR_F32 = 0, SR_BF16 = 1, SR_F16 = 2 } sr_dtype;
 
@@ -310,7 +313,7 @@ typedef struct {
     const int32_t *targets;    /* device [n_rows] */
     const uint8_t *mask;       /* device [n_rows], 0 = the row does not count; NULL: all count */
     const int32_t *seq_start;  /* device [n_seq + 1] */
-    float *token_logprob;      /* device [n_rows], written; may be NULL */
+    float *token_logprob;      /* device [n_rows], written; may be NULL; shares no element with old_logprob and ref_logprob */
     int32_t dtype;             /* sr_dtype of logits and grad */
     int32_t n_rows, vocab, n_seq;
     float grad_scale;          /* multiplies the gradient only (loss scaling for 16-bit gradients) */
@@ -337,7 +340,8 @@ typedef struct {
  * tokens that the clip takes out of the gradient).
  * old_logprob, ref_logprob: device float [n_rows], as sr_score_chunk writes them; ref_logprob may be NULL if kl_coef == 0.
  * advantages: device float [n_seq].
- * SR_E_ARG: null pointers, a bad dtype, shape, stride or option, a workspace that is too small or not 16-byte aligned;
+ * SR_E_ARG: null pointers, a bad dtype, shape, stride or option, token_logprob overlapping old_logprob or ref_logprob, a workspace
+ * that is too small or not 16-byte aligned;
  * SR_E_LIMIT: more than 2^26 - 4 rows or 2^23 sequences, or more threads than a launch may have (2^32 - 1; a row of more than
  * 8 KiB takes 256, and so does every 16 KiB of a preference loss's gradient).  n_rows may be 0.
  */

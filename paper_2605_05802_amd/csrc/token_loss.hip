@@ -1077,6 +1077,12 @@ bool whole_words(std::initializer_list<const void *> pointers) {
     return true;
 }
 
+// Whether two arrays of n floats share any.  What a row's log-probability is compared with may not be what receives it: in the
+// kernels for few rows one workgroup writes while the others still read.
+bool overlap(const float *p, const float *q, int n) {
+    return p && q && n > 0 && (uintptr_t)p < (uintptr_t)(q + n) && (uintptr_t)q < (uintptr_t)(p + n);
+}
+
 int check_rows(const sr_token_rows *x, const void *workspace, size_t bytes) {
     if (!x || !workspace || (uintptr_t)workspace % 16) return SR_E_ARG;
     if (x->dtype < SR_F32 || x->dtype > SR_F16 || x->n_rows < 0 || x->vocab < 1 || x->n_seq < 1) return SR_E_ARG;
@@ -1280,6 +1286,8 @@ extern "C" int sr_policy_loss(const sr_token_rows *rows, const float *old_logpro
     if (!std::isfinite(opt->kl_coef) || (opt->kl_coef != 0.f && !ref_logprob && rows->n_rows > 0)) return SR_E_ARG;
     if (opt->reduce < SR_MEAN_TOKENS || opt->reduce > SR_MEAN_SUMS) return SR_E_ARG;
     if (!sr::whole_words({old_logprob, ref_logprob, advantages, stats})) return SR_E_ARG;
+    for (const float *in : {old_logprob, ref_logprob})
+        if (sr::overlap(rows->token_logprob, in, rows->n_rows)) return SR_E_ARG;
     const sr::PolicyArgs p = {old_logprob, ref_logprob, advantages, opt->clip_low, opt->clip_high, opt->kl_coef, opt->reduce, stats};
     return sr::policy_loss(rows, p, workspace, (hipStream_t)stream);
 }
@@ -1287,7 +1295,7 @@ extern "C" int sr_policy_loss(const sr_token_rows *rows, const float *old_logpro
 extern "C" int sr_preference_loss(const sr_token_rows *rows, const float *ref_logprob, float beta, float label_smoothing,
                                   float *log_ratio, float *stats, void *workspace, size_t workspace_bytes, void *stream) {
     SR_TRY(sr::check_rows(rows, workspace, workspace_bytes));
-    if (!sr::whole_words({ref_logprob, log_ratio, stats})) return SR_E_ARG;
+    if (!sr::whole_words({ref_logprob, log_ratio, stats}) || sr::overlap(rows->token_logprob, ref_logprob, rows->n_rows)) return SR_E_ARG;
     if (!stats || rows->n_seq % 2 || !std::isfinite(beta) || !(label_smoothing >= 0.f && label_smoothing <= 1.f)) return SR_E_ARG;
     const sr::PairArgs p = {ref_logprob, beta, label_smoothing, log_ratio, stats};
     return sr::preference_loss(rows, p, workspace, (hipStream_t)stream);

@@ -713,3 +713,32 @@ def test_few_pairs(dtype, rows, pairs, vocab, pad, shift):
         assert torch.equal(s1, stats) and torch.equal(r1, lr) and torch.equal(l1, lp)
         s2, r2, l2, g2 = run_pairs(x, 0.1, 0.2, in_place=True, scale=scale)
         assert torch.equal(s2, stats) and torch.equal(r2, lr) and torch.equal(l2, lp) and torch.equal(g2, g)
+
+
+def test_refusals_of_log_probabilities_that_are_read_and_written():
+    """The whole array, and one element of four, on either side."""
+    L, fake, base = sr.lib(), ctypes.c_void_p(4096), 1 << 20
+    opt = sr.PolicyOptions(0.2, 0.2, 0.1, 0)
+    for at in (base, base - 12, base + 12):
+        rows, same = ctypes.byref(_rows(token_logprob=base)), ctypes.c_void_p(at)
+        policy = lambda old, ref: L.sr_policy_loss(rows, old, ref, fake, ctypes.byref(opt), fake, fake, 1 << 20, None)
+        assert policy(same, fake) == policy(fake, same) == policy(same, same) == sr.SR_E_ARG
+        assert L.sr_preference_loss(rows, same, 0.1, 0.0, None, fake, fake, 1 << 20, None) == sr.SR_E_ARG
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,vocab", [(6, 300), (6, 50021), (300, 20003)])
+def test_log_probabilities_beside_the_ones_they_are_compared_with(rows, vocab):
+    """Three neighbours in one array."""
+    x = make(rows, 2, vocab, torch.bfloat16, 17)
+    stats, lp, g = run_policy(x, "tokens", 0.04)
+    _, _, plp, pg = run_pairs(x, 0.1, 0.0)
+    three = torch.cat([x["old_logprob"], torch.full_like(lp, 7.0), x["ref_logprob"]])
+    old, out, ref = three.split(rows)
+    ws = torch.empty(sr.token_loss_workspace(rows, 2), dtype=torch.uint8, device="cuda")
+    grad, s = torch.empty_like(g), torch.empty(4, device="cuda")
+    sr.sr_policy_loss(x["logits"], x["targets"], x["seq_start"], old, x["advantages"], s, ws, ref_logprob=ref, grad=grad, token_logprob=out,
+                      clip_low=LOW, clip_high=HIGH, kl_coef=0.04)
+    assert torch.equal(s, stats) and torch.equal(out, lp) and torch.equal(grad, g)
+    sr.sr_preference_loss(x["logits"], x["targets"], x["seq_start"], s, ws, ref_logprob=ref, grad=grad, token_logprob=out.fill_(7.0))
+    assert torch.equal(out, plp) and torch.equal(grad, pg)
