@@ -528,7 +528,9 @@ __global__ __launch_bounds__(kSumThreads) void row_info_small_kernel(RowArgs a, 
 __device__ __forceinline__ float policy_row(const PolicyArgs &p, float2 info, float logprob, float old_logprob, float ref_logprob,
                                             float4 *term) {
     const float A = info.y, ratio = expf(logprob - old_logprob);
-    const float plain = ratio * A, clipped = fminf(fmaxf(ratio, 1.f - p.clip_low), 1.f + p.clip_high) * A;
+    // an advantage of 0 leaves the row out, also where the ratio is beyond single precision (0 times infinity); NaN stays
+    const float plain = A == 0.f && ratio > FLT_MAX ? 0.f : ratio * A;
+    const float clipped = fminf(fmaxf(ratio, 1.f - p.clip_low), 1.f + p.clip_high) * A;
     const bool out = plain > clipped;
     float slope = out ? 0.f : -plain;
     *term = make_float4(out ? clipped : plain, 0.f, out ? 1.f : 0.f, info.x);

@@ -742,3 +742,18 @@ def test_log_probabilities_beside_the_ones_they_are_compared_with(rows, vocab):
     assert torch.equal(s, stats) and torch.equal(out, lp) and torch.equal(grad, g)
     sr.sr_preference_loss(x["logits"], x["targets"], x["seq_start"], s, ws, ref_logprob=ref, grad=grad, token_logprob=out.fill_(7.0))
     assert torch.equal(out, plp) and torch.equal(grad, pg)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab", [(40, 900), (40, 33003), (260, 16001), (300, 152064)])
+def test_advantage_zero_leaves_a_row_out_whatever_its_ratio(dtype, rows, vocab):
+    """exp(l - old) beyond single precision, times 0: the surrogate and the slope are 0, as the formula has them."""
+    x = make(rows, 5, vocab, dtype, 21, cuts=[0, rows // 4, rows // 2, rows // 2, rows - 3, rows])
+    x["old_logprob"][:rows // 4] = -150.0                          # the advantage of sequence 0 is 0
+    assert x["advantages"][0].item() == 0.0
+    for kl in (0.0, 0.04):
+        for grad in (True, False):
+            stats, lp, g = check_policy(x, "sequences", kl, grad=grad, scale=4096.0 if dtype == torch.float16 else 1.0)
+            assert bool(torch.isfinite(stats).all()) and (g is None or bool(torch.isfinite(g).all()))
+            assert kl or g is None or bool((g[:rows // 4] == 0).all())
