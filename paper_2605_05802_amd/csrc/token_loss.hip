@@ -738,6 +738,8 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_grad_kernel(RowArgs a
     const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
     const bool mine = unit < a.n_rows * a.grad_splits;       // false for a wavefront beside others that has nothing left
     const int row = mine ? unit / a.grad_splits : 0, part = mine ? unit - row * a.grad_splits : 0;
+    const bool counts = mine && row_counts(a, row);          // a row that does not is not read; asked first: scalar loads are waited for all at once
+    __builtin_amdgcn_sched_barrier(0);
     const T *x = (const T *)a.logits + row * a.ld_logits;
     T *g = (T *)a.grad + row * a.ld_grad;
     const Part<T> q(x, part, a.grad_elems, a.vocab);
@@ -745,7 +747,7 @@ __global__ __launch_bounds__(row_block(WAVES)) void policy_grad_kernel(RowArgs a
     RowInput in = {{}, read_uniform(a.chosen + row), read_uniform(p.old_logprob + row), p.ref_logprob ? read_uniform(p.ref_logprob + row) : 0.f};
     const int target = read_uniform(a.targets + row);
     EarlyPart<T, LANES> early;
-    if (mine) early.load(x, q, t);
+    if (counts) early.load(x, q, t);
     table.template fill<THREADS>(a, ahead);
     if (!mine) return;
     const float2 info = table.info_of_wave(a, p, row);
@@ -1048,13 +1050,15 @@ __global__ __launch_bounds__(row_block(WAVES)) void pair_grad_kernel(RowArgs a, 
     const int t = WAVES == 1 ? lane : threadIdx.x;
     if (unit >= a.n_rows * a.grad_splits) return;
     const int row = unit / a.grad_splits, part = unit - row * a.grad_splits;
+    const bool counts = row_counts(a, row);                  // a row that does not is not read; asked first: scalar loads are waited for all at once
+    __builtin_amdgcn_sched_barrier(0);
     const T *x = (const T *)a.logits + row * a.ld_logits;
     T *g = (T *)a.grad + row * a.ld_grad;
     const Part<T> q(x, part, a.grad_elems, a.vocab);
     const float2 parts = a.part[(size_t)row * a.splits + min(lane, a.splits - 1)];
     const int target = read_uniform(a.targets + row);
     EarlyPart<T, LANES> early;
-    early.load(x, q, t);
+    if (counts) early.load(x, q, t);
     const RowSum r = whole_row_of_wave(parts, a.splits);
     const int seq = __popcll(__ballot(lane < a.n_seq && starts <= row)) - 1;
     if (r.s == kNoRow || seq < 0) return write_zeros<T, LANES>(g, q, t);

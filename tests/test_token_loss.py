@@ -757,3 +757,47 @@ def test_advantage_zero_leaves_a_row_out_whatever_its_ratio(dtype, rows, vocab):
             stats, lp, g = check_policy(x, "sequences", kl, grad=grad, scale=4096.0 if dtype == torch.float16 else 1.0)
             assert bool(torch.isfinite(stats).all()) and (g is None or bool(torch.isfinite(g).all()))
             assert kl or g is None or bool((g[:rows // 4] == 0).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("pairs,rows,n_seq,vocab,dtype", [(False, 128, 4, 152064, torch.float32), (False, 16, 4, 400000, torch.float16),
+                                                          (True, 64, 4, 10200, torch.float32), (True, 62, 16, 20400, torch.bfloat16)])
+def test_few_rows_that_do_not_count_cost_no_reading(pairs, rows, n_seq, vocab, dtype):
+    """The logits in pinned memory of the host, some hundred times as slow to read: a call in which no row counts, by the mask or because
+    every row lies outside the sequences, takes nothing like the time of one in which all do (both readings of every row)."""
+    x = make(rows, n_seq, vocab, dtype, 5)
+    far = torch.empty(rows, vocab, dtype=dtype, pin_memory=True)
+    far.copy_(x["logits"])
+    lp, stats, grad = torch.empty(rows, device="cuda"), torch.empty(4, device="cuda"), torch.empty_like(x["logits"])
+    ws = torch.empty(sr.token_loss_workspace(rows, n_seq), dtype=torch.uint8, device="cuda")
+    opt, L = sr.PolicyOptions(LOW, HIGH, 0.04, 0), sr.lib()
+    at = lambda t: None if t is None else t.data_ptr()
+
+    def microseconds(mask, seq_start):
+        r = sr.TokenRows(at(far), at(grad), vocab, vocab, at(x["targets"]), at(mask), at(seq_start), at(lp),
+                         {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}[dtype], rows, vocab, n_seq, 1.0, 0)
+        times = []
+        for _ in range(6):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            torch.cuda.synchronize()
+            a.record()
+            stream = torch.cuda.current_stream().cuda_stream
+            if pairs:
+                status = L.sr_preference_loss(r, at(x["ref_logprob"]), 0.1, 0.0, None, at(stats), at(ws), ws.nbytes, stream)
+            else:
+                status = L.sr_policy_loss(r, at(x["old_logprob"]), at(x["ref_logprob"]), at(x["advantages"]), opt, at(stats), at(ws), ws.nbytes, stream)
+            b.record()
+            torch.cuda.synchronize()
+            assert status == sr.SR_OK
+            times.append(1000.0 * a.elapsed_time(b))
+        return min(times[1:])
+
+    all_rows = microseconds(None, x["seq_start"])
+    assert bool(torch.isfinite(grad).all()) and bool((grad != 0).any(1).all())
+    masked = microseconds(torch.zeros(rows, dtype=torch.uint8, device="cuda"), x["seq_start"])
+    assert bool((grad == 0).all()) and bool((lp == 0).all())
+    grad.fill_(7.0)
+    outside = microseconds(None, torch.full_like(x["seq_start"], rows))
+    assert bool((grad == 0).all()) and bool((lp == 0).all())
+    # the second reading alone, or as much of it as a thread asks for ahead, is a third of it at the least
+    assert max(masked, outside) < all_rows / 4, (masked, outside, all_rows)
