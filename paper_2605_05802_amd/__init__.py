@@ -238,15 +238,16 @@ def token_loss_workspace(n_rows: int, n_seq: int) -> int:
     return 65536 + 64 * n_rows + 32 * n_seq
 
 
-_types = {}
+_types = None
 
 
 def _dtypes():
-    """torch's element types -> sr_dtype."""
-    if not _types:
+    """torch's element types -> sr_dtype, and the types of _of_type."""
+    global _types
+    if _types is None:
         import torch
-        _types.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
-        _types["f4"], _types["i4"], _types["u1"] = torch.float32, torch.int32, torch.uint8
+        # whole at once: another thread sees all of it or nothing
+        _types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, "f4": torch.float32, "i4": torch.int32, "u1": torch.uint8}
     return _types
 
 

@@ -801,3 +801,52 @@ def test_few_rows_that_do_not_count_cost_no_reading(pairs, rows, n_seq, vocab, d
     assert bool((grad == 0).all()) and bool((lp == 0).all())
     # the second reading alone, or as much of it as a thread asks for ahead, is a third of it at the least
     assert max(masked, outside) < all_rows / 4, (masked, outside, all_rows)
+
+
+THREADS = """
+import importlib, sys, threading
+import torch
+import paper_2605_05802_amd as sr
+
+def call():
+    try:
+        sr.sr_grad_norm([], torch.zeros(1), torch.zeros(1))
+    except sr.SrError:
+        return                                                     # host tensors
+    except Exception as e:
+        bad.append(repr(e))
+
+bad, k, lines = [], 0, 1
+while k < lines:
+    importlib.reload(sr)                                           # nothing called yet
+    lines = 0
+
+    def trace(frame, event, arg):
+        global lines
+        if frame.f_code.co_filename != sr.__file__:
+            return None
+        if event == "line":
+            lines += 1
+            if lines == k + 1:
+                other = threading.Thread(target=call)
+                other.start()
+                other.join()
+        return trace
+
+    sys.settrace(trace)
+    call()
+    sys.settrace(None)
+    k += 1
+print(k, bad)
+sys.exit(1 if bad or k < 5 else 0)
+"""
+
+
+def test_a_first_call_in_the_middle_of_another_threads_first_call():
+    """At every line of the binding that the first call passes, another thread makes one of its own from beginning to end."""
+    import os
+    import subprocess
+    import sys
+    r = subprocess.run([sys.executable, "-c", THREADS], capture_output=True, text=True, timeout=120,
+                       cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0, r.stdout + r.stderr
