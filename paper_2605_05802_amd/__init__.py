@@ -260,6 +260,13 @@ def _of_type(t, kind: str, n: int, what: str):
     return t.data_ptr()
 
 
+def _workspace(where, t):
+    """Address and size of a workspace: the elements of an expanded one are not as many bytes of memory."""
+    if not t.is_contiguous():
+        raise SrError(SR_E_ARG, f"{where}: workspace: contiguous tensor expected")
+    return t.data_ptr(), t.nbytes
+
+
 def _on_device(where, *tensors):
     for t in tensors:
         if t is not None and not t.is_cuda:
@@ -295,8 +302,9 @@ def sr_policy_loss(logits, targets, seq_start, old_logprob, advantages, stats, w
     opt = PolicyOptions(clip_low, clip_high, kl_coef, REDUCE[reduce])
     old, ref = _of_type(old_logprob, "f4", n, "old_logprob"), _of_type(ref_logprob, "f4", n, "ref_logprob")
     adv, to = _of_type(advantages, "f4", n_seq, "advantages"), _of_type(stats, "f4", 4, "stats")
+    ws, size = _workspace("sr_policy_loss", workspace)
     _on_device("sr_policy_loss", logits, targets, seq_start, mask, grad, token_logprob, old_logprob, ref_logprob, advantages, stats, workspace)
-    _check(lib().sr_policy_loss(rows, old, ref, adv, opt, to, workspace.data_ptr(), workspace.nbytes, _stream(stream)), "sr_policy_loss")
+    _check(lib().sr_policy_loss(rows, old, ref, adv, opt, to, ws, size, _stream(stream)), "sr_policy_loss")
 
 
 def sr_preference_loss(logits, targets, seq_start, stats, workspace, *, mask=None, ref_logprob=None, grad=None,
@@ -306,9 +314,9 @@ def sr_preference_loss(logits, targets, seq_start, stats, workspace, *, mask=Non
     and of the other sequences; log_ratio float32 [sequences]."""
     rows, n, n_seq = _token_rows("sr_preference_loss", logits, targets, seq_start, mask, grad, token_logprob, grad_scale)
     ref, ratio, to = _of_type(ref_logprob, "f4", n, "ref_logprob"), _of_type(log_ratio, "f4", n_seq, "log_ratio"), _of_type(stats, "f4", 4, "stats")
+    ws, size = _workspace("sr_preference_loss", workspace)
     _on_device("sr_preference_loss", logits, targets, seq_start, mask, grad, token_logprob, ref_logprob, log_ratio, stats, workspace)
-    _check(lib().sr_preference_loss(rows, ref, beta, label_smoothing, ratio, to, workspace.data_ptr(), workspace.nbytes, _stream(stream)),
-           "sr_preference_loss")
+    _check(lib().sr_preference_loss(rows, ref, beta, label_smoothing, ratio, to, ws, size, _stream(stream)), "sr_preference_loss")
 
 
 class TensorList:
@@ -359,8 +367,9 @@ def _norm_call(tensors, name, numbers, norm, workspace, stream):
         tensors = TensorList(tensors)
     _dtypes()
     to = _of_type(norm, "f4", 1, "norm")
-    _on_device(name, norm, workspace)
-    tail = to, workspace.data_ptr(), workspace.nbytes, _stream(stream)
+    ws, size = _workspace("sr_" + name, workspace)
+    _on_device("sr_" + name, norm, workspace)
+    tail = to, ws, size, _stream(stream)
     if tensors.plan is not None:
         _check(getattr(lib(), "sr_planned_" + name)(tensors.plan, *numbers, *tail), "sr_" + name)
     else:

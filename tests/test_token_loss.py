@@ -850,3 +850,13 @@ def test_a_first_call_in_the_middle_of_another_threads_first_call():
     r = subprocess.run([sys.executable, "-c", THREADS], capture_output=True, text=True, timeout=120,
                        cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
     assert r.returncode == 0, r.stdout + r.stderr
+
+
+def test_workspaces_of_fewer_bytes_than_elements_are_refused():
+    i32, ws = torch.int32, torch.zeros(1, dtype=torch.uint8).expand(1 << 20)
+    rows = dict(logits=torch.zeros(4, 10), targets=torch.zeros(4, dtype=i32), seq_start=torch.zeros(3, dtype=i32), stats=torch.zeros(4), workspace=ws)
+    for call in (lambda: sr.sr_policy_loss(old_logprob=torch.zeros(4), advantages=torch.zeros(2), **rows), lambda: sr.sr_preference_loss(**rows),
+                 lambda: sr.sr_grad_norm([], torch.zeros(1), ws), lambda: sr.sr_clip_grad_norm([], 1.0, torch.zeros(1), ws)):
+        with pytest.raises(sr.SrError, match="workspace: contiguous") as e:
+            call()
+        assert e.value.status == sr.SR_E_ARG
