@@ -299,6 +299,8 @@ def sr_policy_loss(logits, targets, seq_start, old_logprob, advantages, stats, w
     advantages float32 [sequences]; mask uint8 [rows]; stats float32 [4] receives loss, surrogate, KL, clipped fraction;
     workspace: device bytes, token_loss_workspace(rows, sequences) of them; reduce: "tokens", "sequences" or "sums"."""
     rows, n, n_seq = _token_rows("sr_policy_loss", logits, targets, seq_start, mask, grad, token_logprob, grad_scale)
+    if reduce not in REDUCE:
+        raise SrError(SR_E_ARG, f"sr_policy_loss: reduce: one of {', '.join(REDUCE)} expected, got {reduce!r}")
     opt = PolicyOptions(clip_low, clip_high, kl_coef, REDUCE[reduce])
     old, ref = _of_type(old_logprob, "f4", n, "old_logprob"), _of_type(ref_logprob, "f4", n, "ref_logprob")
     adv, to = _of_type(advantages, "f4", n_seq, "advantages"), _of_type(stats, "f4", 4, "stats")

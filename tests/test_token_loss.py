@@ -860,3 +860,12 @@ def test_workspaces_of_fewer_bytes_than_elements_are_refused():
         with pytest.raises(sr.SrError, match="workspace: contiguous") as e:
             call()
         assert e.value.status == sr.SR_E_ARG
+
+
+@pytest.mark.parametrize("reduce", ["token", "mean", None, 0])
+def test_a_mean_that_does_not_exist_is_refused(reduce):
+    i32 = torch.int32
+    with pytest.raises(sr.SrError, match="reduce: one of tokens, sequences, sums") as e:
+        sr.sr_policy_loss(torch.zeros(4, 10), torch.zeros(4, dtype=i32), torch.zeros(3, dtype=i32), torch.zeros(4), torch.zeros(2), torch.zeros(4),
+                          torch.zeros(sr.token_loss_workspace(4, 2), dtype=torch.uint8), reduce=reduce)
+    assert e.value.status == sr.SR_E_ARG
