@@ -309,3 +309,116 @@ def test_the_largest_norm_that_single_precision_holds_is_scaled():
     top = torch.finfo(F32).max
     check([torch.full((1,), top, device="cuda")], 1.0)
     check([torch.full((1,), top, device="cuda")], 1.0, in_place=True)
+
+
+def clip_direct(ts, max_norm, norm, ws, outs=None, scale=1.0, stream=None):
+    """The call over a list that is not planned: the tensors travel in the arguments of launches of at most 184."""
+    listed = sr.TensorList(ts, outs)
+    assert listed.plan is None
+    sr.sr_clip_grad_norm(listed, max_norm, norm, ws, scale=scale, stream=stream)
+
+
+def check_direct(ts, max_norm, scale=1.0, out_dtype=None, in_place=False):
+    want = norm_of(ts, scale)
+    c = scale * (max_norm / want if want > max_norm else 1.0)
+    expect = [t.double() * c for t in ts]
+    norm, ws = work()
+    outs = None if in_place else [torch.full_like(t, 5.0, dtype=out_dtype or t.dtype) for t in ts]
+    clip_direct(ts, max_norm, norm, ws, outs, scale)
+    assert norm.item() == pytest.approx(want, rel=4 * U)
+    for got, e in zip(ts if in_place else outs, expect):
+        assert bool(((got.double() - e).abs() <= e.abs() * (4 * U + ROUND[got.dtype]) + SMALLEST[got.dtype]).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,out", [(F32, F32), (BF16, BF16), (BF16, F32), (F16, F16), (F16, F32)])
+@pytest.mark.parametrize("sizes", [[1], [0, 3, 0], [8191, 8192, 8193], [5, 100003, 1, 64, 262147], list(range(1, 400)), [1 << 24, 77]])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_lists_in_the_arguments(dtype, out, sizes, shift):
+    ts = tensors_of(sizes, [dtype], 21, shift=shift)
+    norm = norm_of(ts)
+    for limit, scale in ((0.5 * norm, 1.0), (2 * norm, 1.0), (0.1 * norm, -0.5)):
+        check_direct(ts, limit, scale, out)
+    if out == dtype:
+        check_direct(ts, 2 * norm, in_place=True)
+        check_direct(ts, 0.5 * norm, in_place=True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("count", [183, 184, 185, 368, 369, 1500])
+@pytest.mark.parametrize("most", [9, 30000])
+def test_lists_of_several_launches(count, most):
+    """Either side of what one launch takes, empty tensors and all three types among them; few chunks, whose workgroups add the squares
+    up for themselves and of which the first launch writes the norm, and many."""
+    sizes = [(i * 7919) % most for i in range(count)]
+    ts = tensors_of(sizes, [F32, BF16, F16], 22)
+    check_direct(ts, 0.3 * norm_of(ts), scale=0.5, out_dtype=F32)
+    check_direct(ts, 0.3 * norm_of(ts), in_place=True)
+
+
+@pytest.mark.gpu
+def test_launches_that_share_the_workspace_and_read_past_the_caches():
+    """Several thousand tensors, 560 MB of them: sums of many launches, and the part that the second pass finds in the caches begins
+    inside one of them."""
+    ts = tensors_of([3 + i % 5 for i in range(1500)] + ([20_000_001] + [9] * 130) * 7, [F32], 23)
+    check_direct(ts, 0.3)
+    check_direct(ts, 0.2, in_place=True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,out", [(F32, F32), (BF16, BF16), (BF16, F32), (F16, F16)])
+@pytest.mark.parametrize("shift", [0, 1, 3])
+def test_lists_in_the_arguments_write_nothing_but_the_outputs(dtype, out, shift):
+    sizes = [1, 8192, 5, 8191, 20000, 3] * 40
+    ts = tensors_of(sizes, [dtype], 24, shift=shift)
+    before = [t.clone() for t in ts]
+    buf = torch.full((sum(sizes) + 3 * len(sizes) + 64,), 3.0, dtype=out, device="cuda")
+    outs, at, gaps = [], shift, torch.ones_like(buf, dtype=torch.bool)
+    for n in sizes:
+        outs.append(buf[at:at + n])
+        gaps[at:at + n] = False
+        at += n + 3
+    norm = torch.full((3,), 7.0, device="cuda")
+    ws = torch.full((512 + sr.GRAD_NORM_WORKSPACE + 512,), 77, dtype=torch.uint8, device="cuda")
+    want = norm_of(ts)
+    clip_direct(ts, 0.5 * want, norm[1:2], ws[512:-512], outs)
+    for o, t in zip(outs, ts):
+        e = t.double() * 0.5
+        assert bool(((o.double() - e).abs() <= e.abs() * (4 * U + ROUND[out]) + SMALLEST[out]).all())
+    assert bool((buf[gaps] == 3.0).all()) and all(torch.equal(a, b) for a, b in zip(ts, before))
+    assert norm[0].item() == norm[2].item() == 7.0 and norm[1].item() == pytest.approx(want, rel=4 * U)
+    assert bool((ws[:512] == 77).all()) and bool((ws[-512:] == 77).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sizes", [[100000, 33, 9_000_001], [50, 9000] * 150])
+def test_lists_in_the_arguments_on_streams_and_in_graphs(sizes):
+    """A captured call holds its list: every replay gives what an eager call does, also with new values."""
+    ts = tensors_of(sizes, [F32, BF16], 25)
+    outs = [torch.empty_like(t) for t in ts]
+    norm, ws = work()
+    clip_direct(ts, 0.5, norm, ws, outs)
+    want, first = norm.clone(), [o.clone() for o in outs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    norm.fill_(7.0)
+    side.wait_stream(torch.cuda.current_stream())
+    clip_direct(ts, 0.5, norm, ws, outs, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(norm, want) and all(torch.equal(a, b) for a, b in zip(outs, first))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        clip_direct(ts, 0.5, norm, ws, outs)
+    for k in range(4):
+        if k == 2:
+            ts[0].mul_(3.0)
+            clip_direct(ts, 0.5, norm, ws, outs)
+            want, first = norm.clone(), [o.clone() for o in outs]
+        norm.fill_(7.0)
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(norm, want) and all(torch.equal(a, b) for a, b in zip(outs, first))
