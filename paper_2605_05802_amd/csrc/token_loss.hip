@@ -130,18 +130,7 @@ constexpr int64_t kKeepBytes = 384 << 20;
 // s of a row that does not count
 constexpr float kNoRow = -1.f;
 
-// An entry of seq_start as an end of a range of rows, whatever it holds
-__device__ __forceinline__ int row_bound(const RowArgs &a, int row) { return min(max(row, 0), a.n_rows); }
-// the sequence of a row, or -1: the last one that begins at or before it
-__device__ __forceinline__ int sequence_of(const int32_t *seq_start, int n_seq, int row) {
-    int lo = -1, hi = n_seq;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (seq_start[mid] <= row) lo = mid;
-        else hi = mid;
-    }
-    return lo >= 0 && row < seq_start[lo + 1] ? lo : -1;
-}
+__device__ __forceinline__ int row_bound(const RowArgs &a, int row) { return sr::row_bound(row, a.n_rows); }
 // A uniform row's mask, by a scalar load of the word that holds it where all of that word is the mask's
 __device__ __forceinline__ bool masked_in(const RowArgs &a, int row) {
     if (!a.mask) return true;

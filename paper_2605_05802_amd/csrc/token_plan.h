@@ -1,4 +1,4 @@
-// Which kernels the losses over token rows run on, in plain C++ so that the rules can be evaluated without a GPU.
+// Which kernels the losses over token rows run on, and the rows of a sequence, in plain C++ so that the rules can be evaluated without a GPU.
 #pragma once
 #include <cstdint>
 
@@ -54,6 +54,20 @@ inline RowPlan plan_policy_rows(int n_rows, int vocab, int elem_bytes) {
     RowPlan p{waves, each > 0 ? each : 1};
     split_row(ceil_div(vocab, per_vec), per_vec, 1, &p.parts, &p.elems);
     return p;
+}
+
+// An entry of seq_start as an end of a range of rows, whatever it holds
+constexpr int row_bound(int row, int n_rows) { return row < 0 ? 0 : row < n_rows ? row : n_rows; }
+// The sequence of a row, or -1: the last one that begins at or before it, found among seq_start[0 .. n_seq - 1] whatever they hold; then one
+// entry more is read, at most seq_start[n_seq].
+constexpr int sequence_of(const int32_t *seq_start, int n_seq, int row) {
+    int lo = -1, hi = n_seq;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (seq_start[mid] <= row) lo = mid;
+        else hi = mid;
+    }
+    return lo >= 0 && row < seq_start[lo + 1] ? lo : -1;
 }
 
 // A launch has at most 2^32 - 1 threads

@@ -869,3 +869,77 @@ def test_a_mean_that_does_not_exist_is_refused(reduce):
         sr.sr_policy_loss(torch.zeros(4, 10), torch.zeros(4, dtype=i32), torch.zeros(3, dtype=i32), torch.zeros(4), torch.zeros(2), torch.zeros(4),
                           torch.zeros(sr.token_loss_workspace(4, 2), dtype=torch.uint8), reduce=reduce)
     assert e.value.status == sr.SR_E_ARG
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,vocab,n_seq", [(300, 500, 6), (40, 9000, 2), (5000, 64, 1500), (260, 50001, 4), (20, 900, 16), (5, 300, 2)])
+@pytest.mark.parametrize("masked", [0.0, 0.3])
+def test_starts_that_make_no_sense_write_nothing_beside_the_outputs(rows, vocab, n_seq, masked):
+    """Elements around and between the gradient's rows, bytes around the workspace and elements around every small output."""
+    x = make(rows, n_seq, vocab, torch.bfloat16, 6, masked=masked)
+    rng = np.random.default_rng(2)
+    top, ld, need = 2 ** 31 - 1, vocab + 7, sr.token_loss_workspace(rows, n_seq)
+    for starts in ([top] * (n_seq + 1), [-top - 1] * (n_seq + 1), rng.integers(-5, rows + 5, n_seq + 1).tolist(),
+                   [rows] + [0] * (n_seq - 1) + [top], [-3] + [top] * (n_seq - 1) + [rows // 2], [top] + [5] * n_seq,
+                   [-rows] * n_seq + [top], [0] * n_seq + [rows + 1], [-1] + [rows + 1] * n_seq):
+        seq_start = torch.tensor(starts, dtype=torch.int64, device="cuda").to(torch.int32)
+        for pairs, grad in ((False, True), (False, False), (True, True), (True, False)):
+            around = torch.full((64 + rows * ld + 64,), 3.0, dtype=torch.bfloat16, device="cuda")
+            g = around[64:64 + rows * ld].view(rows, ld)[:, :vocab]
+            ws = torch.full((4096 + need + 4096,), 77, dtype=torch.uint8, device="cuda")
+            sizes, small, at = [4, rows, n_seq], torch.full((4 + rows + n_seq + 4 * 1024,), 5.0, device="cuda"), 0
+            outs, gaps = [], torch.ones_like(small, dtype=torch.bool)
+            for n in sizes:
+                at += 1024
+                outs.append(small[at:at + n])
+                gaps[at:at + n] = False
+                at += n
+            inputs = [x[k] for k in ("logits", "targets", "old_logprob", "ref_logprob", "advantages")] + [seq_start]
+            before = [t.clone() for t in inputs]
+            common = dict(mask=x["mask"], ref_logprob=x["ref_logprob"], grad=g if grad else None, token_logprob=outs[1])
+            if pairs:
+                sr.sr_preference_loss(x["logits"], x["targets"], seq_start, outs[0], ws[4096:4096 + need], log_ratio=outs[2], **common)
+            else:
+                sr.sr_policy_loss(x["logits"], x["targets"], seq_start, x["old_logprob"], x["advantages"], outs[0], ws[4096:4096 + need],
+                                  kl_coef=0.04, reduce="sequences", **common)
+            g.fill_(3.0)
+            assert bool((around == 3.0).all()) and bool((small[gaps] == 5.0).all())
+            assert bool((ws[:4096] == 77).all()) and bool((ws[4096 + need:] == 77).all())
+            assert all(torch.equal(a, b) for a, b in zip(inputs, before))
+
+
+BOUNDS = """
+#include "token_plan.h"
+extern "C" int bound(int row, int n_rows) { return sr::row_bound(row, n_rows); }
+extern "C" int sequence(const int *seq_start, int n_seq, int row) { return sr::sequence_of(seq_start, n_seq, row); }
+"""
+
+
+def test_ranges_of_rows_stay_inside_the_rows(tmp_path):
+    """Starts of every kind: each range of rows lies in [0, rows], each row's sequence is -1 or one of the sequences whatever surrounds
+    the array, and for starts that make sense it is the one that owns the row."""
+    import subprocess
+    from paper_2605_05802_amd.build import CSRC
+    (tmp_path / "bounds.cpp").write_text(BOUNDS)
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I" + CSRC, str(tmp_path / "bounds.cpp"), "-o", str(tmp_path / "bounds.so")])
+    lib, rng, top = ctypes.CDLL(str(tmp_path / "bounds.so")), np.random.default_rng(3), 2 ** 31 - 1
+    for rows, n_seq in ((1, 1), (5, 2), (20, 16), (300, 6), (4096, 1024), (5000, 1500), (1 << 26, 3)):
+        some = sorted({0, 1, rows // 2, rows - 1, *rng.integers(0, rows, 30).tolist()} & set(range(rows)))
+        good = np.sort(rng.integers(0, rows + 1, n_seq + 1))
+        for starts in ([top] * (n_seq + 1), [-top - 1] * (n_seq + 1), rng.integers(-5, rows + 5, n_seq + 1), [rows] + [0] * (n_seq - 1) + [top],
+                       [-3] + [top] * (n_seq - 1) + [rows // 2], [top] + [5] * n_seq, [-rows] * n_seq + [top], [-1] + [rows + 1] * n_seq, good):
+            starts = np.array(starts, dtype=np.int64)
+            assert all(0 <= lib.bound(int(s), rows) <= rows for s in starts)
+            assert [lib.bound(int(s), rows) for s in starts] == np.clip(starts, 0, rows).tolist()
+            answers = []
+            for poison in (-top - 1, top):
+                field = np.full(n_seq + 1 + 2 * (n_seq + 8), poison, dtype=np.int32)
+                field[n_seq + 8:2 * n_seq + 9] = starts
+                at = field.ctypes.data_as(ctypes.POINTER(ctypes.c_int))
+                at = ctypes.cast(ctypes.addressof(at.contents) + 4 * (n_seq + 8), ctypes.POINTER(ctypes.c_int))
+                answers.append([lib.sequence(at, n_seq, r) for r in some])
+            assert answers[0] == answers[1] and all(-1 <= a < n_seq for a in answers[0])
+            if np.array_equal(starts, good):
+                for r, a in zip(some, answers[0]):
+                    inside = (starts[:-1] <= r) & (r < starts[1:])
+                    assert a == (int(inside.argmax()) if inside.any() else -1)
