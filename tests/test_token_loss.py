@@ -943,3 +943,39 @@ def test_ranges_of_rows_stay_inside_the_rows(tmp_path):
                 for r, a in zip(some, answers[0]):
                     inside = (starts[:-1] <= r) & (r < starts[1:])
                     assert a == (int(inside.argmax()) if inside.any() else -1)
+
+
+row_terms_of_any_order = row_terms
+
+
+def tight_row_terms(chain):
+    """row_terms with the error of a row's sum as its kernel adds it up.  Every exponential: the difference, its product with log2(e) and
+    that constant 3.2 u of |x - m| together, however many rescalings that distance is made of, and one unit in the last place; sixteen
+    additions in a group; then `chain` steps (groups of a lane, wavefronts, parts) of an exponential and a sum, 5 u each, and ten
+    additions over lanes.  The distance enters with its mean D over the row's distribution:
+        rel(s) <= u (28 + 5 (chain + 2) + 3.2 D)."""
+    def terms(x, counts):
+        l, p, hot, _, _ = row_terms_of_any_order(x, counts)
+        z = torch.where(counts[:, None], x["logits"].double(), torch.zeros((), dtype=torch.float64, device="cuda"))
+        off = z.gather(1, x["targets"].long()[:, None])[:, 0] - z.max(1).values
+        D = float((p * (z.max(1, keepdim=True).values - z)).sum(1).max())
+        S = U * (28 + 5 * (chain + 2) + 3.2 * D)
+        return l, p, hot, S, S + 2 * U * (off.abs() + (off - l).abs() + 1)
+    return terms
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,rows,n_seq,vocab,chain,pair_chain", [
+    (torch.bfloat16, 400, 4, 152064, 11, 22),  # 20 vectors a thread of 16 wavefronts: 10 groups; 2 parts of 40 vectors: 20
+    (torch.float32, 130, 4, 152064, 13, 13),   # 7 parts of 22 vectors a thread: 6 groups
+    (torch.bfloat16, 5, 2, 152064, 39, 39),    # 37 parts of 3 vectors a thread: 2 groups
+    (torch.float16, 300, 6, 32011, 9, 7),      # 16 vectors a thread of 4 wavefronts: 8 groups; 3 parts of 6 vectors: 4
+    (torch.float32, 64, 8, 1024, 2, 2)])       # 4 vectors a thread of one wavefront: 1 group
+def test_sums_of_wide_rows_keep_single_precision(monkeypatch, dtype, rows, n_seq, vocab, chain, pair_chain):
+    """Log-probabilities, loss and gradient of both losses, with bounds that follow the kernels' own order of additions."""
+    x = make(rows, n_seq, vocab, dtype, 27, masked=0.2)
+    scale = 4096.0 if dtype == torch.float16 else 1.0
+    monkeypatch.setitem(globals(), "row_terms", tight_row_terms(chain))
+    check_policy(x, "tokens", 0.04, scale=scale)
+    monkeypatch.setitem(globals(), "row_terms", tight_row_terms(pair_chain))
+    check_pairs(x, 0.1, 0.1, scale=scale)
