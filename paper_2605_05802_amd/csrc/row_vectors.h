@@ -69,7 +69,6 @@ template <> struct Elem<f16_t> {
 };
 
 template <typename T> __device__ __forceinline__ raw16 load_vec(const T *p) { return *(const raw16_any *)p; }
-template <typename T> __device__ __forceinline__ void store_vec(T *p, raw16 v) { *(raw16_any *)p = v; }
 // the same with the non-temporal hint, for data that the call does not touch again
 template <typename T> __device__ __forceinline__ raw16 load_vec_once(const T *p) { return __builtin_nontemporal_load((const raw16_any *)p); }
 template <typename T> __device__ __forceinline__ void store_vec_once(T *p, raw16 v) { __builtin_nontemporal_store(v, (raw16_any *)p); }
