@@ -378,7 +378,8 @@ int sr_preference_loss(const sr_token_rows *rows, const float *ref_logprob, floa
  * host_tensors: HOST array, read during the call only; the data are device memory, contiguous, any alignment that the type
  * allows.  `out` may be `data` itself or NULL (in place; then nothing is written where scale * c is 1) and must not overlap any
  * tensor otherwise; its type is that of the data, or SR_F32.  sr_grad_norm reads `data` only.
- * workspace: SR_GRAD_NORM_WORKSPACE bytes of device memory, 16-byte aligned.
+ * workspace: SR_GRAD_NORM_WORKSPACE bytes of device memory, 16-byte aligned.  Nothing in it outlives the call, and calls that may
+ * overlap (different streams) need one each; it, `norm` and the tensors share no memory.
  * SR_E_ARG: null pointers, n < 0 or > 2^36, a bad type, scale or max_norm not finite, max_norm < 0.  The list and its tensors may
  * be empty.
  */
@@ -398,7 +399,8 @@ int sr_clip_grad_norm(const sr_tensor *host_tensors, int n_tensors, float scale,
  * The same for a list that stays: sr_plan_tensors copies it to `table` (device memory of the caller, 16-byte aligned,
  * SR_TENSOR_TABLE_BYTES(n_tensors) bytes, kept as long as the plan is used), waits for the stream, and fills *host_plan.  The planned
  * calls then take any number of tensors in one launch a pass, on any stream.  A plan names addresses: it has to be made again when
- * a tensor moves.  Results are those of the calls above but for the order in which the squares are added.
+ * a tensor moves, and a list that moves at every step is cheaper in the arguments of the calls above.  Results are those of the calls
+ * above but for the order in which the squares are added.
  * SR_E_ARG as above; SR_E_LIMIT: more than 2^31 pieces of 8192 elements; SR_E_NOMEM, SR_E_HIP.
  */
 #define SR_TENSOR_TABLE_BYTES(n_tensors) ((size_t)64 + (size_t)24 * (size_t)(n_tensors))

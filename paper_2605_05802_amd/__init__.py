@@ -324,7 +324,8 @@ def sr_preference_loss(logits, targets, seq_start, stats, workspace, *, mask=Non
 class TensorList:
     """The tensors of a norm, as the C boundary takes them; keeps them alive.  To be built again when one of them is replaced.
     plan: copied to the device as well (waits for the current stream); the list is then kept until the last call with it has
-    finished, where that runs on another stream."""
+    finished, where that runs on another stream, and as long as a graph that holds such a call is replayed.
+    Making one takes host time: 27 tensors with outputs 17 us, planned 33; 339 of them 173 and 199."""
 
     def __init__(self, tensors, out=None, plan=False):
         self.tensors, self.out = list(tensors), None if out is None else list(out)

@@ -3,9 +3,9 @@
 // norm = |scale| sqrt(sum g^2), out = scale * min(1, max_norm / norm) * g.  Memory bounds it.  Two passes over the data, because no
 // element may be written before the last one has been read: every gradient is read twice and written once, unless the caches
 // still hold it.  The first pass reads the last kKeepBytes with default loads, which leave them in the memory-side cache, and what
-// comes before with the non-temporal hint, which is faster (2 GB of bf16: 290 us, 7.0 TB/s, against 321) but leaves nothing
+// comes before with the non-temporal hint, which is faster (2 GB of bf16: 296 us, 6.8 TB/s; all with default loads 321) but leaves nothing
 // behind (the second pass over 0.47 GB of bf16 into fp32 took 265 us where all had been read so, and 233 where none had).
-// 2 GB of bf16 into bf16: 290 + 648 us (6.2 TB/s) of 956; the list of a small model: two launches, which cost more than their work.
+// 2 GB of bf16 into bf16: 296 + 636 us (6.4 TB/s) of 941 a call; the list of a small model: two launches, which cost more than their work.
 //
 // A list travels in the kernel arguments, kListTensors tensors a launch: no copy to the device, nothing kept between calls, and a
 // captured launch holds its own list.  A planned list lies on the device, of any length, for one launch a pass: 339 tensors of 20 000
@@ -231,7 +231,8 @@ __device__ __forceinline__ void scale_chunk(const Chunk &k, F &&factor) {
     else scale_some<T, U, false>((const T *)k.data, (U *)k.out, k.n, factor);
 }
 
-// One chunk a workgroup, in the order of the list: 2 GB of bf16 in 657 us, 732 with 1024 workgroups that take chunks in turn
+// One chunk a workgroup, in the order of the list: 2 GB of bf16 in 636 us; where 1024 workgroups took chunks in turn
+// it was 732, and this way 657 then.
 // chunk0: that of the launch's first workgroup
 template <typename List>
 __global__ __launch_bounds__(kNormThreads) void scale_kernel(List l, uint32_t chunk0, const double *__restrict__ slots, int used, float scale,

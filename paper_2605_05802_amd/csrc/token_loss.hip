@@ -17,9 +17,9 @@
 //   logit_grad_kernel    the gradient, from the row, (m, s) and the slope; in passing the pairs added up (pair_sum_kernel without one)
 //
 // Memory bounds all of them but the smallest calls, which are bound by their two or three launches.  4096 rows of 152064 bf16 (2.49 GB
-// read and written): 480 us in policy_resident_kernel, 5.2 TB/s, a large copy's rate; counted reads and writes are those of the
-// data.  2048 such rows without a gradient: 95 us in row_stats_kernel, 6.6 TB/s.  16 pairs of 2400 such rows: 126 us in row_stats_kernel and
-// 215 in logit_grad_kernel (6.8 TB/s with the memory-side cache's share).
+// read and written): 484 us in policy_resident_kernel, 5.1 TB/s, a large copy's rate; counted reads and writes are those of the
+// data.  2048 such rows without a gradient: 95 us in row_stats_kernel, 6.5 TB/s.  16 pairs of 2400 such rows: 126 us in row_stats_kernel and
+// 216 in logit_grad_kernel (6.8 TB/s with the memory-side cache's share).
 //
 // Differences x - m are taken before the multiplication by log2(e): rows whose entries all are the type's lowest
 // value, or that hold -infinity, come out as their definition has it, and the largest entry's exponential is exactly 1.
@@ -1007,7 +1007,7 @@ struct PairRows {
 
 // What pair_kernel, logit_grad_kernel and pair_sum_kernel do, for few rows: every wavefront works out the slope of its row's pair while
 // the row's first vectors are on their way, and one workgroup more, the first, the loss.  203 rows of 1024 fp32 in 8 pairs: 15 us
-// a call with a kernel in between, 12 without; the kernels 3.1 + 7.0 instead of 3.2 + 4.6 + 3.7.
+// a call with a kernel in between, 12 without; the kernels 3.2 + 6.5 instead of 3.2 + 4.6 + 3.7.
 template <typename T, int WAVES>
 __global__ __launch_bounds__(row_block(WAVES)) void pair_grad_kernel(RowArgs a, PairArgs p) {
     constexpr int THREADS = row_block(WAVES), LANES = 64 * WAVES;
