@@ -374,7 +374,7 @@ int sr_preference_loss(const sr_token_rows *rows, const float *ref_logprob, floa
  *     out = scale * c * g
  * norm: device float [1].  Squares are added in double, in a fixed order, so that neither 1e30 nor 1e-30 is lost and
  * the norm is the same bit for bit from call to call.  A norm that is infinite or NaN as it is written (a float: beyond FLT_MAX it is
- * infinite) leaves c = 1: the gradients stay as they were, for the caller who looks at the norm.
+ * infinite) leaves c = 1, out = scale * g: for the caller who looks at the norm.
  * host_tensors: HOST array, read during the call only; the data are device memory, contiguous, any alignment that the type
  * allows.  `out` may be `data` itself or NULL (in place; then nothing is written where scale * c is 1) and must not overlap any
  * tensor otherwise; its type is that of the data, or SR_F32.  sr_grad_norm reads `data` only.

@@ -777,7 +777,7 @@ def test_few_rows_that_do_not_count_cost_no_reading(pairs, rows, n_seq, vocab, d
         r = sr.TokenRows(at(far), at(grad), vocab, vocab, at(x["targets"]), at(mask), at(seq_start), at(lp),
                          {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}[dtype], rows, vocab, n_seq, 1.0, 0)
         times = []
-        for _ in range(6):
+        for _ in range(12):
             a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
             torch.cuda.synchronize()
             a.record()
