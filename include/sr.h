@@ -13,8 +13,9 @@
  *     d_K < d_L (Eq. 2); a cut group stops generating and leaves the batch (Section 3.2,
  *     paragraph "The gate"; Appendix C.1).
  *
- * Behind the rollout it has the losses over the kept trajectories' logits with their gradients, and
- * the clipping of a list of gradients (sr_policy_loss, sr_preference_loss, sr_clip_grad_norm).
+ * Behind the rollout it has the losses over the kept trajectories' logits with their gradients, the
+ * clipping of a list of gradients (sr_policy_loss, sr_preference_loss, sr_clip_grad_norm), and what surrounds
+ * the matrix products of the decoder being trained: embedding, residual + norm and dropout with their gradients.
  *
  * Conventions
  *   - Every function returns SR_OK (0) or a negative sr_status; nothing throws or exits.
@@ -303,7 +304,10 @@ int sr_grpo_loss_static(const double *logprob, const float *rewards, int n_group
  * Outputs overlap neither each other, nor the workspace, nor an input; the gradient alone may lie in the place of the logits.
  * That token_logprob shares nothing with old_logprob and ref_logprob is checked: different workgroups would read and write it.
  */
-typedef enum { SR_F32 = 0, SR_BF16 = 1, SR_F16 = 2 } sr_dtype;
+typedef enum {
+    SR_F32 = 0, SR_BF16 = 1, SR_F16 = 2,
+    SR_E4M3 = 3, SR_E5M2 = 4   /* 8 bits: outputs of sr_add_norm alone (largest finite values 448 and 57344) */
+} sr_dtype;
 
 typedef struct {
     const void *logits;        /* device [n_rows][ld_logits], of type dtype, any alignment that the type allows */
@@ -413,6 +417,119 @@ int sr_plan_tensors(const sr_tensor *host_tensors, int n_tensors, void *table, s
 int sr_planned_grad_norm(const sr_tensor_plan *host_plan, float scale, float *norm, void *workspace, size_t workspace_bytes, void *stream);
 int sr_planned_clip_grad_norm(const sr_tensor_plan *host_plan, float scale, float max_norm, float *norm, void *workspace,
                               size_t workspace_bytes, void *stream);
+
+/*
+ * What surrounds the matrix products of the decoder being trained (sr_model_shape: an embedding, pre-norm blocks, RMSNorm), forward
+ * and backward.  No context needed; the caller brings every buffer.  Rows of any width, at any address their type allows, with any
+ * distance >= width between them; what lies between rows is neither read nor written.  Arithmetic, sums and statistics are in single
+ * precision, every output is rounded once, and results are the same bit for bit from call to call.
+ *
+ * Types: a call has one type T of SR_F32, SR_BF16, SR_F16 and a second one for what is wider, T itself or SR_F32 (a residual in single
+ * precision beside 16-bit branches).  Outputs overlap neither each other, nor an input, nor the workspace, except where a call says that
+ * one may lie in the place of an input: then with the same address, type and row distance.
+ */
+typedef struct {
+    void *data;                /* device [rows][ld]; NULL: not there */
+    int64_t ld;                /* elements from one row to the next, >= width */
+    int32_t dtype;             /* sr_dtype */
+    int32_t reserved;
+} sr_rows;
+
+/*
+ * Rows of a table for a list of tokens:  out[i] = scale * table[tokens[i]].  A token outside the vocabulary (padding) has a row of zeros.
+ * table [vocab][width] of type T, out [n][width] of T or SR_F32; tokens: device int32 [n].
+ * SR_E_ARG: null pointers, bad types, sizes or strides, a scale that is not finite; SR_E_LIMIT: width > 2^20, more than 2^31 - 1 threads.
+ */
+int sr_embed(const sr_rows *table, int vocab, int width, const int32_t *tokens, int n, float scale, const sr_rows *out, void *stream);
+
+/*
+ * Its gradient:  d_table[v] = scale * sum of d_out[i] over all i with tokens[i] = v, zeros for every other v; with accumulate != 0 this is
+ * added to what d_table holds, and rows of tokens that do not occur are not touched.  Sums run over ascending i, in parts of a length that
+ * depends on n and width alone.  d_out [n][width] of type T, d_table [vocab][width] of T or SR_F32.
+ * workspace: device memory, 16-byte aligned, SR_EMBED_GRAD_WORKSPACE(n, width) bytes; nothing in it outlives the call, and calls that
+ * may overlap (different streams) need one each.
+ * SR_E_ARG as above; SR_E_LIMIT: n > 2^20 (a larger batch goes in parts that accumulate), width > 2^20, too many rows for a launch.
+ */
+#define SR_EMBED_GRAD_WORKSPACE(n, width) (65536 + (size_t)32 * (size_t)(n) + ((size_t)(n) / 8 + 64) * 4 * (size_t)(width))
+int sr_embed_grad(const sr_rows *d_out, const int32_t *tokens, int n, float scale, const sr_rows *d_table, int vocab, int width,
+                  int accumulate, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Dropout.  Its mask is a function of numbers and is never stored: element (row r, column c) of a batch of `width` columns is dropped iff
+ *     (bits >> 16 (c % 4)) % 2^16 < round(65536 p),   bits = word (first_row + r) * ceil(width / 4) + c / 4
+ * of the SplitMix64 stream keyed (seed, mask + *step): the same mask forward and backward, whatever the types, strides and the operator,
+ * and whatever part of the rows a call is given (first_row).  What is kept is multiplied by 65536 / (65536 - round(65536 p)), the
+ * reciprocal of the share that these bits keep; what is dropped is 0, also where the input is not finite.
+ * `step` (device, may be NULL) is read when the kernel runs, so that a replayed graph draws another mask at every step.
+ */
+typedef struct {
+    float p;                   /* 0 <= p < 1 */
+    uint32_t reserved;
+    uint64_t seed;
+    uint64_t mask;             /* which mask of that seed: a layer's number, for example */
+    uint64_t first_row;        /* number of the first row */
+    const uint64_t *step;      /* device: added to `mask`; NULL: 0 */
+} sr_mask;
+
+/*
+ * out = dropout(x), or residual + dropout(x).  The backward pass is the same call on the gradient, without the residual.
+ * x [rows][width] of type T; residual (NULL, or data NULL: none) of T or SR_F32; out of the residual's type, or T.  out may lie in the
+ * place of x or of the residual.
+ * SR_E_ARG: null pointers, p outside [0, 1), bad types, sizes or strides; SR_E_LIMIT: width > 2^30, more than 2^31 - 1 threads.
+ */
+int sr_dropout(const sr_rows *x, const sr_rows *residual, const sr_rows *out, int rows, int width, const sr_mask *mask, void *stream);
+
+/*
+ * Residual + branch, and the root-mean-square norm of the sum:
+ *     total = residual + dropout(x), rounded to the residual's type
+ *     rstd = 1 / sqrt(mean over a row of total^2 + eps)          out = total * rstd * gain
+ * The norm is that of the sum as it is stored.  x.data NULL: total = residual.  x.dtype is T in any case.
+ * out of type T, or in 8 bits with scales: for each block of scale_block columns (32, 64 or 128; the last one of a row may be shorter), or
+ * for each row (0), scale = max(largest |out| of the block / largest finite value of the type, 2^-126), and the stored code is out / scale,
+ * rounded to nearest even.  NaN does not enter the scale; its code is NaN.
+ * A row whose squares' sum is beyond single precision has rstd 0.
+ * SR_E_ARG: null pointers (rstd, total and dropout may be NULL), bad types, sizes, strides or options, eps < 0 or not finite;
+ * SR_E_LIMIT: width > 16384, more than 2^32 - 1 threads.  rows may be 0.
+ */
+typedef struct {
+    sr_rows x;                 /* branch [rows][width] of type T, or no data */
+    sr_rows residual;          /* of type T or SR_F32 */
+    sr_rows total;             /* of the residual's type; may lie in its place; no data: not stored */
+    sr_rows out;               /* of type T (may lie in the place of x), SR_E4M3 or SR_E5M2 */
+    const void *gain;          /* device [width], of type T or SR_F32 */
+    float *rstd;               /* device [rows], or NULL */
+    float *scales;             /* device [rows][ceil(width / scale_block)], or [rows] where scale_block is 0; 8-bit outputs only */
+    const sr_mask *dropout;    /* HOST, NULL: none */
+    int32_t gain_dtype, rows, width, scale_block;
+    float eps;
+    int32_t reserved;
+} sr_norm_rows;
+int sr_add_norm(const sr_norm_rows *rows, void *stream);
+
+/*
+ * Its gradients.  With n = total * rstd and g = d_out * gain:
+ *     d_residual = rstd * (g - n * mean over the row of g n) + d_total       d_x = dropout(d_residual)       d_gain = sum over rows of d_out * n
+ * d_total is the gradient that reaches the sum from behind it (no data: none); d_x is formed from d_residual before that is rounded.
+ * d_gain is overwritten, or added to with accumulate != 0.  Any of the three outputs may be left out, not all.  With an 8-bit output d_out is the
+ * gradient of what its codes and scales stand for.
+ * workspace (only with d_gain): device memory, 16-byte aligned, SR_NORM_GRAD_WORKSPACE(rows, width) bytes; nothing in it outlives the
+ * call, and calls that may overlap (different streams) need one each.
+ * Errors as above.  rows may be 0: d_gain is then zeros, or stays.
+ */
+typedef struct {
+    sr_rows d_out;             /* [rows][width] of type T */
+    sr_rows total;             /* as sr_add_norm stored it (without a branch: the residual), of type T or SR_F32 */
+    sr_rows d_total;           /* of total's type, or no data */
+    sr_rows d_residual;        /* of total's type; may lie in the place of d_total; or no data */
+    sr_rows d_x;               /* of type T; may lie in the place of d_out; or no data */
+    const float *rstd;         /* device [rows] */
+    const void *gain;          /* device [width], of type T or SR_F32 */
+    void *d_gain;              /* device [width], of type T or SR_F32, or NULL */
+    const sr_mask *dropout;    /* HOST, NULL: none */
+    int32_t gain_dtype, d_gain_dtype, rows, width, accumulate, reserved;
+} sr_norm_grad_rows;
+#define SR_NORM_GRAD_WORKSPACE(rows, width) ((size_t)((rows) < 2048 ? (rows) : 2048) * 4 * (size_t)(width) + 256)
+int sr_add_norm_grad(const sr_norm_grad_rows *rows, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * The in-group divergence signals of Appendix B at step K, and the gates of Eq. 2 and of

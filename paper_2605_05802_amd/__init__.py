@@ -23,7 +23,8 @@ EXPORTS = ("sr_init", "sr_destroy", "sr_load_weights", "sr_prefill_chunk", "sr_d
            "sr_score_chunk", "sr_get_logprob", "sr_grpo_loss", "sr_finish_sequences", "sr_grpo_loss_static",
            "sr_probe_hbm", "sr_probe_mfma_bf16", "sr_probe_mfma_under_loads", "sr_gate_batch_antidiag",
            "sr_probe_decode_attention", "sr_policy_loss", "sr_preference_loss", "sr_grad_norm", "sr_clip_grad_norm",
-           "sr_plan_tensors", "sr_planned_grad_norm", "sr_planned_clip_grad_norm")
+           "sr_plan_tensors", "sr_planned_grad_norm", "sr_planned_clip_grad_norm", "sr_embed", "sr_embed_grad", "sr_dropout",
+           "sr_add_norm", "sr_add_norm_grad")
 
 # ways to take the mean (sr_reduce)
 REDUCE = {"tokens": 0, "sequences": 1, "sums": 2}
@@ -86,6 +87,28 @@ class TensorPlan(ctypes.Structure):
                 ("reserved", ctypes.c_int32)]
 
 
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("ld", ctypes.c_int64), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class Mask(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_float), ("reserved", ctypes.c_uint32), ("seed", ctypes.c_uint64), ("mask", ctypes.c_uint64),
+                ("first_row", ctypes.c_uint64), ("step", ctypes.c_void_p)]
+
+
+class NormRows(ctypes.Structure):
+    _fields_ = [("x", Rows), ("residual", Rows), ("total", Rows), ("out", Rows), ("gain", ctypes.c_void_p), ("rstd", ctypes.c_void_p),
+                ("scales", ctypes.c_void_p), ("dropout", ctypes.POINTER(Mask)), ("gain_dtype", ctypes.c_int32), ("rows", ctypes.c_int32),
+                ("width", ctypes.c_int32), ("scale_block", ctypes.c_int32), ("eps", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class NormGradRows(ctypes.Structure):
+    _fields_ = [("d_out", Rows), ("total", Rows), ("d_total", Rows), ("d_residual", Rows), ("d_x", Rows), ("rstd", ctypes.c_void_p),
+                ("gain", ctypes.c_void_p), ("d_gain", ctypes.c_void_p), ("dropout", ctypes.POINTER(Mask)), ("gain_dtype", ctypes.c_int32),
+                ("d_gain_dtype", ctypes.c_int32), ("rows", ctypes.c_int32), ("width", ctypes.c_int32), ("accumulate", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
 class KernelTime(ctypes.Structure):
     _fields_ = [("launches", ctypes.c_int64), ("total_ms", ctypes.c_double)]
 
@@ -141,6 +164,12 @@ def lib():
         L.sr_plan_tensors.argtypes = [vp, ci, vp, ctypes.c_size_t, plan, vp]
         L.sr_planned_grad_norm.argtypes = [plan, ctypes.c_float, vp, vp, ctypes.c_size_t, vp]
         L.sr_planned_clip_grad_norm.argtypes = [plan, ctypes.c_float, ctypes.c_float, vp, vp, ctypes.c_size_t, vp]
+        rows = ctypes.POINTER(Rows)
+        L.sr_embed.argtypes = [rows, ci, ci, vp, ci, ctypes.c_float, rows, vp]
+        L.sr_embed_grad.argtypes = [rows, vp, ci, ctypes.c_float, rows, ci, ci, ci, vp, ctypes.c_size_t, vp]
+        L.sr_dropout.argtypes = [rows, rows, rows, ci, ci, ctypes.POINTER(Mask), vp]
+        L.sr_add_norm.argtypes = [ctypes.POINTER(NormRows), vp]
+        L.sr_add_norm_grad.argtypes = [ctypes.POINTER(NormGradRows), vp, ctypes.c_size_t, vp]
         L.sr_finish_sequences.argtypes = [vp, vp, ctypes.POINTER(ci), vp]
         L.sr_set_actions.argtypes = [vp, ci, vp, vp]
         L.sr_get_actions.argtypes = [vp, vp, vp]
@@ -388,6 +417,168 @@ def sr_grad_norm(tensors, norm, workspace, *, scale=1.0, stream=None):
 def sr_clip_grad_norm(tensors, max_norm: float, norm, workspace, *, scale=1.0, stream=None):
     """sr_grad_norm, and the tensors times scale * min(1, max_norm / norm), in place or to the list's outputs."""
     _norm_call(tensors, "clip_grad_norm", (scale, max_norm), norm, workspace, stream)
+
+
+def embed_grad_workspace(n: int, width: int) -> int:
+    """Bytes of workspace for sr_embed_grad (SR_EMBED_GRAD_WORKSPACE)."""
+    return 65536 + 32 * n + (n // 8 + 64) * 4 * width
+
+
+def norm_grad_workspace(rows: int, width: int) -> int:
+    """Bytes of workspace for sr_add_norm_grad (SR_NORM_GRAD_WORKSPACE)."""
+    return min(rows, 2048) * 4 * width + 256
+
+
+_row_types = None
+
+
+def _row_dtypes():
+    """torch's element types of rows -> sr_dtype"""
+    global _row_types
+    if _row_types is None:
+        import torch
+        _row_types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3, torch.float8_e5m2: 4}
+    return _row_types
+
+
+def _rows(where, what, t, shape=None):
+    """A tensor [rows, width] with adjacent columns, as the C boundary takes it; None: no data."""
+    if t is None:
+        return Rows()
+    kind = _row_dtypes().get(t.dtype)
+    size = t.shape
+    if kind is None or len(size) != 2 or (shape is not None and size != shape):
+        raise SrError(SR_E_ARG, f"{where}: {what}: {'[rows, width]' if shape is None else list(shape)} of a floating type expected, "
+                                f"got {t.dtype} {tuple(size)}")
+    ld, each = t.stride()
+    if each != 1 and size[1] > 1:
+        raise SrError(SR_E_ARG, f"{where}: {what}: adjacent columns expected")
+    return Rows(t.data_ptr(), ld if size[0] > 1 else max(ld, size[1]), kind, 0)
+
+
+def _vector(where, what, t, n, kinds):
+    """(address, sr_dtype) of a contiguous tensor of n elements of one of `kinds`; None: no address."""
+    if t is None:
+        return None, 0
+    kind = _row_dtypes().get(t.dtype)
+    if kind not in kinds or t.numel() != n or not t.is_contiguous():
+        raise SrError(SR_E_ARG, f"{where}: {what}: contiguous tensor of {n} elements expected, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr(), kind
+
+
+def _same_device(where, *tensors):
+    """Device tensors, all of the current device: the library launches there."""
+    device = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise SrError(SR_E_ARG, f"{where}: device tensors expected")
+        if device is None:
+            import torch
+            device = torch.cuda.current_device()
+        if t.get_device() != device:
+            raise SrError(SR_E_ARG, f"{where}: tensors of the current device ({device}) expected, got one of {t.get_device()}")
+
+
+def _tokens(where, t):
+    _dtypes()
+    return _of_type(t, "i4", t.numel(), f"{where}: tokens")
+
+
+def sr_embed(table, tokens, out, *, scale=1.0, stream=None):
+    """out[i] = scale * table[tokens[i]], zeros where the token lies outside the table.  table: [vocab, width] of float32, bfloat16 or
+    float16; tokens int32 [n]; out: [n, width] of the table's type or float32."""
+    n = tokens.numel()
+    if table.dim() != 2:
+        raise SrError(SR_E_ARG, "sr_embed: table: [vocab, width] expected")
+    vocab, width = table.shape
+    rows, to = _rows("sr_embed", "table", table), _rows("sr_embed", "out", out, (n, width))
+    _same_device("sr_embed", table, tokens, out)
+    _check(lib().sr_embed(rows, vocab, width, _tokens("sr_embed", tokens), n, scale, to, _stream(stream)), "sr_embed")
+
+
+def sr_embed_grad(d_out, tokens, d_table, workspace, *, scale=1.0, accumulate=False, stream=None):
+    """d_table[v] = scale * sum of d_out[i] over tokens[i] = v, in a fixed order; accumulate: added to what d_table holds, whose other rows are
+    not touched.  d_out: [n, width] of float32, bfloat16 or float16; d_table: [vocab, width] of the same type or float32;
+    workspace: device bytes, embed_grad_workspace(n, width) of them."""
+    n = tokens.numel()
+    if d_table.dim() != 2:
+        raise SrError(SR_E_ARG, "sr_embed_grad: d_table: [vocab, width] expected")
+    vocab, width = d_table.shape
+    rows, to = _rows("sr_embed_grad", "d_out", d_out, (n, width)), _rows("sr_embed_grad", "d_table", d_table)
+    ws, size = _workspace("sr_embed_grad", workspace)
+    _same_device("sr_embed_grad", d_out, tokens, d_table, workspace)
+    _check(lib().sr_embed_grad(rows, _tokens("sr_embed_grad", tokens), n, scale, to, vocab, width, int(accumulate), ws, size,
+                               _stream(stream)), "sr_embed_grad")
+
+
+class Dropout:
+    """Which mask: p, a seed, the number of a mask of that seed (a layer's, for example), and the number of the batch's first row.
+    step: device int64 [1], added to `mask` when the kernel runs, for graphs that are replayed; kept alive by this object."""
+
+    __slots__ = ("c", "step")
+
+    def __init__(self, p: float, seed: int, *, mask: int = 0, first_row: int = 0, step=None):
+        if step is not None:
+            import torch
+            if step.dtype is not torch.int64 or step.numel() != 1 or not step.is_cuda:
+                raise SrError(SR_E_ARG, "Dropout: step: device int64 tensor of one element expected")
+        if not 0.0 <= p < 1.0:
+            raise SrError(SR_E_ARG, f"Dropout: 0 <= p < 1 expected, got {p}")
+        self.step = step
+        self.c = Mask(p, 0, seed, mask, first_row, None if step is None else step.data_ptr())
+
+
+def sr_dropout(x, out, dropout: Dropout, *, residual=None, stream=None):
+    """out = dropout(x), or residual + dropout(x).  x: [rows, width] of float32, bfloat16 or float16; residual: the same type or float32; out: of
+    the residual's type, or x's; may be x or the residual itself.  The backward pass is the same call on the gradient."""
+    if x.dim() != 2:
+        raise SrError(SR_E_ARG, "sr_dropout: x: [rows, width] expected")
+    n, width = shape = x.shape
+    rows, add, to = _rows("sr_dropout", "x", x), _rows("sr_dropout", "residual", residual, shape), _rows("sr_dropout", "out", out, shape)
+    _same_device("sr_dropout", x, residual, out, dropout.step)
+    _check(lib().sr_dropout(rows, add, to, n, width, dropout.c, _stream(stream)), "sr_dropout")
+
+
+def sr_add_norm(residual, gain, out, *, x=None, total=None, rstd=None, scales=None, scale_block=0, dropout=None, eps=1e-6, stream=None):
+    """total = residual + dropout(x) (x None: residual), rstd = 1 / sqrt(mean(total^2) + eps) row by row, out = total * rstd * gain.
+
+    residual, total: [rows, width] of float32, or of the type of x, bfloat16 or float16; out: of x's type, or float8_e4m3fn or float8_e5m2
+    with scales float32 [rows, ceil(width / scale_block)] (scale_block 32, 64, 128) or [rows] (0); gain: [width] of x's type or
+    float32; rstd: float32 [rows].  total may be the residual itself, out may be x."""
+    where = "sr_add_norm"
+    if residual.dim() != 2:
+        raise SrError(SR_E_ARG, f"{where}: residual: [rows, width] expected")
+    n, width = shape = residual.shape
+    a, r, t, o = _rows(where, "x", x, shape), _rows(where, "residual", residual), _rows(where, "total", total, shape), _rows(where, "out", out, shape)
+    g, kind = _vector(where, "gain", gain, width, (0, 1, 2))
+    if x is None:                    # the type of the rest: the output's, where that is no type of 8 bits
+        a.dtype = o.dtype if o.dtype <= 2 else kind or r.dtype
+    blocks = n if scale_block == 0 else n * (-(-width // scale_block)) if scale_block > 0 else -1
+    _same_device(where, residual, gain, out, x, total, rstd, scales, None if dropout is None else dropout.step)
+    args = NormRows(a, r, t, o, g, _vector(where, "rstd", rstd, n, (0,))[0], _vector(where, "scales", scales, blocks, (0,))[0],
+                    None if dropout is None else ctypes.pointer(dropout.c), kind, n, width, scale_block, eps, 0)
+    _check(lib().sr_add_norm(args, _stream(stream)), where)
+
+
+def sr_add_norm_grad(d_out, total, rstd, gain, workspace, *, d_total=None, d_residual=None, d_x=None, d_gain=None, dropout=None,
+                     accumulate=False, stream=None):
+    """The gradients of sr_add_norm: d_residual (total's type; may be d_total itself), d_x (d_out's type; may be d_out itself), d_gain ([width] of
+    d_out's type or float32; accumulate: added to).  Each may be None, not all.  d_total: what reaches the sum from behind it, or None.
+    workspace: device bytes, norm_grad_workspace(rows, width) of them; None where d_gain is."""
+    where = "sr_add_norm_grad"
+    if d_out.dim() != 2:
+        raise SrError(SR_E_ARG, f"{where}: d_out: [rows, width] expected")
+    n, width = shape = d_out.shape
+    g, kind = _vector(where, "gain", gain, width, (0, 1, 2))
+    to, to_kind = _vector(where, "d_gain", d_gain, width, (0, 1, 2))
+    ws, size = _workspace(where, workspace) if workspace is not None else (None, 0)
+    _same_device(where, d_out, total, rstd, gain, workspace, d_total, d_residual, d_x, d_gain, None if dropout is None else dropout.step)
+    args = NormGradRows(_rows(where, "d_out", d_out), _rows(where, "total", total, shape), _rows(where, "d_total", d_total, shape),
+                        _rows(where, "d_residual", d_residual, shape), _rows(where, "d_x", d_x, shape), _vector(where, "rstd", rstd, n, (0,))[0], g, to,
+                        None if dropout is None else ctypes.pointer(dropout.c), kind, to_kind, n, width, int(accumulate), 0)
+    _check(lib().sr_add_norm_grad(args, ws, size, _stream(stream)), where)
 
 
 def sr_probe_hbm(src, dst, mode: int, iters: int = 10, stream=None) -> float:

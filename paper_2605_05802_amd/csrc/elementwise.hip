@@ -3,6 +3,7 @@
 // the row index or on the batch size.  (K splits and attention splits do depend on the batch size, and so does the order in which a
 // norm that is finished behind the next projection adds up its squares: see RowSquares.  Rows of one batch are treated alike everywhere.)
 #include "epilogue.h"
+#include "splitmix.h"
 
 namespace sr {
 namespace {
@@ -182,12 +183,6 @@ __device__ __forceinline__ MaxIdx better(MaxIdx a, MaxIdx b) {
     return (b.v > a.v || (b.v == a.v && b.i < a.i)) ? b : a;
 }
 
-__device__ __forceinline__ uint64_t smx_finalize(uint64_t z) {
-    z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ULL;
-    z = (z ^ (z >> 27)) * 0x94D049BB133111EBULL;
-    return z ^ (z >> 31);
-}
-
 // One 1024-thread block per row: strided scan, wavefront shuffle reduction, then 16 wave results.
 // With inv_temperature > 0 every logit is scaled and perturbed by a standard Gumbel variate drawn from a
 // counter-based SplitMix64 stream keyed (seed, original sequence id, position), counter = vocabulary
@@ -203,11 +198,9 @@ __global__ __launch_bounds__(1024) void argmax_kernel(const float *__restrict__ 
     MaxIdx best{-INFINITY, 0x7FFFFFFF};
     const int nvec = vocab >> 2;
     if (inv_temperature > 0.f) {
-        const uint64_t golden = 0x9E3779B97F4A7C15ULL;
-        const uint64_t stream = ((uint64_t)(uint32_t)orig_seq[r] << 32) | (uint32_t)pos;
-        const uint64_t key = smx_finalize(smx_finalize(seed + golden) ^ (stream * 0xD1342543DE82EF95ULL + 1ULL));
+        const uint64_t key = smx_key(seed, ((uint64_t)(uint32_t)orig_seq[r] << 32) | (uint32_t)pos);
         for (int v = threadIdx.x; v < vocab; v += 1024) {
-            const uint64_t rnd = smx_finalize(key + ((uint64_t)v + 1ULL) * golden);
+            const uint64_t rnd = smx_finalize(key + ((uint64_t)v + 1ULL) * kGolden);
             const float u = ((float)(uint32_t)(rnd >> 41) + 0.5f) * (1.0f / 8388608.0f);
             best = better(best, MaxIdx{row[v] * inv_temperature - logf(-logf(u)), v});
         }
