@@ -4,10 +4,11 @@
 // the sums are the same bit for bit from call to call.  Tokens outside the vocabulary have a row of zeros and no gradient.
 // Memory bounds both; of a whole table's gradient most is zeros to write.
 //
-// The gradient sorts (token, i) by counting, for every i, how many come before it.  The sorted list is cut into chunks of equal length whatever
+// The gradient sorts (token, i) by counting, for every i, how many come before it: within a tile of kTile by comparing with all of them, in the
+// other tiles, once those are sorted, by bisection.  The sorted list is cut into chunks of equal length whatever
 // tokens they hold, so that a token of half the batch is as well spread as any: a wavefront adds up a chunk's rows, 64 vectors of columns, and
-// writes the sums of the tokens that lie in its chunk alone; sums of tokens that reach over an end go to the workspace, and a second kernel
-// adds those up, chunk by chunk.
+// writes the sums of the tokens that lie in its chunk alone.  Sums of tokens that reach over an end are joined in LDS by the workgroup that has
+// four chunks next to each other, and those that reach over its ends by a second kernel, by way of the workspace.
 #include <cmath>
 
 #include "row_ops.h"
@@ -74,8 +75,9 @@ int launch_embed(EmbedArgs a, hipStream_t stream) {
 // ---------------------------------------------------------------------------------------------
 // gradient
 // ---------------------------------------------------------------------------------------------
-constexpr uint32_t kNoToken = 0xffffffffu;           // sorts behind every token
-constexpr int kZeroRows = 32;                        // of the table, a workgroup
+constexpr uint32_t kNoToken = 0x80000000u;           // sorts behind every token
+constexpr uint32_t kBehindAll = 0xffffffffu;         // and this behind it
+constexpr int kTile = 4096;                          // tokens that are sorted by comparing all with all
 
 struct EmbedGradArgs {
     const void *d_out;
@@ -84,36 +86,96 @@ struct EmbedGradArgs {
     int64_t ld_d_out, ld_d_table;
     uint32_t *sorted;                // [n] tokens in order, those outside the vocabulary behind them as kNoToken
     int32_t *places;                 // [n] and where they came from
-    float *parts;                    // [chunks][2][width]: sums of the token that comes in from the chunk before, and of the one that goes on
-    int n, vocab, width, chunk, chunks, slices, sum_blocks;
+    uint32_t *tile_sorted;           // the same of every tile by itself, where there are several
+    int32_t *tile_places;
+    float *parts;                    // [spans][2][width]: sums of the token that comes in from the span before, and of the one that goes on
+    int n, vocab, width, chunk, spans, slices, sum_blocks;
+    int zero_rows;                   // of the table, a wavefront that writes zeros
+
     int accumulate;
     float scale;
 };
 
+__device__ __forceinline__ int round_up_4(int n) { return (n + 3) & ~3; }
 __device__ __forceinline__ uint32_t key_of(int token, int vocab) { return (unsigned)token < (unsigned)vocab ? (uint32_t)token : kNoToken; }
 
-// 64 places a workgroup; each wavefront compares them with a sixteenth of the list, which comes through scalar loads
-__global__ __launch_bounds__(1024) void rank_kernel(EmbedGradArgs a) {
-    __shared__ int s_rank[16][64];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int first = (int)blockIdx.x * 64, i = first + lane;
-    const uint32_t key = i < a.n ? key_of(a.tokens[i], a.vocab) : kNoToken;
-    const int each = (a.n + 15) / 16, from = min(wave * each, a.n), to = min(from + each, a.n);
-    int rank = 0;
-    // before the workgroup's places: as many as are not greater; among them: by place; behind them: as many as are less
-    int j = from;
-    for (const int end = min(to, first); j < end; ++j) rank += key_of(read_uniform(a.tokens + j), a.vocab) <= key;
-    for (const int end = min(to, first + 64); j < end; ++j) {
-        const uint32_t other = key_of(read_uniform(a.tokens + j), a.vocab);
-        rank += other < key || (other == key && j < i);
+// Sixteen places a workgroup; each of sixteen groups of lanes compares them with a sixteenth of their tile, which lies in LDS
+constexpr int kRankKeys = 16, kRankGroups = 16;
+__global__ __launch_bounds__(256) void rank_kernel(EmbedGradArgs a, uint32_t *__restrict__ sorted, int32_t *__restrict__ places) {
+    __shared__ __align__(16) uint32_t s_key[kTile + 64 * 4];         // four words more after every 64: groups read different banks
+    __shared__ int s_rank[4][kRankKeys];
+    const int first = (int)blockIdx.x * kRankKeys, begin = first / kTile * kTile, size = min(kTile, a.n - begin);
+    const int each = round_up_4((size + kRankGroups - 1) / kRankGroups);     // of a group
+    auto slot = [](int j) __attribute__((always_inline)) { return j + (j >> 6) * 4; };
+    for (int j0 = threadIdx.x; j0 < each * kRankGroups; j0 += 256 * 8) {     // eight loads before the first is waited for
+        int token[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) token[u] = a.tokens[begin + min(j0 + 256 * u, size - 1)];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int j = j0 + 256 * u;
+            if (j < each * kRankGroups) s_key[slot(j)] = j < size ? key_of(token[u], a.vocab) : kBehindAll;
+        }
     }
-    for (; j < to; ++j) rank += key_of(read_uniform(a.tokens + j), a.vocab) < key;
-    s_rank[wave][lane] = rank;
     __syncthreads();
-    if (wave != 0 || i >= a.n) return;
-    for (int w = 1; w < 16; ++w) rank += s_rank[w][lane];
+    const int mine = first - begin + (int)(threadIdx.x % kRankKeys), group = (int)threadIdx.x / kRankKeys;
+    const uint32_t key = s_key[slot(min(mine, size - 1))];
+    int rank = 0;
+    // before the workgroup's places: those that are not greater; from there on: those that are less, and of its own the equal ones before
+#pragma unroll 4
+    for (int j = group * each; j < (group + 1) * each; j += 4) {
+        const raw16 other = *(const raw16 *)(s_key + slot(j));
+        const uint32_t limit = key + (j < first - begin);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) rank += other[u] < limit;
+    }
+    if (first - begin + group < mine) rank += s_key[slot(first - begin + group)] == key;
+    rank += __shfl_xor(rank, 16, 64);
+    rank += __shfl_xor(rank, 32, 64);
+    if ((threadIdx.x & 63) < kRankKeys) s_rank[threadIdx.x >> 6][threadIdx.x & 63] = rank;
+    __syncthreads();
+    if (threadIdx.x >= kRankKeys || mine >= size) return;
+    rank = s_rank[0][threadIdx.x] + s_rank[1][threadIdx.x] + s_rank[2][threadIdx.x] + s_rank[3][threadIdx.x];
+    sorted[begin + rank] = key;
+    places[begin + rank] = begin + mine;
+}
+
+// Sorted tiles into one sorted list: a key comes behind what is not greater in the tiles before its own, and what is less in those behind it.
+// Searches by quarters in kTogether tiles at a time, whose loads do not wait for each other.
+constexpr int kTogether = 8;
+__global__ __launch_bounds__(256) void merge_kernel(EmbedGradArgs a, const uint32_t *__restrict__ tiles, const int32_t *__restrict__ from) {
+    const int i = (int)(blockIdx.x * 256 + threadIdx.x);
+    if (i >= a.n) return;
+    const uint32_t key = tiles[i];
+    const int own = i / kTile, n_tiles = (a.n + kTile - 1) / kTile;
+    int rank = i - own * kTile;
+    for (int t0 = 0; t0 < n_tiles; t0 += kTogether) {
+        int at[kTogether];                           // this many of the tile come before
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) at[u] = 0;
+        for (int step = kTile / 4; step > 0; step >>= 2) {
+            uint32_t other[kTogether][3];
+#pragma unroll
+            for (int u = 0; u < kTogether; ++u)
+#pragma unroll
+                for (int q = 0; q < 3; ++q) other[u][q] = tiles[min((t0 + u) * kTile + at[u] + (q + 1) * step - 1, a.n - 1)];
+#pragma unroll
+            for (int u = 0; u < kTogether; ++u) {
+                const int base = (t0 + u) * kTile + at[u] + step - 1;
+                const uint32_t limit = key + (t0 + u < own);
+#pragma unroll
+                for (int q = 0; q < 3; ++q) at[u] += base + q * step < a.n && other[u][q] < limit ? step : 0;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) {        // the steps reach kTile - 1 of them
+            const int probe = (t0 + u) * kTile + at[u];
+            at[u] += probe < a.n && tiles[min(probe, a.n - 1)] < key + (t0 + u < own);
+            if (t0 + u != own && t0 + u < n_tiles) rank += at[u];
+        }
+    }
     a.sorted[rank] = key;
-    a.places[rank] = i;
+    a.places[rank] = from[i];
 }
 
 // First place of the sorted list whose token is not below `token`; the wavefront asks at 64 places at a time
@@ -147,148 +209,203 @@ __device__ __forceinline__ void write_row(const EmbedGradArgs &a, uint32_t token
     store_span<N>(row, s, y);
 }
 
-// The first sum_blocks workgroups add up chunks, a wavefront a chunk and slice of columns; the others write the zeros of a whole table
+// The first sum_blocks workgroups add up spans of chunks, a wavefront a chunk and slice of columns; the others write the zeros of a whole table
 template <typename T, typename O, int N>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     if ((int)blockIdx.x >= a.sum_blocks) {
-        __shared__ uint32_t s_named;
-        const uint32_t from = (uint32_t)((int)blockIdx.x - a.sum_blocks) * kZeroRows;
-        const uint32_t to = min(from + kZeroRows, (uint32_t)a.vocab);
-        if (wave == 0) {
-            uint32_t named = 0;
-            // one token after the other: the first that is not below the next one
-            for (uint32_t next = from; next < to;) {
-                const int at = first_at_least(a.sorted, a.n, next, lane);
-                const uint32_t token = at < a.n ? read_uniform(a.sorted + at) : kNoToken;
-                if (token >= to) break;
-                named |= 1u << (token - from);
-                next = token + 1;
-            }
-            if (lane == 0) s_named = named;
+        __shared__ uint32_t s_named[4];
+        const int64_t first = ((int64_t)((int)blockIdx.x - a.sum_blocks) * 4 + wave) * a.zero_rows;
+        if (first >= a.vocab) return;
+        const uint32_t from = (uint32_t)first, to = min(from + (uint32_t)a.zero_rows, (uint32_t)a.vocab);
+        if (lane == 0) s_named[wave] = 0;
+        // 64 places of the list at a time, then those behind the last token seen
+        for (uint32_t next = from;;) {
+            const int at = first_at_least(a.sorted, a.n, next, lane) + lane;
+            const uint32_t token = at < a.n ? a.sorted[at] : kNoToken;
+            if (token < to) atomicOr(&s_named[wave], 1u << (token - from));
+            next = __builtin_amdgcn_readlane(token, 63) + 1;
+            if (next >= to) break;                   // kNoToken among them
         }
-        __syncthreads();
-        const uint32_t named = s_named;
+        const uint32_t named = __builtin_amdgcn_readfirstlane(*(volatile uint32_t *)&s_named[wave]);
         const float zero[N] = {};
         const int vecs = (a.width + N - 1) / N;
         for (uint32_t r = from; r < to; ++r) {
             if (named >> (r - from) & 1) continue;
-            for (int v = threadIdx.x; v < vecs; v += 256) store_span<N>((O *)a.d_table + r * a.ld_d_table, span_of<N>(v, a.width), zero);
+            O *row = (O *)a.d_table + r * a.ld_d_table;
+            for (int v = lane; v < vecs; v += 64) store_span<N>(row, span_of<N>(v, a.width), zero);
         }
         return;
     }
-    const int unit = (int)blockIdx.x * 4 + wave, k = unit / a.slices;
-    if (k >= a.chunks) return;
-    const Span s = span_of<N>((unit - k * a.slices) * 64 + lane, a.width);
-    const int from = k * a.chunk, to = min(from + a.chunk, a.n);
-    const uint32_t before = from > 0 ? read_uniform(a.sorted + from - 1) : kNoToken, behind = to < a.n ? read_uniform(a.sorted + to) : kNoToken;
-    uint32_t token = read_uniform(a.sorted + from);
-    if (token == kNoToken) return;
-    bool comes_in = from > 0 && before == token;
-    float sum[N];
+    __shared__ float s_sum[kSpanChunks][2][N][64];
+    __shared__ uint32_t s_token[kSpanChunks];
+    __shared__ int s_kind[kSpanChunks];
+    const int span = (int)blockIdx.x / a.slices, slice = (int)blockIdx.x - span * a.slices;
+    const Span s = span_of<N>(slice * 64 + lane, a.width);
+    const int from = (span * kSpanChunks + wave) * a.chunk, to = min(from + a.chunk, a.n);
+    // what becomes of the chunk's first and last sum: kHead, it comes in from before; kTail, a later one goes on behind the chunk;
+    // kThrough, the one that comes in goes on
+    enum { kHead = 1, kTail = 2, kThrough = 4 };
+    int kind = 0;
+    uint32_t token = from < to ? read_uniform(a.sorted + from) : kNoToken;
+    if (token != kNoToken) {
+        const uint32_t before = from > 0 ? read_uniform(a.sorted + from - 1) : kNoToken, behind = to < a.n ? read_uniform(a.sorted + to) : kNoToken;
+        bool comes_in = before == token;
+        float sum[N];
+        auto keep = [&](int which) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) sum[j] = 0.f;
-    for (int e0 = from; e0 < to; e0 += 64) {
-        const int e = min(e0 + lane, to - 1);
-        const uint32_t key = a.sorted[e];
-        const int place = a.places[e];
-        const int count = __popcll(__ballot(e0 + lane < to && key != kNoToken));
-        for (int g = 0; g < count; g += 8) {
-            Part<T, N> x[8];
+            for (int j = 0; j < N; ++j) s_sum[wave][which][j][lane] = sum[j];
+        };
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
-                x[u].load((const T *)a.d_out + __builtin_amdgcn_readlane(place, min(g + u, count - 1)) * a.ld_d_out + s.c);
+        for (int j = 0; j < N; ++j) sum[j] = 0.f;
+        for (int e0 = from; e0 < to; e0 += 64) {
+            const int e = min(e0 + lane, to - 1);
+            const uint32_t key = a.sorted[e];
+            const int place = a.places[e];
+            const int count = __popcll(__ballot(e0 + lane < to && key != kNoToken));
+            for (int g = 0; g < count; g += 8) {
+                Part<T, N> x[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                if (g + u >= count) break;
-                const uint32_t t = __builtin_amdgcn_readlane(key, g + u);
-                if (t != token) {
-                    if (comes_in) store_span<N>(a.parts + (size_t)(2 * k) * a.width, s, sum);
-                    else write_row<N, O>(a, token, s, sum);
-                    comes_in = false;
-                    token = t;
+                for (int u = 0; u < 8; ++u)
+                    x[u].load((const T *)a.d_out + __builtin_amdgcn_readlane(place, min(g + u, count - 1)) * a.ld_d_out + s.c);
 #pragma unroll
-                    for (int j = 0; j < N; ++j) sum[j] = 0.f;
+                for (int u = 0; u < 8; ++u) {
+                    if (g + u >= count) break;
+                    const uint32_t t = __builtin_amdgcn_readlane(key, g + u);
+                    if (t != token) {
+                        if (comes_in) {
+                            keep(0);
+                            kind = kHead;
+                        } else write_row<N, O>(a, token, s, sum);
+                        comes_in = false;
+                        token = t;
+#pragma unroll
+                        for (int j = 0; j < N; ++j) sum[j] = 0.f;
+                    }
+                    float y[N];
+                    x[u].widen(y);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) sum[j] += y[j];
                 }
-                float y[N];
-                x[u].widen(y);
+            }
+            if (count < 64) break;
+        }
+        const bool goes_on = behind == token;
+        if (comes_in) {
+            keep(0);
+            kind = goes_on ? kHead | kThrough : kHead;
+        } else if (goes_on) {
+            keep(1);
+            kind |= kTail;
+        } else write_row<N, O>(a, token, s, sum);
+    }
+    if (lane == 0) {
+        s_kind[wave] = kind;
+        s_token[wave] = token;                       // of a tail
+    }
+    __syncthreads();
+    if (wave) return;
+    // the sums that reach over the ends of chunks, in order: those of one span end here
+    float open[N];
+    bool outside = false, any = false;
+    uint32_t open_token = kNoToken;
+    float *parts = a.parts + (size_t)(2 * span) * a.width;
+    for (int w = 0; w < kSpanChunks; ++w) {
+        const int k = __builtin_amdgcn_readfirstlane(s_kind[w]);
+        if (k & kHead) {
+            if (w == 0) outside = true;
 #pragma unroll
-                for (int j = 0; j < N; ++j) sum[j] += y[j];
+            for (int j = 0; j < N; ++j) open[j] = w == 0 ? s_sum[w][0][j][lane] : open[j] + s_sum[w][0][j][lane];
+            any = true;
+            if (!(k & kThrough)) {
+                if (outside) store_span<N>(parts, s, open);
+                else write_row<N, O>(a, open_token, s, open);
+                any = outside = false;
             }
         }
-        if (count < 64) break;
+        if (k & kTail) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) open[j] = s_sum[w][1][j][lane];
+            any = true;
+            open_token = __builtin_amdgcn_readfirstlane(s_token[w]);
+        }
     }
-    const bool goes_on = behind == token;
-    if (comes_in) store_span<N>(a.parts + (size_t)(2 * k) * a.width, s, sum);
-    else if (goes_on) store_span<N>(a.parts + (size_t)(2 * k + 1) * a.width, s, sum);
-    else write_row<N, O>(a, token, s, sum);
+    if (any) store_span<N>(outside ? parts : parts + a.width, s, open);
 }
 
-// Tokens that reach over the ends of chunks: the workgroup of the chunk that one begins in adds up its parts, each wavefront a run of them
+// Tokens that reach over the ends of spans: the workgroup of the span that one begins in adds up its parts, each wavefront a run of them
+constexpr int kJoinWaves = 4;
 template <typename O, int N>
-__global__ __launch_bounds__(256) void embed_join_kernel(EmbedGradArgs a) {
-    __shared__ float s_sum[3][64][N];
+__global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(EmbedGradArgs a) {
+    __shared__ float s_sum[kJoinWaves][N][64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int k = (int)blockIdx.x / a.slices, slice = (int)blockIdx.x - k * a.slices;
-    const int from = k * a.chunk, to = from + a.chunk;               // not the last chunk: to < n
-    const uint32_t token = read_uniform(a.sorted + to);
-    if (token == kNoToken || read_uniform(a.sorted + to - 1) != token) return;
-    if (from > 0 && read_uniform(a.sorted + from) == token && read_uniform(a.sorted + from - 1) == token) return;
-    // chunks behind this one that begin with the token
+    const int length = kSpanChunks * a.chunk, from = k * length, to = from + length;         // not the last span: to < n
+    // asked for together: most workgroups end here
+    const uint32_t token = read_uniform(a.sorted + to), last = read_uniform(a.sorted + to - 1), start = read_uniform(a.sorted + from);
+    const uint32_t before = read_uniform(a.sorted + max(from - 1, 0));
+    if ((token == kNoToken) | (last != token) | ((from > 0) & (start == token) & (before == token))) return;
+    // spans behind this one that begin with the token
     int more = 0;
     for (;;) {
         const int next = k + 1 + more + lane;
-        const uint64_t same = __ballot(next < a.chunks && a.sorted[min(next, a.chunks - 1) * a.chunk] == token);
+        const uint64_t same = __ballot(next < a.spans && a.sorted[min(next, a.spans - 1) * length] == token);
         const int run = ~same ? __ffsll((unsigned long long)~same) - 1 : 64;
         more += run;
         if (run < 64) break;
     }
     const Span s = span_of<N>(slice * 64 + lane, a.width);
-    // parts 0 .. more: this chunk's second, the first of those behind it
-    const int each = (more + 4) / 4, begin = min(wave * each, more + 1), end = min(begin + each, more + 1);
+    // parts 0 .. more: this span's second, the first of those behind it
+    const int each = (more + kJoinWaves) / kJoinWaves, begin = min(wave * each, more + 1), end = min(begin + each, more + 1);
     float sum[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) sum[j] = 0.f;
-    for (int p = begin; p < end; p += 4) {
-        Part<float, N> x[4];
+    for (int p = begin; p < end; p += 16) {
+        Part<float, N> x[16];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < 16; ++u) {
             const int q = min(p + u, end - 1);
             x[u].load(a.parts + (size_t)(2 * (k + q) + (q == 0)) * a.width + s.c);
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < 16; ++u) {
             float y[N];
             x[u].widen(y);
 #pragma unroll
             for (int j = 0; j < N; ++j) sum[j] += p + u < end ? y[j] : 0.f;
         }
     }
-    if (wave) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) s_sum[wave - 1][lane][j] = sum[j];
-    }
+    for (int j = 0; j < N; ++j) s_sum[wave][j][lane] = sum[j];
     __syncthreads();
     if (wave) return;
-    for (int w = 0; w < 3; ++w)
+    const int used = min(kJoinWaves, (more + each) / each);
+    for (int w = 1; w < used; ++w)
 #pragma unroll
-        for (int j = 0; j < N; ++j) sum[j] += s_sum[w][lane][j];
+        for (int j = 0; j < N; ++j) sum[j] += s_sum[w][j][lane];
     write_row<N, O>(a, token, s, sum);
 }
 
 template <typename T, typename O, int N>
 int launch_embed_grad(EmbedGradArgs a, hipStream_t stream) {
     if (a.n > 0) {
-        rank_kernel<<<dim3(ceil_div(a.n, 64)), dim3(1024), 0, stream>>>(a);
+        const bool tiles = a.n > kTile;
+        uint32_t *sorted = tiles ? a.tile_sorted : a.sorted;
+        int32_t *places = tiles ? a.tile_places : a.places;
+        rank_kernel<<<dim3(ceil_div(a.n, kRankKeys)), dim3(256), 0, stream>>>(a, sorted, places);
         SR_HIP(hipGetLastError());
+        if (tiles) {
+            merge_kernel<<<dim3(ceil_div(a.n, 256)), dim3(256), 0, stream>>>(a, sorted, places);
+            SR_HIP(hipGetLastError());
+        }
     }
-    a.sum_blocks = ceil_div(a.chunks * a.slices, 4);
-    const int zero_blocks = a.accumulate ? 0 : (int)(((int64_t)a.vocab + kZeroRows - 1) / kZeroRows);
+    a.sum_blocks = a.spans * a.slices;
+    const int zero_blocks = a.accumulate ? 0 : ceil_div(ceil_div(a.vocab, a.zero_rows), 4);
     if (a.sum_blocks + zero_blocks == 0) return SR_OK;
     embed_sum_kernel<T, O, N><<<dim3((unsigned)a.sum_blocks + (unsigned)zero_blocks), dim3(256), 0, stream>>>(a);
     SR_HIP(hipGetLastError());
-    if (a.chunks > 1) {
-        embed_join_kernel<O, N><<<dim3((unsigned)((a.chunks - 1) * a.slices)), dim3(256), 0, stream>>>(a);
+    if (a.spans > 1) {
+        embed_join_kernel<O, N><<<dim3((unsigned)((a.spans - 1) * a.slices)), dim3(64 * kJoinWaves), 0, stream>>>(a);
         SR_HIP(hipGetLastError());
     }
     return SR_OK;
@@ -302,9 +419,8 @@ int embed_grad(const sr_rows *d_out, const int32_t *tokens, int n, float scale, 
     if (!rows_fit(*d_table, width, SR_F16) || (n > 0 && (!rows_fit(*d_out, width, SR_F16) || !tokens || (uintptr_t)tokens % 4))) return SR_E_ARG;
     if (n > 0 && d_table->data == d_out->data) return SR_E_ARG;
     if (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < SR_EMBED_GRAD_WORKSPACE(n, width)) return SR_E_ARG;
-    if (!accumulate && (int64_t)vocab / kZeroRows + 1 > INT32_MAX / 512) return SR_E_LIMIT;
-    const EmbedGradPlan p = embed_grad_plan(n, width, d_out->dtype == SR_F32 || d_table->dtype == SR_F32);
-    if ((int64_t)p.chunks * p.slices > INT32_MAX / 512) return SR_E_LIMIT;
+    const EmbedGradPlan p = embed_grad_plan(n, width, d_out->dtype == SR_F32 || d_table->dtype == SR_F32, elem_bytes(d_table->dtype));
+    if ((int64_t)p.spans * p.slices > INT32_MAX / 256 || vocab / p.zero_rows > INT32_MAX / 128) return SR_E_LIMIT;
     EmbedGradArgs a{};
     a.d_out = d_out->data;
     a.ld_d_out = d_out->ld;
@@ -313,13 +429,16 @@ int embed_grad(const sr_rows *d_out, const int32_t *tokens, int n, float scale, 
     a.tokens = tokens;
     a.sorted = (uint32_t *)workspace;
     a.places = (int32_t *)workspace + n;
-    a.parts = (float *)((char *)workspace + round_up(8 * n, 16));
+    a.tile_sorted = (uint32_t *)workspace + 2 * (size_t)n;
+    a.tile_places = (int32_t *)workspace + 3 * (size_t)n;
+    a.parts = (float *)((char *)workspace + 16 * (size_t)n);
     a.n = n;
     a.vocab = vocab;
     a.width = width;
     a.chunk = p.chunk;
-    a.chunks = p.chunks;
+    a.spans = p.spans;
     a.slices = p.slices;
+    a.zero_rows = p.zero_rows;
     a.accumulate = accumulate != 0;
     a.scale = scale;
     return with_row_types(d_out->dtype, d_table->dtype, [&](auto *t, auto *o) -> int {

@@ -37,18 +37,23 @@ inline int norm_grad_parts(int rows, const RowShape &s) {
     return rows < parts ? rows : parts;
 }
 
-// The gradient of an embedding: sorted tokens in chunks of `chunk`, a wavefront for 64 * per_vec columns of each
+// The gradient of an embedding: sorted tokens in spans of kSpanChunks chunks of `chunk`, a wavefront for 64 * per_vec columns of each
+// chunk, a workgroup for those of a span
+constexpr int kSpanChunks = 4;
 constexpr int kMostTokens = 1 << 20;
 struct EmbedGradPlan {
-    int per_vec, slices, chunk, chunks;
+    int per_vec, slices, chunk, spans;
+    int zero_rows;           // rows of zeros of a wavefront: about 8 KB of them, and at most 32
 };
-inline EmbedGradPlan embed_grad_plan(int n, int width, bool single) {
+inline EmbedGradPlan embed_grad_plan(int n, int width, bool single, int table_bytes) {
     EmbedGradPlan p{};
     p.per_vec = row_vec(width, single);
     p.slices = ceil_div(ceil_div(width, p.per_vec), 64);
     const int64_t want = ((int64_t)n * p.slices + 8191) / 8192;
     p.chunk = want <= 16 ? 16 : round_up((int)(want < n ? want : n), 16);
-    p.chunks = ceil_div(n, p.chunk);
+    p.spans = ceil_div(n, kSpanChunks * p.chunk);
+    const int rows = 8192 / (table_bytes * (width < 8192 ? width : 8192));
+    p.zero_rows = rows < 1 ? 1 : rows > 32 ? 32 : rows;
     return p;
 }
 
