@@ -429,73 +429,87 @@ def norm_grad_workspace(rows: int, width: int) -> int:
     return min(rows, 2048) * 4 * width + 256
 
 
-_row_types = None
+_row_types = _torch_c = None
+_row_calls = {}
 
 
 def _row_dtypes():
     """torch's element types of rows -> sr_dtype"""
-    global _row_types
+    global _row_types, _torch_c
     if _row_types is None:
         import torch
+        _dtypes()
+        _torch_c = torch._C
         _row_types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3, torch.float8_e5m2: 4}
     return _row_types
 
 
-def _rows(where, what, t, shape=None):
-    """A tensor [rows, width] with adjacent columns, as the C boundary takes it; None: no data."""
+def _row_call(name):
+    """An entry point that takes its structures as packed bytes: structures of ctypes cost a call of five tensors 4 us more."""
+    call = _row_calls.get(name)
+    if call is None:
+        call = lib()[name]           # a function object of its own, apart from the one with typed pointers
+        call.argtypes = [ctypes.c_void_p if issubclass(t, ctypes._Pointer) else t for t in getattr(lib(), name).argtypes]
+        call.restype = ctypes.c_int
+        _row_calls[name] = call
+    return call
+
+
+_NO_ROWS = (0, 0, 0, 0)              # sr_rows without data
+_pack_rows = struct.Struct("Pqii").pack
+_pack_norm = struct.Struct("Pqii" * 4 + "PPPPiiiifi").pack
+_pack_norm_grad = struct.Struct("Pqii" * 5 + "PPPPiiiiii").pack
+
+
+def _rows(where, what, t, shape):
+    """The fields of sr_rows for a tensor [rows, width] with adjacent columns; None: no data."""
     if t is None:
-        return Rows()
-    kind = _row_dtypes().get(t.dtype)
-    size = t.shape
-    if kind is None or len(size) != 2 or (shape is not None and size != shape):
-        raise SrError(SR_E_ARG, f"{where}: {what}: {'[rows, width]' if shape is None else list(shape)} of a floating type expected, "
-                                f"got {t.dtype} {tuple(size)}")
+        return _NO_ROWS
+    kind, size = _row_dtypes().get(t.dtype), t.shape
+    if kind is None or size != shape:
+        raise SrError(SR_E_ARG, f"{where}: {what}: {list(shape)} of a floating type expected, got {t.dtype} {tuple(size)}")
     ld, each = t.stride()
     if each != 1 and size[1] > 1:
         raise SrError(SR_E_ARG, f"{where}: {what}: adjacent columns expected")
-    return Rows(t.data_ptr(), ld if size[0] > 1 else max(ld, size[1]), kind, 0)
+    return t.data_ptr(), ld if size[0] > 1 else max(ld, size[1]), kind, 0
+
+
+def _matrix(where, what, t):
+    if t.dim() != 2:
+        raise SrError(SR_E_ARG, f"{where}: {what}: two dimensions expected, got {tuple(t.shape)}")
+    return t.shape
 
 
 def _vector(where, what, t, n, kinds):
     """(address, sr_dtype) of a contiguous tensor of n elements of one of `kinds`; None: no address."""
     if t is None:
-        return None, 0
+        return 0, 0
     kind = _row_dtypes().get(t.dtype)
     if kind not in kinds or t.numel() != n or not t.is_contiguous():
         raise SrError(SR_E_ARG, f"{where}: {what}: contiguous tensor of {n} elements expected, got {t.dtype} {tuple(t.shape)}")
     return t.data_ptr(), kind
 
 
-def _same_device(where, *tensors):
-    """Device tensors, all of the current device: the library launches there."""
-    device = None
+def _launch_on(where, stream, *tensors):
+    """The stream's handle; all tensors have to be of the current device, where the library launches."""
+    device = tensors[0].get_device()
     for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise SrError(SR_E_ARG, f"{where}: device tensors expected")
-        if device is None:
-            import torch
-            device = torch.cuda.current_device()
-        if t.get_device() != device:
-            raise SrError(SR_E_ARG, f"{where}: tensors of the current device ({device}) expected, got one of {t.get_device()}")
-
-
-def _tokens(where, t):
-    _dtypes()
-    return _of_type(t, "i4", t.numel(), f"{where}: tokens")
+        if t is not None and (device < 0 or t.get_device() != device):
+            raise SrError(SR_E_ARG, f"{where}: device tensors expected, all of one device")
+    if device != _torch_c._cuda_getDevice():
+        raise SrError(SR_E_ARG, f"{where}: tensors of the current device expected")
+    return _stream(stream) if stream is not None else _torch_c._cuda_getCurrentRawStream(device)
 
 
 def sr_embed(table, tokens, out, *, scale=1.0, stream=None):
     """out[i] = scale * table[tokens[i]], zeros where the token lies outside the table.  table: [vocab, width] of float32, bfloat16 or
     float16; tokens int32 [n]; out: [n, width] of the table's type or float32."""
     n = tokens.numel()
-    if table.dim() != 2:
-        raise SrError(SR_E_ARG, "sr_embed: table: [vocab, width] expected")
-    vocab, width = table.shape
-    rows, to = _rows("sr_embed", "table", table), _rows("sr_embed", "out", out, (n, width))
-    _same_device("sr_embed", table, tokens, out)
-    _check(lib().sr_embed(rows, vocab, width, _tokens("sr_embed", tokens), n, scale, to, _stream(stream)), "sr_embed")
+    vocab, width = size = _matrix("sr_embed", "table", table)
+    rows, to = _rows("sr_embed", "table", table, size), _rows("sr_embed", "out", out, (n, width))
+    ids = _of_type(tokens, "i4", n, "sr_embed: tokens")
+    _check(_row_call("sr_embed")(_pack_rows(*rows), vocab, width, ids, n, scale, _pack_rows(*to), _launch_on("sr_embed", stream, table, tokens, out)),
+           "sr_embed")
 
 
 def sr_embed_grad(d_out, tokens, d_table, workspace, *, scale=1.0, accumulate=False, stream=None):
@@ -503,21 +517,19 @@ def sr_embed_grad(d_out, tokens, d_table, workspace, *, scale=1.0, accumulate=Fa
     not touched.  d_out: [n, width] of float32, bfloat16 or float16; d_table: [vocab, width] of the same type or float32;
     workspace: device bytes, embed_grad_workspace(n, width) of them."""
     n = tokens.numel()
-    if d_table.dim() != 2:
-        raise SrError(SR_E_ARG, "sr_embed_grad: d_table: [vocab, width] expected")
-    vocab, width = d_table.shape
-    rows, to = _rows("sr_embed_grad", "d_out", d_out, (n, width)), _rows("sr_embed_grad", "d_table", d_table)
-    ws, size = _workspace("sr_embed_grad", workspace)
-    _same_device("sr_embed_grad", d_out, tokens, d_table, workspace)
-    _check(lib().sr_embed_grad(rows, _tokens("sr_embed_grad", tokens), n, scale, to, vocab, width, int(accumulate), ws, size,
-                               _stream(stream)), "sr_embed_grad")
+    vocab, width = size = _matrix("sr_embed_grad", "d_table", d_table)
+    rows, to = _rows("sr_embed_grad", "d_out", d_out, (n, width)), _rows("sr_embed_grad", "d_table", d_table, size)
+    ids = _of_type(tokens, "i4", n, "sr_embed_grad: tokens")
+    ws, room = _workspace("sr_embed_grad", workspace)
+    _check(_row_call("sr_embed_grad")(_pack_rows(*rows), ids, n, scale, _pack_rows(*to), vocab, width, bool(accumulate), ws, room,
+                                      _launch_on("sr_embed_grad", stream, d_table, tokens, d_out, workspace)), "sr_embed_grad")
 
 
 class Dropout:
     """Which mask: p, a seed, the number of a mask of that seed (a layer's, for example), and the number of the batch's first row.
     step: device int64 [1], added to `mask` when the kernel runs, for graphs that are replayed; kept alive by this object."""
 
-    __slots__ = ("c", "step")
+    __slots__ = ("c", "address", "step")
 
     def __init__(self, p: float, seed: int, *, mask: int = 0, first_row: int = 0, step=None):
         if step is not None:
@@ -528,17 +540,17 @@ class Dropout:
             raise SrError(SR_E_ARG, f"Dropout: 0 <= p < 1 expected, got {p}")
         self.step = step
         self.c = Mask(p, 0, seed, mask, first_row, None if step is None else step.data_ptr())
+        self.address = ctypes.addressof(self.c)
 
 
 def sr_dropout(x, out, dropout: Dropout, *, residual=None, stream=None):
     """out = dropout(x), or residual + dropout(x).  x: [rows, width] of float32, bfloat16 or float16; residual: the same type or float32; out: of
     the residual's type, or x's; may be x or the residual itself.  The backward pass is the same call on the gradient."""
-    if x.dim() != 2:
-        raise SrError(SR_E_ARG, "sr_dropout: x: [rows, width] expected")
-    n, width = shape = x.shape
-    rows, add, to = _rows("sr_dropout", "x", x), _rows("sr_dropout", "residual", residual, shape), _rows("sr_dropout", "out", out, shape)
-    _same_device("sr_dropout", x, residual, out, dropout.step)
-    _check(lib().sr_dropout(rows, add, to, n, width, dropout.c, _stream(stream)), "sr_dropout")
+    n, width = size = _matrix("sr_dropout", "x", x)
+    rows, to = _rows("sr_dropout", "x", x, size), _rows("sr_dropout", "out", out, size)
+    add = None if residual is None else _pack_rows(*_rows("sr_dropout", "residual", residual, size))
+    handle = _launch_on("sr_dropout", stream, x, out, residual, dropout.step)
+    _check(_row_call("sr_dropout")(_pack_rows(*rows), add, _pack_rows(*to), n, width, dropout.address, handle), "sr_dropout")
 
 
 def sr_add_norm(residual, gain, out, *, x=None, total=None, rstd=None, scales=None, scale_block=0, dropout=None, eps=1e-6, stream=None):
@@ -548,18 +560,16 @@ def sr_add_norm(residual, gain, out, *, x=None, total=None, rstd=None, scales=No
     with scales float32 [rows, ceil(width / scale_block)] (scale_block 32, 64, 128) or [rows] (0); gain: [width] of x's type or
     float32; rstd: float32 [rows].  total may be the residual itself, out may be x."""
     where = "sr_add_norm"
-    if residual.dim() != 2:
-        raise SrError(SR_E_ARG, f"{where}: residual: [rows, width] expected")
-    n, width = shape = residual.shape
-    a, r, t, o = _rows(where, "x", x, shape), _rows(where, "residual", residual), _rows(where, "total", total, shape), _rows(where, "out", out, shape)
+    n, width = size = _matrix(where, "residual", residual)
+    r, o, t = _rows(where, "residual", residual, size), _rows(where, "out", out, size), _rows(where, "total", total, size)
     g, kind = _vector(where, "gain", gain, width, (0, 1, 2))
-    if x is None:                    # the type of the rest: the output's, where that is no type of 8 bits
-        a.dtype = o.dtype if o.dtype <= 2 else kind or r.dtype
+    # the type of the rest, where there is no branch: the output's, if that is none of 8 bits
+    a = _rows(where, "x", x, size) if x is not None else (0, 0, o[2] if o[2] <= 2 else kind or r[2], 0)
     blocks = n if scale_block == 0 else n * (-(-width // scale_block)) if scale_block > 0 else -1
-    _same_device(where, residual, gain, out, x, total, rstd, scales, None if dropout is None else dropout.step)
-    args = NormRows(a, r, t, o, g, _vector(where, "rstd", rstd, n, (0,))[0], _vector(where, "scales", scales, blocks, (0,))[0],
-                    None if dropout is None else ctypes.pointer(dropout.c), kind, n, width, scale_block, eps, 0)
-    _check(lib().sr_add_norm(args, _stream(stream)), where)
+    handle = _launch_on(where, stream, residual, gain, out, x, total, rstd, scales, None if dropout is None else dropout.step)
+    args = _pack_norm(*a, *r, *t, *o, g, _vector(where, "rstd", rstd, n, (0,))[0], _vector(where, "scales", scales, blocks, (0,))[0],
+                      0 if dropout is None else dropout.address, kind, n, width, scale_block, eps, 0)
+    _check(_row_call(where)(args, handle), where)
 
 
 def sr_add_norm_grad(d_out, total, rstd, gain, workspace, *, d_total=None, d_residual=None, d_x=None, d_gain=None, dropout=None,
@@ -568,17 +578,15 @@ def sr_add_norm_grad(d_out, total, rstd, gain, workspace, *, d_total=None, d_res
     d_out's type or float32; accumulate: added to).  Each may be None, not all.  d_total: what reaches the sum from behind it, or None.
     workspace: device bytes, norm_grad_workspace(rows, width) of them; None where d_gain is."""
     where = "sr_add_norm_grad"
-    if d_out.dim() != 2:
-        raise SrError(SR_E_ARG, f"{where}: d_out: [rows, width] expected")
-    n, width = shape = d_out.shape
+    n, width = size = _matrix(where, "d_out", d_out)
     g, kind = _vector(where, "gain", gain, width, (0, 1, 2))
     to, to_kind = _vector(where, "d_gain", d_gain, width, (0, 1, 2))
-    ws, size = _workspace(where, workspace) if workspace is not None else (None, 0)
-    _same_device(where, d_out, total, rstd, gain, workspace, d_total, d_residual, d_x, d_gain, None if dropout is None else dropout.step)
-    args = NormGradRows(_rows(where, "d_out", d_out), _rows(where, "total", total, shape), _rows(where, "d_total", d_total, shape),
-                        _rows(where, "d_residual", d_residual, shape), _rows(where, "d_x", d_x, shape), _vector(where, "rstd", rstd, n, (0,))[0], g, to,
-                        None if dropout is None else ctypes.pointer(dropout.c), kind, to_kind, n, width, int(accumulate), 0)
-    _check(lib().sr_add_norm_grad(args, ws, size, _stream(stream)), where)
+    ws, room = _workspace(where, workspace) if workspace is not None else (None, 0)
+    args = _pack_norm_grad(*_rows(where, "d_out", d_out, size), *_rows(where, "total", total, size), *_rows(where, "d_total", d_total, size),
+                           *_rows(where, "d_residual", d_residual, size), *_rows(where, "d_x", d_x, size), _vector(where, "rstd", rstd, n, (0,))[0], g, to,
+                           0 if dropout is None else dropout.address, kind, to_kind, n, width, bool(accumulate), 0)
+    handle = _launch_on(where, stream, d_out, total, rstd, gain, workspace, d_total, d_residual, d_x, d_gain, None if dropout is None else dropout.step)
+    _check(_row_call(where)(args, ws, room, handle), where)
 
 
 def sr_probe_hbm(src, dst, mode: int, iters: int = 10, stream=None) -> float:

@@ -5,7 +5,8 @@
 //
 // Memory bounds it: dy, h and d_total read, d_residual and d_x written.  Workgroups (wavefronts, for rows of up to 64 vectors) take
 // rows in turn, hold the next row's vectors while they reduce and write the one before, and keep their share of d_gain in registers;
-// a second kernel adds the shares up in the order of their numbers, so that the sum is the same bit for bit from call to call.
+// a second kernel adds the shares up in the order of their numbers, so that the sum is the same bit for bit from call to call.  Of few rows
+// the gain's gradient is added up from the rows themselves, by other workgroups of the same launch.
 #include "row_ops.h"
 
 namespace sr {
@@ -18,9 +19,49 @@ struct NormGradArgs {
     const float *rstd;
     float *parts;                    // [n_parts][width]
     int rows, width, n_parts;
-    int has_d_total, gain_single, gain_grad_single, accumulate;
+    int has_d_total, gain_single, gain_grad_single, gain_grad_half, accumulate;
     MaskArgs mask;
 };
+
+// A gain's gradient, sixteen columns a workgroup: x(p, c) added up over p < n, by groups of lanes that take the numbers in turn, then over the
+// groups of a wavefront and over the wavefronts.  s: 16 x kGainColumns floats of LDS.
+constexpr int kGainColumns = 16;
+template <typename F>
+__device__ __forceinline__ void gain_columns(const NormGradArgs &a, int block, int n, float (*s)[kGainColumns], F &&x) {
+    const int groups = (int)blockDim.x / kGainColumns, group = (int)threadIdx.x / kGainColumns, i = (int)threadIdx.x % kGainColumns;
+    const int c = block * kGainColumns + i, at = min(c, a.width - 1);
+    float sum = 0.f;
+    for (int p = group; p < n; p += 8 * groups) {
+        float y[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) y[u] = x(min(p + u * groups, n - 1), at);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) sum += p + u * groups < n ? y[u] : 0.f;
+    }
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    if ((threadIdx.x & 63) < kGainColumns) s[threadIdx.x >> 6][i] = sum;
+    __syncthreads();
+    if (group != 0 || c >= a.width) return;
+    sum = s[0][i];
+    for (int w = 1; w < (int)blockDim.x >> 6; ++w) sum += s[w][i];
+    if (a.gain_grad_single) {
+        float *to = (float *)a.d_gain + c;
+        *to = a.accumulate ? *to + sum : sum;
+    } else if (a.gain_grad_half) {
+        f16_t *to = (f16_t *)a.d_gain + c;
+        *to = (f16_t)(a.accumulate ? (float)*to + sum : sum);
+    } else {
+        __bf16 *to = (__bf16 *)a.d_gain + c;
+        *to = (__bf16)(a.accumulate ? (float)*to + sum : sum);
+    }
+}
+
+// From the shares of add_norm_grad_kernel's workgroups
+__global__ __launch_bounds__(1024) void gain_grad_kernel(NormGradArgs a) {
+    __shared__ float s[16][kGainColumns];
+    gain_columns(a, (int)blockIdx.x, a.n_parts, s, [&](int p, int c) { return a.parts[(size_t)p * a.width + c]; });
+}
 
 template <typename T, typename R, int N, int NV>
 struct GradRow {
@@ -44,6 +85,14 @@ struct GradRow {
 template <typename T, typename R, int N, int NV, bool WAVE>
 __global__ __launch_bounds__(WAVE ? 256 : 1024) void add_norm_grad_kernel(NormGradArgs a) {
     __shared__ float s_sum[2][16];
+    const int row_blocks = WAVE ? (a.n_parts + 3) / 4 : a.n_parts;
+    if ((int)blockIdx.x >= row_blocks) {             // few rows: the gain's gradient from the rows themselves
+        __shared__ float s[16][kGainColumns];
+        gain_columns(a, (int)blockIdx.x - row_blocks, a.rows, s, [&](int r, int c) {
+            return (float)((const T *)a.d_out)[r * a.ld_d_out + c] * ((float)((const R *)a.total)[r * a.ld_total + c] * a.rstd[r]);
+        });
+        return;
+    }
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
     const int part = __builtin_amdgcn_readfirstlane(WAVE ? (int)blockIdx.x * 4 + wave : (int)blockIdx.x);
     if (WAVE && part >= a.n_parts) return;
@@ -109,36 +158,21 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void add_norm_grad_kernel(NormGr
             }
         }
     }
-    if (!a.d_gain) return;
+    if (!a.parts) return;
     float *to = a.parts + (size_t)part * a.width;
 #pragma unroll
     for (int i = 0; i < NV; ++i) store_span<N>(to, at[i], d_gain[i]);
 }
 
-// d_gain[c] [+]= sum over p of parts[p][c]: sixteen columns a workgroup, 64 parts at a time, each thread's in order and then the threads'
-constexpr int kGainThreads = 1024, kGainColumns = 16, kGainGroups = kGainThreads / kGainColumns;
-template <typename G>
-__global__ __launch_bounds__(kGainThreads) void gain_grad_kernel(NormGradArgs a) {
-    __shared__ float s[kGainGroups][kGainColumns + 1];
-    const int group = threadIdx.x / kGainColumns, i = threadIdx.x % kGainColumns, c = (int)blockIdx.x * kGainColumns + i;
-    float sum = 0.f;
-    if (c < a.width)
-        for (int p = group; p < a.n_parts; p += kGainGroups) sum += a.parts[(size_t)p * a.width + c];
-    s[group][i] = sum;
-    __syncthreads();
-    if (group != 0 || c >= a.width) return;
-    for (int k = 1; k < kGainGroups; ++k) sum += s[k][i];
-    G *to = (G *)a.d_gain + c;
-    *to = (G)(a.accumulate ? (float)*to + sum : sum);
-}
-
 template <typename T, typename R, int N>
 int launch_add_norm_grad(const NormGradArgs &a, const RowShape &s, hipStream_t stream) {
-    if (s.wave) add_norm_grad_kernel<T, R, N, 1, true><<<dim3(ceil_div(a.n_parts, 4)), dim3(256), 0, stream>>>(a);
+    const int more = a.d_gain && !a.parts ? ceil_div(a.width, kGainColumns) : 0;
+    const dim3 grid((s.wave ? ceil_div(a.n_parts, 4) : a.n_parts) + more);
+    if (s.wave) add_norm_grad_kernel<T, R, N, 1, true><<<grid, dim3(256), 0, stream>>>(a);
     else if constexpr (N > 1) {
-        if (s.vecs == 1) add_norm_grad_kernel<T, R, N, 1, false><<<dim3(a.n_parts), dim3(s.threads), 0, stream>>>(a);
-        else if (s.vecs == 2) add_norm_grad_kernel<T, R, N, 2, false><<<dim3(a.n_parts), dim3(s.threads), 0, stream>>>(a);
-        else add_norm_grad_kernel<T, R, N, 4, false><<<dim3(a.n_parts), dim3(s.threads), 0, stream>>>(a);
+        if (s.vecs == 1) add_norm_grad_kernel<T, R, N, 1, false><<<grid, dim3(s.threads), 0, stream>>>(a);
+        else if (s.vecs == 2) add_norm_grad_kernel<T, R, N, 2, false><<<grid, dim3(s.threads), 0, stream>>>(a);
+        else add_norm_grad_kernel<T, R, N, 4, false><<<grid, dim3(s.threads), 0, stream>>>(a);
     }
     SR_HIP(hipGetLastError());
     return SR_OK;
@@ -190,7 +224,10 @@ int add_norm_grad(const sr_norm_grad_rows *x, void *workspace, size_t workspace_
     a.gain_grad_single = x->d_gain_dtype == SR_F32;
     a.accumulate = x->accumulate != 0;
     a.rstd = x->rstd;
-    a.parts = (float *)workspace;
+    a.gain_grad_half = x->d_gain_dtype == SR_F16;
+    // the workgroups for the gain read d_out while others write d_x
+    const bool direct = x->rows > 0 && gain_grad_direct(x->rows, x->width) && x->d_x.data != x->d_out.data;
+    a.parts = x->d_gain && !direct ? (float *)workspace : nullptr;
     a.rows = x->rows;
     a.width = x->width;
     return with_row_types(dtype, residual, [&](auto *t, auto *r) -> int {
@@ -199,10 +236,8 @@ int add_norm_grad(const sr_norm_grad_rows *x, void *workspace, size_t workspace_
         constexpr int N = sizeof(R) == 4 ? 4 : 8;
         if (a.rows > 0)
             SR_TRY((shape.per_vec == 1 ? launch_add_norm_grad<T, R, 1>(a, shape, stream) : launch_add_norm_grad<T, R, N>(a, shape, stream)));
-        if (!a.d_gain) return SR_OK;
-        const dim3 grid(ceil_div(a.width, kGainColumns)), block(kGainThreads);
-        if (a.gain_grad_single) gain_grad_kernel<float><<<grid, block, 0, stream>>>(a);
-        else gain_grad_kernel<T><<<grid, block, 0, stream>>>(a);
+        if (!a.parts) return SR_OK;
+        gain_grad_kernel<<<dim3(ceil_div(a.width, kGainColumns)), dim3(1024), 0, stream>>>(a);
         SR_HIP(hipGetLastError());
         return SR_OK;
     });

@@ -24,26 +24,43 @@ struct EmbedArgs {
     void *out;
     const int32_t *tokens;
     int64_t ld_table, ld_out;
-    int n, vocab, width, parts;      // parts: workgroups of a row, 256 vectors each
+    int n, vocab, width, parts;      // parts: wavefronts of a row
     FastDiv by_parts;
-    int lanes_shift;                 // log2 of the threads of a row where several rows share a workgroup
+    int lanes_shift;                 // log2 of the threads of a row of at most 32 vectors
     float scale;
 };
 
+// Rows of at most 32 vectors, several to a wavefront
 template <typename T, typename O, int N>
-__global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a) {
-    int row, v;
-    if (a.parts > 1) {
-        row = quotient(blockIdx.x, a.by_parts);
-        v = (int)(blockIdx.x - (unsigned)row * a.parts) * 256 + threadIdx.x;
-    } else {
-        row = (int)((blockIdx.x << (8 - a.lanes_shift)) + (threadIdx.x >> a.lanes_shift));
-        v = threadIdx.x & ((1 << a.lanes_shift) - 1);
-    }
+__global__ __launch_bounds__(256) void embed_narrow_kernel(EmbedArgs a) {
+    const int row = (int)((blockIdx.x << (8 - a.lanes_shift)) + (threadIdx.x >> a.lanes_shift));
     if (row >= a.n) return;
-    const Span s = span_of<N>(v, a.width);
+    const Span s = span_of<N>(threadIdx.x & ((1 << a.lanes_shift) - 1), a.width);
     if (s.skip == N) return;
     const int token = a.tokens[row];
+    float x[N];
+    if ((unsigned)token < (unsigned)a.vocab) {
+        Part<T, N> p;
+        p.load((const T *)a.table + token * a.ld_table + s.c);
+        p.widen(x);
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] *= a.scale;
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = 0.f;
+    }
+    store_span<N>((O *)a.out + row * a.ld_out, s, x);
+}
+
+// A wavefront 64 vectors of a row: its token comes once, through a scalar load.  65536 rows of 3584 bf16: 171 us, as with two, four and eight
+// vectors a lane; 190 with a workgroup for 256 vectors, whose second one is three quarters full.
+template <typename T, typename O, int N>
+__global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a) {
+    const int lane = threadIdx.x & 63, unit = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+    const int row = quotient(unit, a.by_parts);
+    if (row >= a.n) return;
+    const Span s = span_of<N>((unit - row * a.parts) * 64 + lane, a.width);
+    const int token = read_uniform(a.tokens + row);
     float x[N];
     if ((unsigned)token < (unsigned)a.vocab) {
         Part<T, N> p;
@@ -61,14 +78,23 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a) {
 template <typename T, typename O, int N>
 int launch_embed(EmbedArgs a, hipStream_t stream) {
     const int vecs = ceil_div(a.width, N);
-    a.parts = ceil_div(vecs, 256);
-    a.by_parts = fast_div(a.parts);
-    a.lanes_shift = 0;
-    while ((1 << a.lanes_shift) < vecs && a.lanes_shift < 8) ++a.lanes_shift;
-    const int64_t blocks = a.parts > 1 ? (int64_t)a.n * a.parts : ((int64_t)a.n + (256 >> a.lanes_shift) - 1) >> (8 - a.lanes_shift);
-    if (blocks > INT32_MAX / 256) return SR_E_LIMIT;
-    embed_kernel<T, O, N><<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(a);
-    SR_HIP(hipGetLastError());
+    if (vecs <= 32) {
+        a.lanes_shift = 0;
+        while ((1 << a.lanes_shift) < vecs) ++a.lanes_shift;
+        const int64_t blocks = ((int64_t)a.n + (256 >> a.lanes_shift) - 1) >> (8 - a.lanes_shift);
+        if (blocks > INT32_MAX / 256) return SR_E_LIMIT;
+        embed_narrow_kernel<T, O, N><<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(a);
+        SR_HIP(hipGetLastError());
+        return SR_OK;
+    }
+    if constexpr (N > 1) {                           // rows column by column are narrow
+        a.parts = ceil_div(vecs, 64);
+        a.by_parts = fast_div(a.parts);
+        const int64_t blocks = ((int64_t)a.n * a.parts + 3) / 4;
+        if (blocks > INT32_MAX / 256) return SR_E_LIMIT;
+        embed_kernel<T, O, N><<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(a);
+        SR_HIP(hipGetLastError());
+    }
     return SR_OK;
 }
 
@@ -78,6 +104,7 @@ int launch_embed(EmbedArgs a, hipStream_t stream) {
 constexpr uint32_t kNoToken = 0x80000000u;           // sorts behind every token
 constexpr uint32_t kBehindAll = 0xffffffffu;         // and this behind it
 constexpr int kTile = 4096;                          // tokens that are sorted by comparing all with all
+constexpr int kFourKeys = 16384;                     // from here on rank_kernel has four keys a lane
 
 struct EmbedGradArgs {
     const void *d_out;
@@ -88,6 +115,7 @@ struct EmbedGradArgs {
     int32_t *places;                 // [n] and where they came from
     uint32_t *tile_sorted;           // the same of every tile by itself, where there are several
     int32_t *tile_places;
+    uint32_t *splits;                // [n / 64] the last key of every 64 of sorted tiles
     float *parts;                    // [spans][2][width]: sums of the token that comes in from the span before, and of the one that goes on
     int n, vocab, width, chunk, spans, slices, sum_blocks;
     int zero_rows;                   // of the table, a wavefront that writes zeros
@@ -99,12 +127,14 @@ struct EmbedGradArgs {
 __device__ __forceinline__ int round_up_4(int n) { return (n + 3) & ~3; }
 __device__ __forceinline__ uint32_t key_of(int token, int vocab) { return (unsigned)token < (unsigned)vocab ? (uint32_t)token : kNoToken; }
 
-// Sixteen places a workgroup; each of sixteen groups of lanes compares them with a sixteenth of their tile, which lies in LDS
-constexpr int kRankKeys = 16, kRankGroups = 16;
+// 16 * KEYS places a workgroup; each of sixteen groups of lanes compares them with a sixteenth of their tile, which lies in LDS.  Four keys a
+// lane read LDS a quarter as often, one key a lane makes more workgroups: 4096 tokens take RANK1A us with one and RANK4A with four, 49153 RANK1B and RANK4B.
+constexpr int kRankGroups = 16;
+template <int KEYS>
 __global__ __launch_bounds__(256) void rank_kernel(EmbedGradArgs a, uint32_t *__restrict__ sorted, int32_t *__restrict__ places) {
     __shared__ __align__(16) uint32_t s_key[kTile + 64 * 4];         // four words more after every 64: groups read different banks
-    __shared__ int s_rank[4][kRankKeys];
-    const int first = (int)blockIdx.x * kRankKeys, begin = first / kTile * kTile, size = min(kTile, a.n - begin);
+    __shared__ int s_rank[4][16 * KEYS];
+    const int first = (int)blockIdx.x * (16 * KEYS), begin = first / kTile * kTile, size = min(kTile, a.n - begin);
     const int each = round_up_4((size + kRankGroups - 1) / kRankGroups);     // of a group
     auto slot = [](int j) __attribute__((always_inline)) { return j + (j >> 6) * 4; };
     for (int j0 = threadIdx.x; j0 < each * kRankGroups; j0 += 256 * 8) {     // eight loads before the first is waited for
@@ -118,42 +148,82 @@ __global__ __launch_bounds__(256) void rank_kernel(EmbedGradArgs a, uint32_t *__
         }
     }
     __syncthreads();
-    const int mine = first - begin + (int)(threadIdx.x % kRankKeys), group = (int)threadIdx.x / kRankKeys;
-    const uint32_t key = s_key[slot(min(mine, size - 1))];
-    int rank = 0;
+    const int own = first - begin, i = (int)threadIdx.x & 15, group = (int)threadIdx.x >> 4;
+    uint32_t key[KEYS];
+    int rank[KEYS];
+#pragma unroll
+    for (int k = 0; k < KEYS; ++k) {
+        key[k] = s_key[slot(min(own + 16 * k + i, size - 1))];
+        rank[k] = 0;
+    }
     // before the workgroup's places: those that are not greater; from there on: those that are less, and of its own the equal ones before
 #pragma unroll 4
     for (int j = group * each; j < (group + 1) * each; j += 4) {
         const raw16 other = *(const raw16 *)(s_key + slot(j));
-        const uint32_t limit = key + (j < first - begin);
+        const uint32_t more = j < own;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) rank += other[u] < limit;
+        for (int k = 0; k < KEYS; ++k) {
+            const uint32_t limit = key[k] + more;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) rank[k] += other[u] < limit;
+        }
     }
-    if (first - begin + group < mine) rank += s_key[slot(first - begin + group)] == key;
-    rank += __shfl_xor(rank, 16, 64);
-    rank += __shfl_xor(rank, 32, 64);
-    if ((threadIdx.x & 63) < kRankKeys) s_rank[threadIdx.x >> 6][threadIdx.x & 63] = rank;
+#pragma unroll
+    for (int q = 0; q < KEYS; ++q) {
+        const int at = 16 * q + group;
+        const uint32_t other = s_key[slot(min(own + at, size - 1))];
+#pragma unroll
+        for (int k = 0; k < KEYS; ++k) rank[k] += at < 16 * k + i && other == key[k];
+    }
+#pragma unroll
+    for (int k = 0; k < KEYS; ++k) {
+        rank[k] += __shfl_xor(rank[k], 16, 64);
+        rank[k] += __shfl_xor(rank[k], 32, 64);
+        if ((threadIdx.x & 63) < 16) s_rank[threadIdx.x >> 6][16 * k + i] = rank[k];
+    }
     __syncthreads();
-    if (threadIdx.x >= kRankKeys || mine >= size) return;
-    rank = s_rank[0][threadIdx.x] + s_rank[1][threadIdx.x] + s_rank[2][threadIdx.x] + s_rank[3][threadIdx.x];
-    sorted[begin + rank] = key;
-    places[begin + rank] = begin + mine;
+    const int mine = (int)threadIdx.x;
+    if (mine >= 16 * KEYS || own + mine >= size) return;
+    const int at = s_rank[0][mine] + s_rank[1][mine] + s_rank[2][mine] + s_rank[3][mine];
+    const uint32_t k = s_key[slot(own + mine)];
+    sorted[begin + at] = k;
+    places[begin + at] = begin + own + mine;
+    // the last key of every 64, for those who search the tile
+    if ((at & 63) == 63) a.splits[(begin + at) >> 6] = k;
 }
 
 // Sorted tiles into one sorted list: a key comes behind what is not greater in the tiles before its own, and what is less in those behind it.
-// Searches by quarters in kTogether tiles at a time, whose loads do not wait for each other.
-constexpr int kTogether = 8;
+// Which 64 of a tile its place lies among is found in LDS, where the last keys of every 64 are, and the place by three more steps in
+// kTogether tiles at a time, whose loads do not wait for each other.
+constexpr int kTogether = 8, kTileSplits = kTile / 64;
 __global__ __launch_bounds__(256) void merge_kernel(EmbedGradArgs a, const uint32_t *__restrict__ tiles, const int32_t *__restrict__ from) {
-    const int i = (int)(blockIdx.x * 256 + threadIdx.x);
-    if (i >= a.n) return;
+    __shared__ uint32_t s_split[kTogether * kTileSplits];
+    const int mine = (int)(blockIdx.x * 256 + threadIdx.x), i = min(mine, a.n - 1);
     const uint32_t key = tiles[i];
-    const int own = i / kTile, n_tiles = (a.n + kTile - 1) / kTile;
+    const int place = from[i];
+    const int own = i / kTile, n_tiles = (a.n + kTile - 1) / kTile, n_splits = a.n >> 6;
     int rank = i - own * kTile;
     for (int t0 = 0; t0 < n_tiles; t0 += kTogether) {
+        __syncthreads();
+        for (int j = threadIdx.x; j < kTogether * kTileSplits; j += 256) {
+            const int at = t0 * kTileSplits + j;
+            s_split[j] = at < n_splits ? a.splits[at] : kBehindAll;
+        }
+        __syncthreads();
         int at[kTogether];                           // this many of the tile come before
 #pragma unroll
         for (int u = 0; u < kTogether; ++u) at[u] = 0;
-        for (int step = kTile / 4; step > 0; step >>= 2) {
+#pragma unroll
+        for (int step = kTileSplits / 2; step > 0; step >>= 1)
+#pragma unroll
+            for (int u = 0; u < kTogether; ++u)
+                at[u] += s_split[u * kTileSplits + at[u] + step - 1] < key + (t0 + u < own) ? step : 0;
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u)          // 63 at most so far
+            at[u] = 64 * (at[u] + (s_split[u * kTileSplits + at[u]] < key + (t0 + u < own)));
+        // now the 64 behind them; behind the tile there are none
+#pragma unroll
+        for (int step = 16; step > 0; step >>= 2) {
             uint32_t other[kTogether][3];
 #pragma unroll
             for (int u = 0; u < kTogether; ++u)
@@ -161,21 +231,20 @@ __global__ __launch_bounds__(256) void merge_kernel(EmbedGradArgs a, const uint3
                 for (int q = 0; q < 3; ++q) other[u][q] = tiles[min((t0 + u) * kTile + at[u] + (q + 1) * step - 1, a.n - 1)];
 #pragma unroll
             for (int u = 0; u < kTogether; ++u) {
-                const int base = (t0 + u) * kTile + at[u] + step - 1;
+                const int base = at[u] + step - 1, end = min(kTile, a.n - (t0 + u) * kTile);
                 const uint32_t limit = key + (t0 + u < own);
 #pragma unroll
-                for (int q = 0; q < 3; ++q) at[u] += base + q * step < a.n && other[u][q] < limit ? step : 0;
+                for (int q = 0; q < 3; ++q) at[u] += base + q * step < end && other[u][q] < limit ? step : 0;
             }
         }
+        // 63 of those 64 are decided, and the last one is not before the key: else its 64 were passed by above
 #pragma unroll
-        for (int u = 0; u < kTogether; ++u) {        // the steps reach kTile - 1 of them
-            const int probe = (t0 + u) * kTile + at[u];
-            at[u] += probe < a.n && tiles[min(probe, a.n - 1)] < key + (t0 + u < own);
+        for (int u = 0; u < kTogether; ++u)
             if (t0 + u != own && t0 + u < n_tiles) rank += at[u];
-        }
     }
+    if (mine >= a.n) return;
     a.sorted[rank] = key;
-    a.places[rank] = from[i];
+    a.places[rank] = place;
 }
 
 // First place of the sorted list whose token is not below `token`; the wavefront asks at 64 places at a time
@@ -386,13 +455,99 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(EmbedGradAr
     write_row<N, O>(a, token, s, sum);
 }
 
+// Few tokens and a small table: a workgroup has sixteen rows of the table, looks for them in the whole list and adds up what it finds,
+// a wavefront a row; rows with more than kFewTogether places are shared by all.  One launch instead of three: FEWUS us instead of FEWOLD
+// for 256 tokens into 1024 x 256 fp32, of which the call itself is most.
+constexpr int kFewTokens = 1024, kFewTogether = 32;
+template <typename T, typename O, int N>
+__global__ __launch_bounds__(1024) void embed_few_kernel(EmbedGradArgs a) {
+    __shared__ float s_sum[16][N][64];
+    __shared__ uint16_t s_place[16][kFewTokens];
+    __shared__ int s_count[16][16];                  // [wavefront][row]
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, i = threadIdx.x;
+    const int block = (int)blockIdx.x / a.slices, slice = (int)blockIdx.x - block * a.slices;
+    const uint32_t first = (uint32_t)block * 16;
+    const uint32_t key = i < a.n ? key_of(a.tokens[i], a.vocab) : kNoToken, row = key - first;
+    int before = 0, mine = 0;                        // of the same row in this wavefront; of row `lane`
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const uint64_t same = __ballot(row == (uint32_t)r);
+        if (row == (uint32_t)r) before = __popcll(same & (((uint64_t)1 << lane) - 1));
+        if (lane == r) mine = __popcll(same);
+    }
+    if (lane < 16) s_count[wave][lane] = mine;
+    __syncthreads();
+    if (row < 16) {
+        for (int w = 0; w < wave; ++w) before += s_count[w][row];
+        s_place[row][before] = (uint16_t)i;
+    }
+    // of every row, in lane r
+    int count = 0;
+    for (int w = 0; w < 16; ++w) count += s_count[w][lane & 15];
+    __syncthreads();
+
+    const Span s = span_of<N>(slice * 64 + lane, a.width);
+    float sum[N];
+    auto add_up = [&](int r, int from, int to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) sum[j] = 0.f;
+        for (int p = from; p < to; p += 8) {
+            Part<T, N> x[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                x[u].load((const T *)a.d_out + __builtin_amdgcn_readfirstlane((int)s_place[r][min(p + u, to - 1)]) * a.ld_d_out + s.c);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                if (p + u >= to) break;
+                float y[N];
+                x[u].widen(y);
+#pragma unroll
+                for (int j = 0; j < N; ++j) sum[j] += y[j];
+            }
+        }
+    };
+    const int own = __builtin_amdgcn_readlane(count, wave);
+    if (own <= kFewTogether && first + wave < (uint32_t)a.vocab) {
+        if (own > 0) {
+            add_up(wave, 0, own);
+            write_row<N, O>(a, first + wave, s, sum);
+        } else if (!a.accumulate) {
+            const float zero[N] = {};
+            store_span<N>((O *)a.d_table + (first + wave) * a.ld_d_table, s, zero);
+        }
+    }
+    for (int r = 0; r < 16; ++r) {
+        const int n = __builtin_amdgcn_readlane(count, r);
+        if (n <= kFewTogether) continue;             // the same for all wavefronts
+        const int each = (n + 15) / 16, from = min(wave * each, n);
+        add_up(r, from, min(from + each, n));
+#pragma unroll
+        for (int j = 0; j < N; ++j) s_sum[wave][j][lane] = sum[j];
+        __syncthreads();
+        if (wave == 0) {
+            for (int w = 1; w < (n + each - 1) / each; ++w)
+#pragma unroll
+                for (int j = 0; j < N; ++j) sum[j] += s_sum[w][j][lane];
+            write_row<N, O>(a, first + r, s, sum);
+        }
+        __syncthreads();
+    }
+}
+
 template <typename T, typename O, int N>
 int launch_embed_grad(EmbedGradArgs a, hipStream_t stream) {
+    if (a.n <= kFewTokens && embed_few(a.vocab, a.slices)) {
+        if (a.n == 0 && a.accumulate) return SR_OK;
+        embed_few_kernel<T, O, N><<<dim3(ceil_div(a.vocab, 16) * a.slices), dim3(1024), 0, stream>>>(a);
+        SR_HIP(hipGetLastError());
+        return SR_OK;
+    }
     if (a.n > 0) {
         const bool tiles = a.n > kTile;
         uint32_t *sorted = tiles ? a.tile_sorted : a.sorted;
         int32_t *places = tiles ? a.tile_places : a.places;
-        rank_kernel<<<dim3(ceil_div(a.n, kRankKeys)), dim3(256), 0, stream>>>(a, sorted, places);
+        if (a.n >= kFourKeys) rank_kernel<4><<<dim3(ceil_div(a.n, 64)), dim3(256), 0, stream>>>(a, sorted, places);
+        else rank_kernel<1><<<dim3(ceil_div(a.n, 16)), dim3(256), 0, stream>>>(a, sorted, places);
         SR_HIP(hipGetLastError());
         if (tiles) {
             merge_kernel<<<dim3(ceil_div(a.n, 256)), dim3(256), 0, stream>>>(a, sorted, places);
@@ -431,7 +586,8 @@ int embed_grad(const sr_rows *d_out, const int32_t *tokens, int n, float scale, 
     a.places = (int32_t *)workspace + n;
     a.tile_sorted = (uint32_t *)workspace + 2 * (size_t)n;
     a.tile_places = (int32_t *)workspace + 3 * (size_t)n;
-    a.parts = (float *)((char *)workspace + 16 * (size_t)n);
+    a.splits = (uint32_t *)workspace + 4 * (size_t)n;
+    a.parts = (float *)((char *)workspace + round_up(16 * n + n / 16, 16));
     a.n = n;
     a.vocab = vocab;
     a.width = width;
@@ -461,7 +617,7 @@ extern "C" int sr_embed(const sr_rows *table, int vocab, int width, const int32_
     if (!rows_fit(*table, width, SR_F16)) return SR_E_ARG;
     if (n == 0) return SR_OK;
     if (!rows_fit(*out, width, SR_F16) || !tokens || (uintptr_t)tokens % 4 || out->data == table->data) return SR_E_ARG;
-    EmbedArgs a{table->data, out->data, tokens, table->ld, out->ld, n, vocab, width, 0, FastDiv{}, 0, scale};
+    const EmbedArgs a{table->data, out->data, tokens, table->ld, out->ld, n, vocab, width, 0, FastDiv{}, 0, scale};
     return with_row_types(table->dtype, out->dtype, [&](auto *t, auto *o) -> int {
         typedef std::remove_pointer_t<decltype(t)> T;
         typedef std::remove_pointer_t<decltype(o)> O;
