@@ -2,7 +2,8 @@
 //
 // h = residual + dropout(x), rounded to the residual's type; out = h * rstd * gain, rstd = 1 / sqrt(mean(h^2) + eps), of h as it is stored,
 // so that the backward pass, which reads it, differentiates what was computed.  Memory bounds it: x and residual read, h and out
-// written.  A row lies in the registers of its workgroup (of a wavefront, up to 64 vectors) between the sum and its use.
+// written.  A row lies in the registers of its workgroup (of a wavefront, up to 64
+// vectors, of 16 or 32 lanes, up to 16 or 32) between the sum and its use.
 //
 // Output in 8 bits: a scale for a row or for 32, 64 or 128 of its columns, max |out| / (largest finite value), which the block's columns
 // are divided by; adjacent lanes hold a block and find its largest value between them.
@@ -63,13 +64,15 @@ __device__ __forceinline__ void store_bytes(uint8_t *row, const Span &s, const f
     }
 }
 
-template <typename T, typename R, bool BYTES, int N, int NV, bool WAVE>
-__global__ __launch_bounds__(WAVE ? 256 : 1024) void add_norm_kernel(NormRowArgs a) {
+// LANES: of a row that is a part of a wavefront or a whole one; 0: a workgroup
+template <typename T, typename R, bool BYTES, int N, int NV, int LANES>
+__global__ __launch_bounds__(LANES ? 256 : 1024) void add_norm_kernel(NormRowArgs a) {
     __shared__ float s_sum[16], s_max[16];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
-    const int row = __builtin_amdgcn_readfirstlane(WAVE ? (int)blockIdx.x * 4 + wave : (int)blockIdx.x);
-    if (WAVE && row >= a.rows) return;
-    const int first = WAVE ? lane : (int)threadIdx.x, step = WAVE ? 64 : (int)blockDim.x;
+    const int row = LANES && LANES < 64 ? (int)(blockIdx.x * (256 / LANES) + threadIdx.x / LANES)
+                                        : __builtin_amdgcn_readfirstlane(LANES ? (int)blockIdx.x * 4 + wave : (int)blockIdx.x);
+    if (LANES && row >= a.rows) return;
+    const int first = LANES ? (int)threadIdx.x & (LANES - 1) : (int)threadIdx.x, step = (int)blockDim.x;
     const T *x = (const T *)a.x + row * a.ld_x;
     const R *residual = (const R *)a.residual + row * a.ld_residual;
 
@@ -116,8 +119,8 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void add_norm_kernel(NormRowArgs
 #pragma unroll
         for (int j = 0; j < N; ++j) sum += j >= at[i].skip ? h[i][j] * h[i][j] : 0.f;
     }
-    sum = reduce_64(sum, [](float p, float q) { return p + q; });
-    if (!WAVE) {
+    sum = reduce_lanes<LANES>(sum, [](float p, float q) { return p + q; });
+    if (!LANES) {
         if (lane == 0) s_sum[wave] = sum;
         __syncthreads();
         sum = s_sum[0];
@@ -149,8 +152,8 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void add_norm_kernel(NormRowArgs
         } else {
 #pragma unroll
             for (int i = 1; i < NV; ++i) most[0] = fmaxf(most[0], most[i]);
-            most[0] = reduce_64(most[0], [](float p, float q) { return fmaxf(p, q); });
-            if (!WAVE) {
+            most[0] = reduce_lanes<LANES>(most[0], [](float p, float q) { return fmaxf(p, q); });
+            if (!LANES) {
                 if (lane == 0) s_max[wave] = most[0];
                 __syncthreads();
                 for (int w = 0; w < waves; ++w) most[0] = fmaxf(most[0], s_max[w]);
@@ -175,11 +178,15 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void add_norm_kernel(NormRowArgs
 
 template <typename T, typename R, bool BYTES, int N>
 int launch_add_norm(const NormRowArgs &a, const RowShape &s, hipStream_t stream) {
-    if (s.wave) add_norm_kernel<T, R, BYTES, N, 1, true><<<dim3((unsigned)(((int64_t)a.rows + 3) / 4)), dim3(256), 0, stream>>>(a);
+    const int each = s.lanes ? 256 / s.lanes : 1;
+    const dim3 grid((unsigned)(((int64_t)a.rows + each - 1) / each));
+    if (s.lanes == 16) add_norm_kernel<T, R, BYTES, N, 1, 16><<<grid, dim3(256), 0, stream>>>(a);
     else if constexpr (N > 1) {
-        if (s.vecs == 1) add_norm_kernel<T, R, BYTES, N, 1, false><<<dim3(a.rows), dim3(s.threads), 0, stream>>>(a);
-        else if (s.vecs == 2) add_norm_kernel<T, R, BYTES, N, 2, false><<<dim3(a.rows), dim3(s.threads), 0, stream>>>(a);
-        else add_norm_kernel<T, R, BYTES, N, 4, false><<<dim3(a.rows), dim3(s.threads), 0, stream>>>(a);
+        if (s.lanes == 32) add_norm_kernel<T, R, BYTES, N, 1, 32><<<grid, dim3(256), 0, stream>>>(a);
+        else if (s.lanes) add_norm_kernel<T, R, BYTES, N, 1, 64><<<grid, dim3(256), 0, stream>>>(a);
+        else if (s.vecs == 1) add_norm_kernel<T, R, BYTES, N, 1, 0><<<grid, dim3(s.threads), 0, stream>>>(a);
+        else if (s.vecs == 2) add_norm_kernel<T, R, BYTES, N, 2, 0><<<grid, dim3(s.threads), 0, stream>>>(a);
+        else add_norm_kernel<T, R, BYTES, N, 4, 0><<<grid, dim3(s.threads), 0, stream>>>(a);
     }
     SR_HIP(hipGetLastError());
     return SR_OK;
@@ -207,7 +214,7 @@ int add_norm(const sr_norm_rows *x, hipStream_t stream) {
         return SR_E_ARG;
     const bool single = dtype == SR_F32 || residual == SR_F32;
     const RowShape shape = norm_shape(x->width, single);
-    if ((int64_t)x->rows * (shape.wave ? 64 : shape.threads) > UINT32_MAX - 255) return SR_E_LIMIT;
+    if ((int64_t)x->rows * shape.threads > UINT32_MAX - 255) return SR_E_LIMIT;
     a.has_x = x->x.data != nullptr;
     a.x = a.has_x ? x->x.data : x->residual.data;
     a.ld_x = a.has_x ? x->x.ld : x->residual.ld;
@@ -225,8 +232,8 @@ int add_norm(const sr_norm_rows *x, hipStream_t stream) {
     a.rows = x->rows;
     a.width = x->width;
     a.e5m2 = x->out.dtype == SR_E5M2;
-    // rows that go column by column are shorter than any block
-    a.block_lanes = block && shape.per_vec > 1 ? block / shape.per_vec : 0;
+    // a block that holds the row is the row
+    a.block_lanes = block && block < x->width ? block / shape.per_vec : 0;
     a.blocks = block ? ceil_div(x->width, block) : 1;
     a.eps = x->eps;
     return with_row_types(dtype, residual, [&](auto *t, auto *r) -> int {

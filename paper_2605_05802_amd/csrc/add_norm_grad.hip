@@ -3,7 +3,7 @@
 // With dy the gradient of the output, h the stored sum, n = h * rstd: g = dy * gain, dh = rstd * (g - n * mean(g n)) + d_total, where
 // d_total arrives at the sum from behind it; d_residual = dh, d_x = dropout(dh), d_gain = sum over rows of dy * n.
 //
-// Memory bounds it: dy, h and d_total read, d_residual and d_x written.  Workgroups (wavefronts, for rows of up to 64 vectors) take
+// Memory bounds it: dy, h and d_total read, d_residual and d_x written.  Workgroups (wavefronts, for rows of up to 64 vectors, two and four at a time up to 32 and 16) take
 // rows in turn, hold the next row's vectors while they reduce and write the one before, and keep their share of d_gain in registers;
 // a second kernel adds the shares up in the order of their numbers, so that the sum is the same bit for bit from call to call.  Of few rows
 // the gain's gradient is added up from the rows themselves, by other workgroups of the same launch.
@@ -78,14 +78,15 @@ struct GradRow {
             h[i].load(total + at[i].c);
             dt[i].load(d_total + at[i].c);
         }
-        rstd = read_uniform(a.rstd + row);
+        rstd = a.rstd[row];
     }
 };
 
-template <typename T, typename R, int N, int NV, bool WAVE>
-__global__ __launch_bounds__(WAVE ? 256 : 1024) void add_norm_grad_kernel(NormGradArgs a) {
+// LANES: of a row that is a part of a wavefront or a whole one; 0: a workgroup
+template <typename T, typename R, int N, int NV, int LANES>
+__global__ __launch_bounds__(LANES ? 256 : 1024) void add_norm_grad_kernel(NormGradArgs a) {
     __shared__ float s_sum[2][16];
-    const int row_blocks = WAVE ? (a.n_parts + 3) / 4 : a.n_parts;
+    const int row_blocks = LANES ? (a.n_parts + 3) / 4 : a.n_parts;
     if ((int)blockIdx.x >= row_blocks) {             // few rows: the gain's gradient from the rows themselves
         __shared__ float s[16][kGainColumns];
         gain_columns(a, (int)blockIdx.x - row_blocks, a.rows, s, [&](int r, int c) {
@@ -94,9 +95,11 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void add_norm_grad_kernel(NormGr
         return;
     }
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
-    const int part = __builtin_amdgcn_readfirstlane(WAVE ? (int)blockIdx.x * 4 + wave : (int)blockIdx.x);
-    if (WAVE && part >= a.n_parts) return;
-    const int first = WAVE ? lane : (int)threadIdx.x, step = WAVE ? 64 : (int)blockDim.x;
+    const int part = __builtin_amdgcn_readfirstlane(LANES ? (int)blockIdx.x * 4 + wave : (int)blockIdx.x);
+    if (LANES && part >= a.n_parts) return;
+    const int first = LANES ? lane & (LANES - 1) : (int)threadIdx.x, step = (int)blockDim.x;
+    constexpr int kBeside = LANES ? 64 / LANES : 1;              // rows beside each other
+    const int begin = part * kBeside + (LANES ? lane / LANES : 0), stride = a.n_parts * kBeside;
     Span at[NV];
     float gain[NV][N], d_gain[NV][N];
 #pragma unroll
@@ -117,11 +120,11 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void add_norm_grad_kernel(NormGr
     const uint64_t key = mask_key(a.mask);
 
     GradRow<T, R, N, NV> next;
-    next.load(a, part, at);
+    next.load(a, min(begin, a.rows - 1), at);
     int turn = 0;
-    for (int row = part; row < a.rows; row += a.n_parts, turn ^= 1) {
+    for (int row = begin; row < a.rows; row += stride, turn ^= 1) {
         const GradRow<T, R, N, NV> x = next;
-        next.load(a, min(row + a.n_parts, a.rows - 1), at);
+        next.load(a, min(row + stride, a.rows - 1), at);
         float g[NV][N], n[NV][N], sum = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -136,8 +139,8 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void add_norm_grad_kernel(NormGr
                 sum += j >= at[i].skip ? g[i][j] * n[i][j] : 0.f;
             }
         }
-        sum = reduce_64(sum, [](float p, float q) { return p + q; });
-        if (!WAVE) {
+        sum = reduce_lanes<LANES>(sum, [](float p, float q) { return p + q; });
+        if (!LANES) {
             if (lane == 0) s_sum[turn][wave] = sum;
             __syncthreads();
             sum = s_sum[turn][0];
@@ -159,6 +162,14 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void add_norm_grad_kernel(NormGr
         }
     }
     if (!a.parts) return;
+    if (kBeside > 1) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            if (kBeside == 4) d_gain[0][j] += __shfl_xor(d_gain[0][j], 16, 64);
+            d_gain[0][j] += __shfl_xor(d_gain[0][j], 32, 64);
+        }
+        if (lane >= LANES) return;
+    }
     float *to = a.parts + (size_t)part * a.width;
 #pragma unroll
     for (int i = 0; i < NV; ++i) store_span<N>(to, at[i], d_gain[i]);
@@ -167,12 +178,14 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void add_norm_grad_kernel(NormGr
 template <typename T, typename R, int N>
 int launch_add_norm_grad(const NormGradArgs &a, const RowShape &s, hipStream_t stream) {
     const int more = a.d_gain && !a.parts ? ceil_div(a.width, kGainColumns) : 0;
-    const dim3 grid((s.wave ? ceil_div(a.n_parts, 4) : a.n_parts) + more);
-    if (s.wave) add_norm_grad_kernel<T, R, N, 1, true><<<grid, dim3(256), 0, stream>>>(a);
+    const dim3 grid((s.lanes ? ceil_div(a.n_parts, 4) : a.n_parts) + more);
+    if (s.lanes == 16) add_norm_grad_kernel<T, R, N, 1, 16><<<grid, dim3(256), 0, stream>>>(a);
     else if constexpr (N > 1) {
-        if (s.vecs == 1) add_norm_grad_kernel<T, R, N, 1, false><<<grid, dim3(s.threads), 0, stream>>>(a);
-        else if (s.vecs == 2) add_norm_grad_kernel<T, R, N, 2, false><<<grid, dim3(s.threads), 0, stream>>>(a);
-        else add_norm_grad_kernel<T, R, N, 4, false><<<grid, dim3(s.threads), 0, stream>>>(a);
+        if (s.lanes == 32) add_norm_grad_kernel<T, R, N, 1, 32><<<grid, dim3(256), 0, stream>>>(a);
+        else if (s.lanes) add_norm_grad_kernel<T, R, N, 1, 64><<<grid, dim3(256), 0, stream>>>(a);
+        else if (s.vecs == 1) add_norm_grad_kernel<T, R, N, 1, 0><<<grid, dim3(s.threads), 0, stream>>>(a);
+        else if (s.vecs == 2) add_norm_grad_kernel<T, R, N, 2, 0><<<grid, dim3(s.threads), 0, stream>>>(a);
+        else add_norm_grad_kernel<T, R, N, 4, 0><<<grid, dim3(s.threads), 0, stream>>>(a);
     }
     SR_HIP(hipGetLastError());
     return SR_OK;

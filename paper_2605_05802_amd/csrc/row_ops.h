@@ -84,6 +84,16 @@ __device__ __forceinline__ void store_span(T *row, const Span &s, const float *x
     }
 }
 
+// Over the lanes of a row: 16 or 32 of them or the wavefront
+template <int LANES, typename F>
+__device__ __forceinline__ float reduce_lanes(float x, F &&f) {
+    if (LANES != 16 && LANES != 32) return reduce_64(x, f);
+    x = reduce_16(x, f);
+    if (LANES == 16) return x;
+    const auto q = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return f(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+
 // ---------------------------------------------------------------------------------------------
 // dropout
 // ---------------------------------------------------------------------------------------------

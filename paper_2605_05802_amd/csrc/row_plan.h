@@ -15,35 +15,40 @@ constexpr int row_vec(int width, bool single) { return width < 8 ? 1 : single ? 
 struct RowShape {
     int per_vec, vecs;       // vectors that a thread holds: 1, 2 or 4
     int threads;             // of a row
-    bool wave;               // a wavefront a row, four rows to a workgroup, no barrier
+    int lanes;               // 16, 32 or 64 where rows are a part of a wavefront or a whole one, 0 where they are workgroups
 };
 constexpr int kMostNormWidth = 16384, kMostDropWidth = 1 << 30, kMostEmbedWidth = 1 << 20;
 
 inline RowShape norm_shape(int width, bool single) {
-    RowShape s{row_vec(width, single), 1, 64, true};
+    RowShape s{row_vec(width, single), 1, 0, 0};
     const int n = ceil_div(width, s.per_vec);
-    if (n <= 64) return s;
-    s.wave = false;
+    if (n <= 64) {
+        s.threads = s.lanes = n <= 16 ? 16 : n <= 32 ? 32 : 64;
+        return s;
+    }
     s.vecs = n <= 512 ? 1 : n <= 1024 ? 2 : 4;
     s.threads = round_up(ceil_div(n, s.vecs), 64);
     return s;
 }
 
-// Rows of the partial sums of a gain's gradient: workgroups (wavefronts, where each has a row of its own) that take rows in turn
+// Rows of the partial sums of a gain's gradient: workgroups (wavefronts, for rows that are not) that take rows in turn.  Workgroups: 1024
+// threads to a compute unit, two at least, while each has two rows under way (16384 rows of 3584 bf16 beside fp32 186 us, with 2048 threads 191;
+// 2500 of 8192 bf16 57 and 70, 30000 of 1031 83 and 91).  Wavefronts: as many as fit (60000 rows of 256 bf16 beside fp32 52 us, with half of them
+// 58, with a quarter 96).
 constexpr int kMostNormParts = 2048;
 inline int norm_grad_parts(int rows, const RowShape &s) {
-    int parts = s.wave ? 2048 : 256 * (2048 / s.threads > 8 ? 8 : 2048 / s.threads);
-    if (parts > kMostNormParts) parts = kMostNormParts;
-    return rows < parts ? rows : parts;
+    const int each = 1024 / (s.lanes ? 64 : s.threads), units = s.lanes ? ceil_div(rows, 64 / s.lanes) : rows;
+    const int parts = s.lanes ? kMostNormParts : 256 * (each > 8 ? 8 : each < 2 ? 2 : each);
+    return units < parts ? units : parts;
 }
-
-// Whether the gradient of a short list of tokens goes row by row of the table: not more workgroups than run at once
-inline bool embed_few(int vocab, int slices) { return ((int64_t)vocab + 15) / 16 * slices <= 512; }
 
 // Few rows: the gain's gradient from the rows themselves, by workgroups for sixteen columns in the same launch
 // (with the call: 256 rows of 256 fp32 8.2 us instead of 10.9, 128 of 3584 bf16 beside fp32 8.2 and 10.7, 512 12.5 and 14.0, 128 of 16384 bf16 32 and 37;
 // 512 of 8192 23.0 and 22.4)
 inline bool gain_grad_direct(int rows, int width) { return rows <= 512 && (int64_t)rows * width <= 1 << 21; }
+
+// Whether the gradient of a short list of tokens goes row by row of the table: not more workgroups than run at once
+inline bool embed_few(int vocab, int slices) { return ((int64_t)vocab + 15) / 16 * slices <= 512; }
 
 // The gradient of an embedding: sorted tokens in spans of kSpanChunks chunks of `chunk`, a wavefront for 64 * per_vec columns of each
 // chunk, a workgroup for those of a span
