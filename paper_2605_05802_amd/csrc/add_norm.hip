@@ -192,6 +192,7 @@ int launch_add_norm(const NormRowArgs &a, const RowShape &s, hipStream_t stream)
     return SR_OK;
 }
 
+static_assert(sizeof(sr_rows) == 24 && sizeof(sr_norm_rows) == 152, "the binding packs them by hand");
 int add_norm(const sr_norm_rows *x, hipStream_t stream) {
     if (!x || x->rows < 0 || x->width < 1 || !std::isfinite(x->eps) || x->eps < 0.f) return SR_E_ARG;
     const int dtype = x->x.dtype, residual = x->residual.dtype;

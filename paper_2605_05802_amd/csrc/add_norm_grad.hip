@@ -191,6 +191,7 @@ int launch_add_norm_grad(const NormGradArgs &a, const RowShape &s, hipStream_t s
     return SR_OK;
 }
 
+static_assert(sizeof(sr_norm_grad_rows) == 176, "the binding packs it by hand");
 int add_norm_grad(const sr_norm_grad_rows *x, void *workspace, size_t workspace_bytes, hipStream_t stream) {
     if (!x || x->rows < 0 || x->width < 1) return SR_E_ARG;
     const int dtype = x->d_out.dtype, residual = x->total.dtype;
@@ -201,7 +202,7 @@ int add_norm_grad(const sr_norm_grad_rows *x, void *workspace, size_t workspace_
     if (x->d_gain && x->d_gain_dtype != dtype && x->d_gain_dtype != SR_F32) return SR_E_ARG;
     if (x->rows > 0 && !x->d_residual.data && !x->d_x.data && !x->d_gain) return SR_E_ARG;
     if (x->width > kMostNormWidth) return SR_E_LIMIT;
-    if (x->d_gain && (uintptr_t)x->d_gain % elem_bytes(x->d_gain_dtype)) return SR_E_ARG;
+    if (x->d_gain && ((uintptr_t)x->d_gain % elem_bytes(x->d_gain_dtype) || x->d_gain == x->gain)) return SR_E_ARG;
     if (x->rows > 0) {
         if (!rows_fit(x->d_out, x->width, SR_F16) || !rows_fit(x->total, x->width, SR_F16)) return SR_E_ARG;
         for (const sr_rows *r : {&x->d_total, &x->d_residual})

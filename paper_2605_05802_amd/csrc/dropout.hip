@@ -8,7 +8,6 @@ namespace sr {
 int mask_args(const sr_mask *m, MaskArgs *a) {
     *a = MaskArgs{0, 0, 0, nullptr, 0, 1.f};
     if (!m) return SR_OK;
-    static_assert(sizeof(sr_mask) == 40, "the binding lays it out by hand");
     if (!(m->p >= 0.f && m->p < 1.f) || (uintptr_t)m->step % 8) return SR_E_ARG;
     uint32_t drop = (uint32_t)((double)m->p * 65536.0 + 0.5);
     if (drop > 65535) drop = 65535;

@@ -196,7 +196,7 @@ def test_add_norm_grad_refusals():
               call(d_out=rows_of(dtype=1)), call(d_out=rows_of(dtype=4)), call(d_total=rows_of(data=12288, dtype=1)), call(d_residual=rows_of(data=16384, dtype=2)),
               call(d_x=rows_of(data=20480, dtype=1)), call(d_x=rows_of(data=20480, ld=1)), call(d_residual=none, d_x=none, d_gain=None),
               call(d_residual=rows_of(data=8192)), call(d_x=rows_of(data=8192)), call(d_x=rows_of(data=16384)), call(d_x=rows_of(data=12288)),
-              call(d_residual=rows_of()), call(d_residual=rows_of(data=12288, ld=128)), call(d_x=rows_of(ld=128)), call(dropout=ctypes.pointer(mask_of(p=-1.0)))):
+              call(d_residual=rows_of()), call(d_gain=FAKE), call(d_residual=rows_of(data=12288, ld=128)), call(d_x=rows_of(ld=128)), call(dropout=ctypes.pointer(mask_of(p=-1.0)))):
         assert r == sr.SR_E_ARG
     wide = {k: rows_of(data=v.data, ld=1 << 15) for k, v in good.items() if isinstance(v, sr.Rows)}
     assert call(width=16385, **wide) == sr.SR_E_LIMIT
@@ -789,3 +789,38 @@ def test_a_training_pass_in_a_graph_and_on_another_stream():
             assert all(torch.equal(p, q) for p, q in zip(out, want[step]))
     b.step.fill_(1)
     assert all(torch.equal(p, q) for p, q in zip(b.run(), want[1]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dropout,norm", [(0.0, False), (0.25, False), (0.0, True), (0.25, True)])
+def test_gradients_of_the_policy_step_s_adapter(dropout, norm):
+    """Against differentiation in 64 bits, at the second update's mask.  A chain of five operators in single precision, products of 1024 terms among them:
+    2-norms within 2000 u."""
+    from paper_2605_05802_amd.policy_step import SHAPE, Adapter
+    gen = rng(4)
+    rows, rank = 300, 16
+    a = Adapter(rank, 3, dropout, norm)
+    a.step.fill_(1)
+    a.B.copy_(torch.randn(rank, SHAPE.vocab, generator=gen, device="cuda"))
+    if norm:
+        a.gain.copy_(1 + 0.3 * torch.randn(rank, generator=gen, device="cuda"))
+    before = torch.randint(0, 40, (rows,), generator=gen, device="cuda")
+    base, d = torch.randn(rows, SHAPE.vocab, generator=gen, device="cuda"), torch.randn(rows, SHAPE.vocab, generator=gen, device="cuda")
+    logits = a.logits(base, before)
+    got = a.gradients(d, before)
+    leaves = [w.double().requires_grad_(True) for w in a.weights]
+    x = leaves[0][before]
+    if norm:
+        x = x * torch.rsqrt(x.square().mean(1, keepdim=True) + 1e-6) * leaves[3]
+    if dropout:
+        x = x * torch.from_numpy(kept(rows, rank, dropout, 3, step=1)).cuda()
+    want = base.double() + x @ leaves[1] + leaves[2]
+    for g, w in zip([logits, *got], [want.detach(), *torch.autograd.grad((want * d.double()).sum(), leaves)]):
+        assert (g.double() - w).norm() <= 2000 * U * w.norm()
+
+
+@pytest.mark.gpu
+def test_the_policy_step_runs_with_norm_and_dropout():
+    from paper_2605_05802_amd.policy_step import train
+    losses, pair_losses, norms = train(groups=3, G=4, updates=2, pair_updates=1, dropout=0.1, norm=True)
+    assert len(losses) == 2 and all(math.isfinite(x) for x in [*losses, *pair_losses, *norms])
