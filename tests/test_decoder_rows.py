@@ -326,6 +326,16 @@ def test_embed_grad_of_many_tokens(n, width):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("types", [(BF16, BF16), (BF16, F32), (F32, F32)])
+@pytest.mark.parametrize("vocab,width,pad,shift", [(60000, 1031, 0, 0), (60000, 1031, 0, 1), (60001, 1031, 0, 3), (60000, 1031, 5, 1), (50000, 2048, 0, 0),
+                                                   (700000, 64, 0, 7), (700000, 64, 8, 0), (3000000, 24, 1, 0)])
+def test_embed_grad_of_large_tables(types, vocab, width, pad, shift):
+    """Tables that are filled with zeros before the sums are written, at any address and distance of rows."""
+    for n in (0, 1, 777, 9000):
+        check_embed_grad(rng(vocab + n), n, vocab, width, *types, pad=pad, shift=shift, hot=0.3, outside=0.1)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("n,hot", [(300, 0.2), (5000, 0.5), (20000, 0.9)])
 def test_embed_grad_is_the_same_every_time(n, hot):
     gen = rng(n)
