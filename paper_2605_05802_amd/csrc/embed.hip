@@ -7,7 +7,7 @@
 // The gradient sorts the tokens and keeps equal ones in order.  The sorted list is cut into chunks of equal length whatever
 // tokens they hold, so that a token of half the batch is as well spread as any: a wavefront adds up a chunk's rows, 64 vectors of columns, and
 // writes the sums of the tokens that lie in its chunk alone.  Sums of tokens that reach over an end are joined in LDS by the workgroup that has
-// four chunks next to each other, and those that reach over its ends by a second kernel, by way of the workspace.
+// kSpanChunks chunks next to each other, and those that reach over its ends by a second kernel, by way of the workspace.
 #include <cmath>
 
 #include "row_ops.h"
@@ -136,7 +136,8 @@ struct EmbedGradArgs {
     uint32_t *counts;                // [tiles][kDigits]
     float *parts;                    // [spans][2][width]: sums of the token that comes in from the span before, and of the one that goes on
     int n, vocab, width, chunk, spans, slices, sum_blocks;
-    int zero_rows;                   // of the table, a wavefront that writes zeros
+    int zero_rows;                   // of the table, a workgroup that writes zeros
+    FastDiv by_vecs;                 // vectors of a row
 
     int accumulate;
     float scale;
@@ -354,29 +355,35 @@ __device__ __forceinline__ void write_row(const EmbedGradArgs &a, uint32_t token
 
 // The first sum_blocks workgroups add up spans of chunks, a wavefront a chunk and slice of columns; the others write the zeros of a whole table
 template <typename T, typename O, int N>
-__global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a) {
+__global__ __launch_bounds__(64 * kSpanChunks) void embed_sum_kernel(EmbedGradArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     if ((int)blockIdx.x >= a.sum_blocks) {
-        __shared__ uint32_t s_named[4];
-        const int64_t first = ((int64_t)((int)blockIdx.x - a.sum_blocks) * 4 + wave) * a.zero_rows;
-        if (first >= a.vocab) return;
-        const uint32_t from = (uint32_t)first, to = min(from + (uint32_t)a.zero_rows, (uint32_t)a.vocab);
-        if (lane == 0) s_named[wave] = 0;
-        // 64 places of the list at a time, then those behind the last token seen
-        for (uint32_t next = from;;) {
-            const int at = first_at_least(a.sorted, a.n, next, lane) + lane;
-            const uint32_t token = at < a.n ? a.sorted[at] : kNoToken;
-            if (token < to) atomicOr(&s_named[wave], 1u << (token - from));
-            next = __builtin_amdgcn_readlane(token, 63) + 1;
-            if (next >= to) break;                   // kNoToken among them
+        __shared__ int s_bound[2];
+        __shared__ uint8_t s_named[kMostZeroRows];
+        const uint32_t from = ((uint32_t)blockIdx.x - (uint32_t)a.sum_blocks) * (uint32_t)a.zero_rows;
+        const int rows = (int)min((uint32_t)a.zero_rows, (uint32_t)a.vocab - from);
+        // the part of the list with these rows, and each of them in it
+        if (wave < 2) {
+            const int at = first_at_least(a.sorted, a.n, from + (wave ? rows : 0), lane);
+            if (lane == 0) s_bound[wave] = at;
         }
-        const uint32_t named = __builtin_amdgcn_readfirstlane(*(volatile uint32_t *)&s_named[wave]);
+        __syncthreads();
+        const int end = s_bound[1];
+        if ((int)threadIdx.x < rows) {
+            int lo = s_bound[0], hi = end;
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (a.sorted[mid] < from + threadIdx.x) lo = mid + 1;
+                else hi = mid;
+            }
+            s_named[threadIdx.x] = lo < end && a.sorted[lo] == from + threadIdx.x;
+        }
+        __syncthreads();
         const float zero[N] = {};
         const int vecs = (a.width + N - 1) / N;
-        for (uint32_t r = from; r < to; ++r) {
-            if (named >> (r - from) & 1) continue;
-            O *row = (O *)a.d_table + r * a.ld_d_table;
-            for (int v = lane; v < vecs; v += 64) store_span<N>(row, span_of<N>(v, a.width), zero);
+        for (int i = threadIdx.x; i < rows * vecs; i += 64 * kSpanChunks) {
+            const int r = quotient(i, a.by_vecs);
+            if (!s_named[r]) store_span<N>((O *)a.d_table + (from + r) * a.ld_d_table, span_of<N>(i - r * vecs, a.width), zero);
         }
         return;
     }
@@ -477,7 +484,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGradArgs a) {
 }
 
 // Tokens that reach over the ends of spans: the workgroup of the span that one begins in adds up its parts, each wavefront a run of them
-constexpr int kJoinWaves = 4;
+constexpr int kJoinWaves = 8;
 template <typename O, int N>
 __global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(EmbedGradArgs a) {
     __shared__ float s_sum[kJoinWaves][N][64];
@@ -627,9 +634,10 @@ int launch_embed_grad(EmbedGradArgs a, hipStream_t stream) {
     }
     if (a.n > 0) SR_TRY(launch_sort(a, stream));
     a.sum_blocks = a.spans * a.slices;
-    const int zero_blocks = a.accumulate || zeros_first ? 0 : ceil_div(ceil_div(a.vocab, a.zero_rows), 4);
+    a.by_vecs = fast_div(ceil_div(a.width, N));
+    const int zero_blocks = a.accumulate || zeros_first ? 0 : ceil_div(a.vocab, a.zero_rows);
     if (a.sum_blocks + zero_blocks == 0) return SR_OK;
-    embed_sum_kernel<T, O, N><<<dim3((unsigned)a.sum_blocks + (unsigned)zero_blocks), dim3(256), 0, stream>>>(a);
+    embed_sum_kernel<T, O, N><<<dim3((unsigned)a.sum_blocks + (unsigned)zero_blocks), dim3(64 * kSpanChunks), 0, stream>>>(a);
     SR_HIP(hipGetLastError());
     if (a.spans > 1) {
         embed_join_kernel<O, N><<<dim3((unsigned)((a.spans - 1) * a.slices)), dim3(64 * kJoinWaves), 0, stream>>>(a);
@@ -647,7 +655,7 @@ int embed_grad(const sr_rows *d_out, const int32_t *tokens, int n, float scale, 
     if (n > 0 && d_table->data == d_out->data) return SR_E_ARG;
     if (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < SR_EMBED_GRAD_WORKSPACE(n, width)) return SR_E_ARG;
     const EmbedGradPlan p = embed_grad_plan(n, width, d_out->dtype == SR_F32 || d_table->dtype == SR_F32, elem_bytes(d_table->dtype));
-    if ((int64_t)p.spans * p.slices > INT32_MAX / 256 || vocab / p.zero_rows > INT32_MAX / 128) return SR_E_LIMIT;
+    if ((int64_t)p.spans * p.slices > INT32_MAX / 1024 || vocab / p.zero_rows > INT32_MAX / 1024) return SR_E_LIMIT;
     EmbedGradArgs a{};
     a.d_out = d_out->data;
     a.ld_d_out = d_out->ld;

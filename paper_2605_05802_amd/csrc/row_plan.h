@@ -57,11 +57,11 @@ inline bool zeros_go_first(int n, int vocab, int64_t row_bytes) { return ((int64
 
 // The gradient of an embedding: sorted tokens in spans of kSpanChunks chunks of `chunk`, a wavefront for 64 * per_vec columns of each
 // chunk, a workgroup for those of a span
-constexpr int kSpanChunks = 4;
+constexpr int kSpanChunks = 8, kMostZeroRows = 64 * kSpanChunks;
 constexpr int kMostTokens = 1 << 20;
 struct EmbedGradPlan {
     int per_vec, slices, chunk, spans;
-    int zero_rows;           // rows of zeros of a wavefront: about 8 KB of them, and at most 32
+    int zero_rows;           // rows of the table of a workgroup that writes zeros: about 32 KB of them
 };
 inline EmbedGradPlan embed_grad_plan(int n, int width, bool single, int table_bytes) {
     EmbedGradPlan p{};
@@ -70,8 +70,8 @@ inline EmbedGradPlan embed_grad_plan(int n, int width, bool single, int table_by
     const int64_t want = ((int64_t)n * p.slices + 8191) / 8192;      // 8192 wavefronts run at once
     p.chunk = want <= 8 ? 8 : round_up((int)(want < n ? want : n), 8);
     p.spans = ceil_div(n, kSpanChunks * p.chunk);
-    const int rows = 8192 / (table_bytes * (width < 8192 ? width : 8192));
-    p.zero_rows = rows < 1 ? 1 : rows > 32 ? 32 : rows;
+    const int64_t rows = 32768 / ((int64_t)table_bytes * width);
+    p.zero_rows = rows < 4 ? 4 : rows > kMostZeroRows ? kMostZeroRows : (int)rows;
     return p;
 }
 
