@@ -429,19 +429,21 @@ def norm_grad_workspace(rows: int, width: int) -> int:
     return min(rows, 2048) * 4 * width + 256
 
 
-_row_types = _torch_c = None
+class _RowTypes(dict):
+    """torch's element types of rows -> sr_dtype; None for others.  Filled when it is first asked, which saves every later question a call."""
+
+    def __missing__(self, dtype):
+        global _torch_c
+        if not self:
+            import torch
+            _dtypes()
+            _torch_c = torch._C
+            self.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3, torch.float8_e5m2: 4})
+        return self.get(dtype)
+
+
+_row_types, _torch_c = _RowTypes(), None
 _row_calls = {}
-
-
-def _row_dtypes():
-    """torch's element types of rows -> sr_dtype"""
-    global _row_types, _torch_c
-    if _row_types is None:
-        import torch
-        _dtypes()
-        _torch_c = torch._C
-        _row_types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3, torch.float8_e5m2: 4}
-    return _row_types
 
 
 def _row_call(name):
@@ -465,26 +467,29 @@ def _rows(where, what, t, shape):
     """The fields of sr_rows for a tensor [rows, width] with adjacent columns; None: no data."""
     if t is None:
         return _NO_ROWS
-    kind, size = _row_dtypes().get(t.dtype), t.shape
-    if kind is None or size != shape:
-        raise SrError(SR_E_ARG, f"{where}: {what}: {list(shape)} of a floating type expected, got {t.dtype} {tuple(size)}")
+    kind = _row_types[t.dtype]
+    if t.shape != shape or kind is None:
+        raise SrError(SR_E_ARG, f"{where}: {what}: {list(shape)} of a floating type expected, got {t.dtype} {tuple(t.shape)}")
     ld, each = t.stride()
-    if each != 1 and size[1] > 1:
+    if each == 1 and shape[0] > 1:
+        return t.data_ptr(), ld, kind, 0
+    if each != 1 and shape[1] > 1:
         raise SrError(SR_E_ARG, f"{where}: {what}: adjacent columns expected")
-    return t.data_ptr(), ld if size[0] > 1 else max(ld, size[1]), kind, 0
+    return t.data_ptr(), ld if shape[0] > 1 else max(ld, shape[1]), kind, 0
 
 
 def _matrix(where, what, t):
-    if t.dim() != 2:
-        raise SrError(SR_E_ARG, f"{where}: {what}: two dimensions expected, got {tuple(t.shape)}")
-    return t.shape
+    size = t.shape
+    if len(size) != 2:
+        raise SrError(SR_E_ARG, f"{where}: {what}: two dimensions expected, got {tuple(size)}")
+    return size
 
 
 def _vector(where, what, t, n, kinds):
     """(address, sr_dtype) of a contiguous tensor of n elements of one of `kinds`; None: no address."""
     if t is None:
         return 0, 0
-    kind = _row_dtypes().get(t.dtype)
+    kind = _row_types[t.dtype]
     if kind not in kinds or t.numel() != n or not t.is_contiguous():
         raise SrError(SR_E_ARG, f"{where}: {what}: contiguous tensor of {n} elements expected, got {t.dtype} {tuple(t.shape)}")
     return t.data_ptr(), kind

@@ -219,6 +219,7 @@ int add_norm_grad(const sr_norm_grad_rows *x, void *workspace, size_t workspace_
     }
     const bool single = dtype == SR_F32 || residual == SR_F32;
     const RowShape shape = norm_shape(x->width, single);
+    if ((int64_t)x->rows * shape.threads > UINT32_MAX - 255) return SR_E_LIMIT;      // as forward; row numbers then have room above them
     a.n_parts = norm_grad_parts(x->rows, shape);
     if (x->d_gain && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < SR_NORM_GRAD_WORKSPACE(x->rows, x->width))) return SR_E_ARG;
     a.d_out = x->d_out.data;

@@ -193,7 +193,7 @@ __global__ __launch_bounds__(kRankThreads) void rank_kernel(EmbedGradArgs a) {
 // moves the keys.  49153 tokens below 32011: 25 us in two passes (with 256 threads a tile 31); comparing tiles of 2048 with all of
 // themselves and finding every key's place in the other tiles by search took 30, most of it for loads of single words by address.  Up to kOneTile
 // tokens rank_kernel is faster (8192: 22 us with the rest of the call, sorted by digits 32; 4096: 6 us by itself).
-constexpr int kMostDigitBits = 9, kDigits = 1 << kMostDigitBits, kSortTile = 2048, kSortThreads = 512;
+constexpr int kSortThreads = 512;
 static_assert(kSortThreads == kDigits, "a thread a digit");
 constexpr int kSortRounds = kSortTile / kSortThreads, kWaveKeys = kSortTile / (kSortThreads / 64);
 struct SortPass {
@@ -655,19 +655,21 @@ int embed_grad(const sr_rows *d_out, const int32_t *tokens, int n, float scale, 
     if (n > 0 && d_table->data == d_out->data) return SR_E_ARG;
     if (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < SR_EMBED_GRAD_WORKSPACE(n, width)) return SR_E_ARG;
     const EmbedGradPlan p = embed_grad_plan(n, width, d_out->dtype == SR_F32 || d_table->dtype == SR_F32, elem_bytes(d_table->dtype));
-    if ((int64_t)p.spans * p.slices > INT32_MAX / 1024 || vocab / p.zero_rows > INT32_MAX / 1024) return SR_E_LIMIT;
+    if ((int64_t)p.spans * p.slices > INT32_MAX / 1024 || (!accumulate && vocab / p.zero_rows > INT32_MAX / 1024)) return SR_E_LIMIT;
     EmbedGradArgs a{};
     a.d_out = d_out->data;
     a.ld_d_out = d_out->ld;
     a.d_table = d_table->data;
     a.ld_d_table = d_table->ld;
     a.tokens = tokens;
-    a.sorted = (uint32_t *)workspace;
-    a.places = (int32_t *)workspace + n;
-    a.other_sorted = (uint32_t *)workspace + 2 * (size_t)n;
-    a.other_places = (int32_t *)workspace + 3 * (size_t)n;
-    a.counts = (uint32_t *)((char *)workspace + 16 * (size_t)n);
-    a.parts = (float *)((char *)a.counts + (size_t)4 * kDigits * ceil_div(n, kSortTile));
+    const EmbedGradRoom room = embed_grad_room(n, width, p);
+    char *const at = (char *)workspace;
+    a.sorted = (uint32_t *)at;
+    a.places = (int32_t *)(at + room.places);
+    a.other_sorted = (uint32_t *)(at + room.other_sorted);
+    a.other_places = (int32_t *)(at + room.other_places);
+    a.counts = (uint32_t *)(at + room.counts);
+    a.parts = (float *)(at + room.parts);
     a.n = n;
     a.vocab = vocab;
     a.width = width;

@@ -37,7 +37,8 @@ inline RowShape norm_shape(int width, bool single) {
 // 58, with a quarter 96).
 constexpr int kMostNormParts = 2048;
 inline int norm_grad_parts(int rows, const RowShape &s) {
-    const int each = 1024 / (s.lanes ? 64 : s.threads), units = s.lanes ? ceil_div(rows, 64 / s.lanes) : rows;
+    const int each = 1024 / (s.lanes ? 64 : s.threads), some = rows < 4 * kMostNormParts ? rows : 4 * kMostNormParts;
+    const int units = s.lanes ? ceil_div(some, 64 / s.lanes) : some;
     const int parts = s.lanes ? kMostNormParts : 256 * (each > 8 ? 8 : each < 2 ? 2 : each);
     return units < parts ? units : parts;
 }
@@ -73,6 +74,20 @@ inline EmbedGradPlan embed_grad_plan(int n, int width, bool single, int table_by
     const int64_t rows = 32768 / ((int64_t)table_bytes * width);
     p.zero_rows = rows < 4 ? 4 : rows > kMostZeroRows ? kMostZeroRows : (int)rows;
     return p;
+}
+
+// Where things lie in the workspace, in bytes: sorted tokens and their places, the same between passes of the sort, digit counts of every tile, and
+// two rows of partial sums for every span
+constexpr int kMostDigitBits = 9, kDigits = 1 << kMostDigitBits, kSortTile = 2048;
+struct EmbedGradRoom {
+    size_t places, other_sorted, other_places, counts, parts, end;
+};
+inline EmbedGradRoom embed_grad_room(int n, int width, const EmbedGradPlan &p) {
+    const size_t list = 4 * (size_t)n;
+    EmbedGradRoom r{list, 2 * list, 3 * list, 4 * list, 0, 0};
+    r.parts = r.counts + (size_t)4 * kDigits * ceil_div(n, kSortTile);
+    r.end = r.parts + (size_t)8 * width * p.spans;
+    return r;
 }
 
 }  // namespace sr

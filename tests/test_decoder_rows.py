@@ -141,7 +141,67 @@ def test_embed_grad_refusals():
     assert call(n=(1 << 20) + 1) == sr.SR_E_LIMIT
     wide = rows_of(ld=1 << 21)
     assert call(d=wide, t=wide, width=(1 << 20) + 1) == sr.SR_E_LIMIT
+    assert call(vocab=(1 << 31) - 1) == sr.SR_E_LIMIT
     assert call(n=0, tokens=None, accumulate=1, d=rows_of(data=None)) == sr.SR_OK            # nothing to add
+
+
+ROW_PLAN = """
+#include "row_plan.h"
+#include "sr.h"
+extern "C" {
+void norm_shape(int width, int single, int *out) {
+    const sr::RowShape s = sr::norm_shape(width, single);
+    out[0] = s.per_vec; out[1] = s.vecs; out[2] = s.threads; out[3] = s.lanes;
+}
+int norm_parts(int rows, int width, int single) { return sr::norm_grad_parts(rows, sr::norm_shape(width, single)); }
+void grad_plan(int n, int width, int single, int bytes, long long *out) {
+    const sr::EmbedGradPlan p = sr::embed_grad_plan(n, width, single, bytes);
+    const sr::EmbedGradRoom r = sr::embed_grad_room(n, width, p);
+    const long long v[] = {p.per_vec, p.slices, p.chunk, p.spans, p.zero_rows, (long long)r.parts, (long long)r.end, (long long)SR_EMBED_GRAD_WORKSPACE(n, width)};
+    for (int i = 0; i < 8; ++i) out[i] = v[i];
+}
+size_t norm_workspace(int rows, int width) { return SR_NORM_GRAD_WORKSPACE(rows, width); }
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def row_plan(tmp_path_factory):
+    import subprocess
+    from paper_2605_05802_amd.build import CSRC, INCLUDE
+    d = tmp_path_factory.mktemp("row_plan")
+    (d / "p.cpp").write_text(ROW_PLAN)
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I" + CSRC, "-I" + INCLUDE, str(d / "p.cpp"), "-o", str(d / "p.so")])
+    lib = ctypes.CDLL(str(d / "p.so"))
+    lib.norm_workspace.restype = ctypes.c_size_t
+    return lib
+
+
+def test_every_width_fits_the_threads_of_its_rows(row_plan):
+    out = (ctypes.c_int * 4)()
+    for single in (0, 1):
+        for width in range(1, 16385):
+            row_plan.norm_shape(width, single, out)
+            per_vec, vecs, threads, lanes = out
+            assert width >= per_vec and threads * vecs * per_vec >= width and vecs in (1, 2, 4)
+            assert (lanes == threads and vecs == 1 and lanes in (16, 32, 64)) if lanes else (threads % 64 == 0 and 64 < threads <= 1024)
+            assert per_vec > 1 or lanes == 16                       # columns one by one: one kernel
+
+
+def test_partial_sums_fit_their_workspaces(row_plan):
+    for width in (1, 7, 64, 65, 256, 257, 1031, 3584, 4097, 16384):
+        for rows in (0, 1, 2, 63, 512, 2047, 2048, 2049, 10 ** 6, 2 ** 31 - 1):
+            for single in (0, 1):
+                parts = row_plan.norm_parts(rows, width, single)
+                assert min(rows, 1) <= parts <= min(rows, 2048) and 4 * parts * width <= row_plan.norm_workspace(rows, width) == sr.norm_grad_workspace(rows, width)
+    out = (ctypes.c_longlong * 8)()
+    for width in (1, 7, 8, 63, 256, 257, 1031, 3584, 16384, 1 << 20):
+        for n in [*range(0, 300), 1023, 2047, 2048, 2049, 4096, 8191, 8192, 8193, 50001, 2 ** 20 - 1, 2 ** 20]:
+            for single, bytes_ in ((0, 2), (1, 4)):
+                row_plan.grad_plan(n, width, single, bytes_, out)
+                per_vec, slices, chunk, spans, zero_rows, parts, end, room = out
+                assert width >= per_vec and slices * 64 * per_vec >= width and spans * 8 * chunk >= n > (spans - 1) * 8 * chunk - (n == 0)
+                assert parts % 16 == 0 and end <= room == sr.embed_grad_workspace(n, width) and 1 <= zero_rows <= 512
 
 
 def mask_of(**k):
@@ -181,6 +241,7 @@ def test_add_norm_refusals():
     wide = {k: rows_of(data=v.data, ld=1 << 15) for k, v in good.items() if isinstance(v, sr.Rows)}
     assert call(width=16385, **wide) == sr.SR_E_LIMIT
     assert call(width=16384, rows=(1 << 31) - 1, **wide) == sr.SR_E_LIMIT
+    assert call(width=1, rows=(1 << 31) - 1) == sr.SR_E_LIMIT
     assert call(rows=0) == sr.SR_OK
 
 
@@ -200,6 +261,8 @@ def test_add_norm_grad_refusals():
         assert r == sr.SR_E_ARG
     wide = {k: rows_of(data=v.data, ld=1 << 15) for k, v in good.items() if isinstance(v, sr.Rows)}
     assert call(width=16385, **wide) == sr.SR_E_LIMIT
+    assert call(width=16384, rows=(1 << 31) - 1, **wide) == sr.SR_E_LIMIT
+    assert call(width=1, rows=(1 << 31) - 1) == sr.SR_E_LIMIT
 
 
 def test_the_binding_refuses_host_tensors_and_other_shapes():
@@ -333,6 +396,40 @@ def test_embed_grad_of_large_tables(types, vocab, width, pad, shift):
     """Tables that are filled with zeros before the sums are written, at any address and distance of rows."""
     for n in (0, 1, 777, 9000):
         check_embed_grad(rng(vocab + n), n, vocab, width, *types, pad=pad, shift=shift, hot=0.3, outside=0.1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,vocab,width,accumulate", [(200, 100, 64, False), (5000, 300, 72, False), (5000, 300, 72, True), (9001, 1000, 40, False), (30000, 50, 33, False),
+                                                      (3000, 60000, 1031, False), (12000, 100000, 520, False)])
+def test_embed_grad_in_graphs_that_run_beside_each_other(n, vocab, width, accumulate):
+    """Two captured calls, a workspace each, replayed on two streams at once over tokens that change; each gives what an eager call does."""
+    gen = rng(n)
+    calls = []
+    for k in range(2):
+        tokens, d = some_tokens(gen, n, vocab, hot=0.4 * k, outside=0.1), torch.randn(n, width, generator=gen, device="cuda")
+        table, ws = torch.zeros(vocab, width, device="cuda"), torch.empty(sr.embed_grad_workspace(n, width), dtype=torch.uint8, device="cuda")
+        call = lambda t=tokens, d=d, table=table, ws=ws: sr.sr_embed_grad(d, t, table, ws, accumulate=accumulate)
+        call()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        calls.append((tokens, table, call, graph, torch.cuda.Stream()))
+    for turn in range(3):
+        want = []
+        for tokens, table, call, graph, stream in calls:
+            tokens.copy_(some_tokens(gen, n, vocab, hot=0.3 * turn, outside=0.1))
+            table.fill_(1.0)
+            call()
+            want.append(table.clone())
+            table.fill_(1.0)
+        torch.cuda.synchronize()
+        for tokens, table, call, graph, stream in calls:
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for w, (tokens, table, call, graph, stream) in zip(want, calls):
+            assert torch.equal(table, w)
 
 
 @pytest.mark.gpu
