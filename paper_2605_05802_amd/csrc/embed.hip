@@ -8,6 +8,9 @@
 // tokens they hold, so that a token of half the batch is as well spread as any: a wavefront adds up a chunk's rows, 64 vectors of columns, and
 // writes the sums of the tokens that lie in its chunk alone.  Sums of tokens that reach over an end are joined in LDS by the workgroup that has
 // kSpanChunks chunks next to each other, and those that reach over its ends by a second kernel, by way of the workspace.
+//
+// 4096 tokens into a whole table of 152064 x 3584 bf16: 190 us, of which zeros take 160, the sort 6, sums 18 and 5; 49153 tokens, half of
+// them one, into 32011 x 1031 fp32: 85 us, 25 + 55 + 5.
 #include <cmath>
 
 #include "row_ops.h"
