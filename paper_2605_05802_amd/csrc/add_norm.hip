@@ -190,7 +190,7 @@ int launch_add_norm(const NormRowArgs &a, const RowShape &s, hipStream_t stream)
         else if (s.lanes) add_norm_kernel<T, R, BYTES, N, 1, 64><<<grid, dim3(256), 0, stream>>>(a);
         else if (s.vecs == 1) add_norm_kernel<T, R, BYTES, N, 1, 0><<<grid, dim3(s.threads), 0, stream>>>(a);
         else if (s.vecs == 2) add_norm_kernel<T, R, BYTES, N, 2, 0><<<grid, dim3(s.threads), 0, stream>>>(a);
-        else add_norm_kernel<T, R, BYTES, N, 4, 0><<<grid, dim3(s.threads), 0, stream>>>(a);
+        else if constexpr (N == 4) add_norm_kernel<T, R, BYTES, N, 4, 0><<<grid, dim3(s.threads), 0, stream>>>(a);
     }
     SR_HIP(hipGetLastError());
     return SR_OK;

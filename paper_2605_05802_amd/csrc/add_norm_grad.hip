@@ -120,12 +120,15 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void add_norm_grad_kernel(NormG
     }
     const uint64_t key = mask_key(a.mask);
 
+    // the next row's vectors beside this one's, where registers hold both
+    constexpr bool kAhead = N * NV <= 8;
     GradRow<T, R, N, NV> next;
-    next.load(a, min(begin, a.rows - 1), at);
+    if (kAhead) next.load(a, min(begin, a.rows - 1), at);
     int turn = 0;
     for (int row = begin; row < a.rows; row += stride, turn ^= 1) {
+        if (!kAhead) next.load(a, row, at);
         const GradRow<T, R, N, NV> x = next;
-        next.load(a, min(row + stride, a.rows - 1), at);
+        if (kAhead) next.load(a, min(row + stride, a.rows - 1), at);
         float g[NV][N], n[NV][N], sum = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -186,7 +189,7 @@ int launch_add_norm_grad(const NormGradArgs &a, const RowShape &s, hipStream_t s
         else if (s.lanes) add_norm_grad_kernel<T, R, N, 1, 64><<<grid, dim3(256), 0, stream>>>(a);
         else if (s.vecs == 1) add_norm_grad_kernel<T, R, N, 1, 0><<<grid, dim3(s.threads), 0, stream>>>(a);
         else if (s.vecs == 2) add_norm_grad_kernel<T, R, N, 2, 0><<<grid, dim3(s.threads), 0, stream>>>(a);
-        else add_norm_grad_kernel<T, R, N, 4, 0><<<grid, dim3(s.threads), 0, stream>>>(a);
+        else if constexpr (N == 4) add_norm_grad_kernel<T, R, N, 4, 0><<<grid, dim3(s.threads), 0, stream>>>(a);
     }
     SR_HIP(hipGetLastError());
     return SR_OK;
