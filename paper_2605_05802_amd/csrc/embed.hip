@@ -393,7 +393,9 @@ __global__ __launch_bounds__(64 * kSpanChunks) void embed_sum_kernel(EmbedGradAr
     __shared__ float s_sum[kSpanChunks][2][N][64];
     __shared__ uint32_t s_token[kSpanChunks];
     __shared__ int s_kind[kSpanChunks];
-    const int span = (int)blockIdx.x / a.slices, slice = (int)blockIdx.x - span * a.slices;
+    // the slices of a span to one XCD, one soon after the other: they share lines where rows do not begin with one
+    const int octet = (int)blockIdx.x / (8 * a.slices), rest = (int)blockIdx.x - octet * 8 * a.slices, slice = rest >> 3, span = octet * 8 + (rest & 7);
+    if (span >= a.spans) return;
     const Span s = span_of<N>(slice * 64 + lane, a.width);
     const int from = (span * kSpanChunks + wave) * a.chunk, to = min(from + a.chunk, a.n);
     // what becomes of the chunk's first and last sum: kHead, it comes in from before; kTail, a later one goes on behind the chunk;
@@ -636,7 +638,7 @@ int launch_embed_grad(EmbedGradArgs a, hipStream_t stream) {
         SR_TRY((launch_embed<O, O, N>(zeros, stream)));
     }
     if (a.n > 0) SR_TRY(launch_sort(a, stream));
-    a.sum_blocks = a.spans * a.slices;
+    a.sum_blocks = round_up(a.spans, 8) * a.slices;
     a.by_vecs = fast_div(ceil_div(a.width, N));
     const int zero_blocks = a.accumulate || zeros_first ? 0 : ceil_div(a.vocab, a.zero_rows);
     if (a.sum_blocks + zero_blocks == 0) return SR_OK;
