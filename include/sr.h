@@ -487,7 +487,8 @@ int sr_dropout(const sr_rows *x, const sr_rows *residual, const sr_rows *out, in
  * out of type T, or in 8 bits with scales: for each block of scale_block columns (32, 64 or 128; the last one of a row may be shorter), or
  * for each row (0), scale = max(largest |out| of the block / largest finite value of the type, 2^-126), and the stored code is out / scale,
  * rounded to nearest even.  NaN does not enter the scale; its code is NaN.
- * A row whose squares' sum is beyond single precision has rstd 0, one whose squares all vanish in it 1 / sqrt(eps).
+ * A row whose squares' sum is beyond single precision has rstd 0, one whose squares all vanish in it 1 / sqrt(eps): with eps 0 infinity,
+ * and NaN where the row is 0.
  * SR_E_ARG: null pointers (rstd, total and dropout may be NULL), bad types, sizes, strides or options, eps < 0 or not finite;
  * SR_E_LIMIT: width > 16384, more than 2^32 - 1 threads.  rows may be 0.
  */

@@ -551,6 +551,8 @@ class Dropout:
 def sr_dropout(x, out, dropout: Dropout, *, residual=None, stream=None):
     """out = dropout(x), or residual + dropout(x).  x: [rows, width] of float32, bfloat16 or float16; residual: the same type or float32; out: of
     the residual's type, or x's; may be x or the residual itself.  The backward pass is the same call on the gradient."""
+    if not isinstance(dropout, Dropout):
+        raise SrError(SR_E_ARG, "sr_dropout: dropout: a Dropout expected")
     n, width = size = _matrix("sr_dropout", "x", x)
     rows, to = _rows("sr_dropout", "x", x, size), _rows("sr_dropout", "out", out, size)
     add = None if residual is None else _pack_rows(*_rows("sr_dropout", "residual", residual, size))

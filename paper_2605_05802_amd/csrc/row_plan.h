@@ -65,7 +65,8 @@ constexpr int kSpanChunks = 8, kMostZeroRows = 64 * kSpanChunks;
 constexpr int kMostTokens = 1 << 20;
 struct EmbedGradPlan {
     int per_vec, slices, chunk, spans;
-    int zero_rows;           // rows of the table of a workgroup that writes zeros: about 32 KB of them
+    int zero_rows;           // rows of the table of a workgroup that writes zeros: about 64 KB of them (76000 tokens into 152064 x 1024
+                             // fp32 184 us, with 32 KB, and so twice the searches, 204)
 };
 inline EmbedGradPlan embed_grad_plan(int n, int width, bool single, int table_bytes) {
     EmbedGradPlan p{};
@@ -74,7 +75,7 @@ inline EmbedGradPlan embed_grad_plan(int n, int width, bool single, int table_by
     const int64_t want = ((int64_t)n * p.slices + 8191) / 8192;      // 8192 wavefronts run at once
     p.chunk = want <= 8 ? 8 : round_up((int)(want < n ? want : n), 8);
     p.spans = ceil_div(n, kSpanChunks * p.chunk);
-    const int64_t rows = 32768 / ((int64_t)table_bytes * width);
+    const int64_t rows = 65536 / ((int64_t)table_bytes * width);
     p.zero_rows = rows < 4 ? 4 : rows > kMostZeroRows ? kMostZeroRows : (int)rows;
     return p;
 }

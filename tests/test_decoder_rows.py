@@ -280,6 +280,7 @@ def test_the_binding_refuses_host_tensors_and_other_shapes():
             (lambda: sr.sr_embed_grad(z(4, 8), tok, z(10, 8), ws[::2]), "workspace"),
             (lambda: sr.sr_dropout(z(4, 8), z(4, 8), sr.Dropout(0.1, 1)), "device tensors"),
             (lambda: sr.sr_dropout(z(4, 8), z(4, 8), sr.Dropout(0.1, 1), residual=z(4, 9)), "residual"),
+            (lambda: sr.sr_dropout(z(4, 8), z(4, 8), 0.1), "a Dropout"),
             (lambda: sr.Dropout(1.0, 1), "p < 1"), (lambda: sr.Dropout(0.1, 1, step=z(1, t=torch.int64)), "step"),
             (lambda: sr.sr_add_norm(z(4, 8), z(8), z(4, 8)), "device tensors"),
             (lambda: sr.sr_add_norm(z(4, 8), z(9), z(4, 8)), "gain"),
@@ -779,6 +780,34 @@ def test_rows_that_lie_further_apart_than_32_bits_reach():
     sr.sr_embed_grad(x, tokens, w, ws)
     sr.sr_embed_grad(a, tokens, e, ws)
     assert torch.equal(w, e)
+
+
+@pytest.mark.gpu
+def test_a_stream_that_is_named():
+    """The calls go where `stream` says: work of that stream before them is seen, and the current stream does not wait."""
+    gen = rng(6)
+    n, width, vocab = 3000, 320, 500
+    d, tokens = torch.randn(n, width, generator=gen, device="cuda"), some_tokens(gen, n, vocab)
+    gain, drop = torch.randn(width, generator=gen, device="cuda"), sr.Dropout(0.3, 2)
+    ws = torch.empty(max(sr.embed_grad_workspace(n, width), sr.norm_grad_workspace(n, width)), dtype=torch.uint8, device="cuda")
+    E = lambda *s: torch.zeros(*s, device="cuda")
+
+    def run(x, stream):
+        out, total, rstd, dx, dg, table, rows = E(n, width), E(n, width), E(n), E(n, width), E(width), E(vocab, width), E(n, width)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            x.mul_(2.0)
+        sr.sr_dropout(x, x, drop, stream=stream)
+        sr.sr_add_norm(d, gain, out, x=x, total=total, rstd=rstd, stream=stream)
+        sr.sr_add_norm_grad(x, total, rstd, gain, ws, d_x=dx, d_gain=dg, stream=stream.cuda_stream)
+        sr.sr_embed_grad(dx, tokens, table, ws, stream=stream)
+        sr.sr_embed(table, tokens, rows, stream=stream)
+        stream.synchronize()
+        return out, dg, table, rows
+    x = torch.randn(n, width, generator=gen, device="cuda")
+    want = run(x.clone(), torch.cuda.current_stream())
+    got = run(x.clone(), torch.cuda.Stream())
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
 
 
 class Block:
