@@ -10,7 +10,7 @@
 // kSpanChunks chunks next to each other, and those that reach over its ends by a second kernel, by way of the workspace.
 //
 // 4096 tokens into a whole table of 152064 x 3584 bf16: 190 us, of which zeros take 160, the sort 6, sums 18 and 5; 49153 tokens, half of
-// them one, into 32011 x 1031 fp32: 85 us, 25 + 55 + 5.
+// them one, into 32011 x 1031 fp32: 83 us, 25 + 53 + 5.
 #include <cmath>
 
 #include "row_ops.h"
@@ -393,7 +393,8 @@ __global__ __launch_bounds__(64 * kSpanChunks) void embed_sum_kernel(EmbedGradAr
     __shared__ float s_sum[kSpanChunks][2][N][64];
     __shared__ uint32_t s_token[kSpanChunks];
     __shared__ int s_kind[kSpanChunks];
-    // the slices of a span to one XCD, one soon after the other: they share lines where rows do not begin with one
+    // the slices of a span to one XCD, one soon after the other: they share lines where rows do not begin with one (rows
+    // of 1031 halves: 104 MB read instead of 130)
     const int octet = (int)blockIdx.x / (8 * a.slices), rest = (int)blockIdx.x - octet * 8 * a.slices, slice = rest >> 3, span = octet * 8 + (rest & 7);
     if (span >= a.spans) return;
     const Span s = span_of<N>(slice * 64 + lane, a.width);

@@ -36,7 +36,7 @@ inline RowShape norm_shape(int width, bool single) {
 
 // Rows of the partial sums of a gain's gradient: workgroups (wavefronts, for rows that are not) that take rows in turn.  Workgroups: 1024
 // threads to a compute unit, two at least, while each has two rows under way (16384 rows of 3584 bf16 beside fp32 186 us, with 2048 threads 191;
-// 2500 of 8192 bf16 57 and 70, 30000 of 1031 83 and 91).  Wavefronts: as many as fit (60000 rows of 256 bf16 beside fp32 52 us, with half of them
+// 30000 of 1031 83 and 91).  Wavefronts: as many as fit (60000 rows of 256 bf16 beside fp32 52 us, with half of them
 // 58, with a quarter 96).
 constexpr int kMostNormParts = 2048;
 inline int norm_grad_parts(int rows, const RowShape &s) {
