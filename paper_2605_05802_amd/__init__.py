@@ -448,34 +448,32 @@ _row_calls = {}
 
 def _row_call(name):
     """An entry point that takes its structures as packed bytes: structures of ctypes cost a call of five tensors 4 us more."""
-    call = _row_calls.get(name)
-    if call is None:
-        call = lib()[name]           # a function object of its own, apart from the one with typed pointers
-        call.argtypes = [ctypes.c_void_p if issubclass(t, ctypes._Pointer) else t for t in getattr(lib(), name).argtypes]
-        call.restype = ctypes.c_int
-        _row_calls[name] = call
+    call = lib()[name]               # a function object of its own, apart from the one with typed pointers
+    call.argtypes = [ctypes.c_void_p if issubclass(t, ctypes._Pointer) else t for t in getattr(lib(), name).argtypes]
+    call.restype = ctypes.c_int
+    _row_calls[name] = call
     return call
 
 
-_NO_ROWS = (0, 0, 0, 0)              # sr_rows without data
 _pack_rows = struct.Struct("Pqii").pack
-_pack_norm = struct.Struct("Pqii" * 4 + "PPPPiiiifi").pack
-_pack_norm_grad = struct.Struct("Pqii" * 5 + "PPPPiiiiii").pack
+_pack_norm = struct.Struct("PPPPiiiifi").pack              # what follows the rows of sr_norm_rows
+_pack_norm_grad = struct.Struct("PPPPiiiiii").pack         # and of sr_norm_grad_rows
+_NO_ROWS = bytes(24)                 # sr_rows without data
 
 
 def _rows(where, what, t, shape):
-    """The fields of sr_rows for a tensor [rows, width] with adjacent columns; None: no data."""
+    """sr_rows, as bytes, of a tensor [rows, width] with adjacent columns; None: no data."""
     if t is None:
         return _NO_ROWS
     kind = _row_types[t.dtype]
     if t.shape != shape or kind is None:
         raise SrError(SR_E_ARG, f"{where}: {what}: {list(shape)} of a floating type expected, got {t.dtype} {tuple(t.shape)}")
     ld, each = t.stride()
-    if each == 1 and shape[0] > 1:
-        return t.data_ptr(), ld, kind, 0
-    if each != 1 and shape[1] > 1:
-        raise SrError(SR_E_ARG, f"{where}: {what}: adjacent columns expected")
-    return t.data_ptr(), ld if shape[0] > 1 else max(ld, shape[1]), kind, 0
+    if each != 1 or shape[0] < 2:    # where there is one row or column, its distance says nothing
+        if each != 1 and shape[1] > 1:
+            raise SrError(SR_E_ARG, f"{where}: {what}: adjacent columns expected")
+        ld = ld if shape[0] > 1 else max(ld, shape[1])
+    return _pack_rows(t.data_ptr(), ld, kind, 0)
 
 
 def _matrix(where, what, t):
@@ -485,25 +483,26 @@ def _matrix(where, what, t):
     return size
 
 
-def _vector(where, what, t, n, kinds):
-    """(address, sr_dtype) of a contiguous tensor of n elements of one of `kinds`; None: no address."""
+def _vector(where, what, t, n, last=0):
+    """(address, sr_dtype) of a contiguous tensor of n elements of a type up to `last`; None: no address."""
     if t is None:
         return 0, 0
     kind = _row_types[t.dtype]
-    if kind not in kinds or t.numel() != n or not t.is_contiguous():
+    if kind is None or kind > last or t.numel() != n or not t.is_contiguous():
         raise SrError(SR_E_ARG, f"{where}: {what}: contiguous tensor of {n} elements expected, got {t.dtype} {tuple(t.shape)}")
     return t.data_ptr(), kind
 
 
-def _launch_on(where, stream, *tensors):
-    """The stream's handle; all tensors have to be of the current device, where the library launches."""
-    device = tensors[0].get_device()
-    for t in tensors:
-        if t is not None and (device < 0 or t.get_device() != device):
-            raise SrError(SR_E_ARG, f"{where}: device tensors expected, all of one device")
+def _launch_on(where, stream, device, *others):
+    """The stream's handle; `device` and those of the other tensors have to be the current one, where the library launches."""
+    for t in others:
+        if t is not None and t.get_device() != device:
+            device = -1
+    if device < 0:
+        raise SrError(SR_E_ARG, f"{where}: device tensors expected, all of one device")
     if device != _torch_c._cuda_getDevice():
         raise SrError(SR_E_ARG, f"{where}: tensors of the current device expected")
-    return _stream(stream) if stream is not None else _torch_c._cuda_getCurrentRawStream(device)
+    return _torch_c._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
 
 
 def sr_embed(table, tokens, out, *, scale=1.0, stream=None):
@@ -513,8 +512,10 @@ def sr_embed(table, tokens, out, *, scale=1.0, stream=None):
     vocab, width = size = _matrix("sr_embed", "table", table)
     rows, to = _rows("sr_embed", "table", table, size), _rows("sr_embed", "out", out, (n, width))
     ids = _of_type(tokens, "i4", n, "sr_embed: tokens")
-    _check(_row_call("sr_embed")(_pack_rows(*rows), vocab, width, ids, n, scale, _pack_rows(*to), _launch_on("sr_embed", stream, table, tokens, out)),
-           "sr_embed")
+    handle = _launch_on("sr_embed", stream, table.get_device(), tokens, out)
+    status = (_row_calls.get("sr_embed") or _row_call("sr_embed"))(rows, vocab, width, ids, n, scale, to, handle)
+    if status:
+        _check(status, "sr_embed")
 
 
 def sr_embed_grad(d_out, tokens, d_table, workspace, *, scale=1.0, accumulate=False, stream=None):
@@ -526,8 +527,10 @@ def sr_embed_grad(d_out, tokens, d_table, workspace, *, scale=1.0, accumulate=Fa
     rows, to = _rows("sr_embed_grad", "d_out", d_out, (n, width)), _rows("sr_embed_grad", "d_table", d_table, size)
     ids = _of_type(tokens, "i4", n, "sr_embed_grad: tokens")
     ws, room = _workspace("sr_embed_grad", workspace)
-    _check(_row_call("sr_embed_grad")(_pack_rows(*rows), ids, n, scale, _pack_rows(*to), vocab, width, bool(accumulate), ws, room,
-                                      _launch_on("sr_embed_grad", stream, d_table, tokens, d_out, workspace)), "sr_embed_grad")
+    handle = _launch_on("sr_embed_grad", stream, d_table.get_device(), tokens, d_out, workspace)
+    status = (_row_calls.get("sr_embed_grad") or _row_call("sr_embed_grad"))(rows, ids, n, scale, to, vocab, width, bool(accumulate), ws, room, handle)
+    if status:
+        _check(status, "sr_embed_grad")
 
 
 class Dropout:
@@ -555,9 +558,11 @@ def sr_dropout(x, out, dropout: Dropout, *, residual=None, stream=None):
         raise SrError(SR_E_ARG, "sr_dropout: dropout: a Dropout expected")
     n, width = size = _matrix("sr_dropout", "x", x)
     rows, to = _rows("sr_dropout", "x", x, size), _rows("sr_dropout", "out", out, size)
-    add = None if residual is None else _pack_rows(*_rows("sr_dropout", "residual", residual, size))
-    handle = _launch_on("sr_dropout", stream, x, out, residual, dropout.step)
-    _check(_row_call("sr_dropout")(_pack_rows(*rows), add, _pack_rows(*to), n, width, dropout.address, handle), "sr_dropout")
+    add = None if residual is None else _rows("sr_dropout", "residual", residual, size)
+    handle = _launch_on("sr_dropout", stream, x.get_device(), out, residual, dropout.step)
+    status = (_row_calls.get("sr_dropout") or _row_call("sr_dropout"))(rows, add, to, n, width, dropout.address, handle)
+    if status:
+        _check(status, "sr_dropout")
 
 
 def sr_add_norm(residual, gain, out, *, x=None, total=None, rstd=None, scales=None, scale_block=0, dropout=None, eps=1e-6, stream=None):
@@ -569,14 +574,23 @@ def sr_add_norm(residual, gain, out, *, x=None, total=None, rstd=None, scales=No
     where = "sr_add_norm"
     n, width = size = _matrix(where, "residual", residual)
     r, o, t = _rows(where, "residual", residual, size), _rows(where, "out", out, size), _rows(where, "total", total, size)
-    g, kind = _vector(where, "gain", gain, width, (0, 1, 2))
-    # the type of the rest, where there is no branch: the output's, if that is none of 8 bits
-    a = _rows(where, "x", x, size) if x is not None else (0, 0, o[2] if o[2] <= 2 else kind or r[2], 0)
-    blocks = n if scale_block == 0 else n * (-(-width // scale_block)) if scale_block > 0 else -1
-    handle = _launch_on(where, stream, residual, gain, out, x, total, rstd, scales, None if dropout is None else dropout.step)
-    args = _pack_norm(*a, *r, *t, *o, g, _vector(where, "rstd", rstd, n, (0,))[0], _vector(where, "scales", scales, blocks, (0,))[0],
-                      0 if dropout is None else dropout.address, kind, n, width, scale_block, eps, 0)
-    _check(_row_call(where)(args, handle), where)
+    g, kind = _vector(where, "gain", gain, width, 2)
+    if x is not None:
+        a = _rows(where, "x", x, size)
+    else:                            # the type of the rest: the output's, if that is none of 8 bits
+        to = _row_types[out.dtype]
+        a = _pack_rows(0, 0, to if to <= 2 else kind or _row_types[residual.dtype], 0)
+    sums, s, mask, step = 0, 0, 0, None
+    if rstd is not None:
+        sums = _vector(where, "rstd", rstd, n)[0]
+    if scales is not None:
+        s = _vector(where, "scales", scales, n if scale_block == 0 else n * (-(-width // scale_block)) if scale_block > 0 else -1)[0]
+    if dropout is not None:
+        mask, step = dropout.address, dropout.step
+    handle = _launch_on(where, stream, residual.get_device(), gain, out, x, total, rstd, scales, step)
+    status = (_row_calls.get(where) or _row_call(where))(a + r + t + o + _pack_norm(g, sums, s, mask, kind, n, width, scale_block, eps, 0), handle)
+    if status:
+        _check(status, where)
 
 
 def sr_add_norm_grad(d_out, total, rstd, gain, workspace, *, d_total=None, d_residual=None, d_x=None, d_gain=None, dropout=None,
@@ -586,14 +600,20 @@ def sr_add_norm_grad(d_out, total, rstd, gain, workspace, *, d_total=None, d_res
     workspace: device bytes, norm_grad_workspace(rows, width) of them; None where d_gain is."""
     where = "sr_add_norm_grad"
     n, width = size = _matrix(where, "d_out", d_out)
-    g, kind = _vector(where, "gain", gain, width, (0, 1, 2))
-    to, to_kind = _vector(where, "d_gain", d_gain, width, (0, 1, 2))
-    ws, room = _workspace(where, workspace) if workspace is not None else (None, 0)
-    args = _pack_norm_grad(*_rows(where, "d_out", d_out, size), *_rows(where, "total", total, size), *_rows(where, "d_total", d_total, size),
-                           *_rows(where, "d_residual", d_residual, size), *_rows(where, "d_x", d_x, size), _vector(where, "rstd", rstd, n, (0,))[0], g, to,
-                           0 if dropout is None else dropout.address, kind, to_kind, n, width, bool(accumulate), 0)
-    handle = _launch_on(where, stream, d_out, total, rstd, gain, workspace, d_total, d_residual, d_x, d_gain, None if dropout is None else dropout.step)
-    _check(_row_call(where)(args, ws, room, handle), where)
+    g, kind = _vector(where, "gain", gain, width, 2)
+    to, to_kind = _vector(where, "d_gain", d_gain, width, 2)
+    ws, room, mask, step = None, 0, 0, None
+    if workspace is not None:
+        ws, room = _workspace(where, workspace)
+    if dropout is not None:
+        mask, step = dropout.address, dropout.step
+    args = (_rows(where, "d_out", d_out, size) + _rows(where, "total", total, size) + _rows(where, "d_total", d_total, size) +
+            _rows(where, "d_residual", d_residual, size) + _rows(where, "d_x", d_x, size) +
+            _pack_norm_grad(_vector(where, "rstd", rstd, n)[0], g, to, mask, kind, to_kind, n, width, bool(accumulate), 0))
+    handle = _launch_on(where, stream, d_out.get_device(), total, rstd, gain, workspace, d_total, d_residual, d_x, d_gain, step)
+    status = (_row_calls.get(where) or _row_call(where))(args, ws, room, handle)
+    if status:
+        _check(status, where)
 
 
 def sr_probe_hbm(src, dst, mode: int, iters: int = 10, stream=None) -> float:
