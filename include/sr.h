@@ -444,8 +444,8 @@ int sr_embed(const sr_rows *table, int vocab, int width, const int32_t *tokens, 
 
 /*
  * Its gradient:  d_table[v] = scale * sum of d_out[i] over all i with tokens[i] = v, zeros for every other v; with accumulate != 0 this is
- * added to what d_table holds, and rows of tokens that do not occur are not touched.  Sums run over ascending i, in parts of a length that
- * depends on n and width alone.  d_out [n][width] of type T, d_table [vocab][width] of T or SR_F32.
+ * added to what d_table holds, and rows of tokens that do not occur are not touched.  Sums run over ascending i, in parts whose length
+ * depends on sizes and types alone.  d_out [n][width] of type T, d_table [vocab][width] of T or SR_F32.
  * workspace: device memory, 16-byte aligned, SR_EMBED_GRAD_WORKSPACE(n, width) bytes; nothing in it outlives the call, and calls that
  * may overlap (different streams) need one each.
  * SR_E_ARG as above; SR_E_LIMIT: n > 2^20 (a larger batch goes in parts that accumulate), width > 2^20, too many rows for a launch.

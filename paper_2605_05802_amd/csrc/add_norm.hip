@@ -121,7 +121,7 @@ __global__ __launch_bounds__(LANES ? 256 : 1024) void add_norm_kernel(NormRowArg
         }
         if (a.total) store_span<N>((R *)a.total + row * a.ld_total, at[i], h[i]);
 #pragma unroll
-        for (int j = 0; j < N; ++j) sum += j >= at[i].skip ? h[i][j] * h[i][j] : 0.f;
+        for (int j = 0; j < N; ++j) sum = j >= at[i].skip ? fmaf(h[i][j], h[i][j], sum) : sum;
     }
     sum = reduce_lanes<LANES>(sum, [](float p, float q) { return p + q; });
     if (!LANES) {

@@ -132,8 +132,8 @@ __device__ __forceinline__ void drop_out(const MaskRow &m, int c, bool ragged, f
         w[0] >>= 16 * (c & 3);
     } else if (ragged) {
         const int shift = 16 * (c & 3);
-        const uint64_t more = smx_finalize(at + (uint64_t)kWords * kGolden);
-        if (shift) {
+        if (shift) {                                 // a row's last vector alone: no lane of most wavefronts
+            const uint64_t more = smx_finalize(at + (uint64_t)kWords * kGolden);
 #pragma unroll
             for (int i = 0; i < kWords; ++i) w[i] = w[i] >> shift | (i + 1 < kWords ? w[i + 1] : more) << (64 - shift);
         }
