@@ -136,7 +136,7 @@ struct EmbedGradArgs {
     int32_t *places;                 // [n] and where they came from
     uint32_t *other_sorted;          // the same between passes of the sort
     int32_t *other_places;
-    uint32_t *counts;                // [tiles][kDigits]
+    uint32_t *counts;                // of digits, of every tile
     float *parts;                    // [spans][2][width]: sums of the token that comes in from the span before, and of the one that goes on
     int n, vocab, width, chunk, spans, slices, sum_blocks;
     int zero_rows;                   // of the table, a workgroup that writes zeros
@@ -197,7 +197,6 @@ __global__ __launch_bounds__(kRankThreads) void rank_kernel(EmbedGradArgs a) {
 // themselves and finding every key's place in the other tiles by search took 30, most of it for loads of single words by address.  Up to kOneTile
 // tokens rank_kernel is faster (8192: 22 us with the rest of the call, sorted by digits 32; 4096: 6 us by itself).
 constexpr int kSortThreads = 512;
-static_assert(kSortThreads == kDigits, "a thread a digit");
 constexpr int kSortRounds = kSortTile / kSortThreads, kWaveKeys = kSortTile / (kSortThreads / 64);
 struct SortPass {
     const int32_t *tokens;           // of the first pass, else null
@@ -205,7 +204,7 @@ struct SortPass {
     const int32_t *places;
     uint32_t *to_keys;
     int32_t *to_places;
-    uint32_t *counts;                // [tiles][kDigits]
+    uint32_t *counts;                // [tiles][2^BITS]
     int n, tiles, vocab, shift, bits, last;
 };
 // Tokens outside the vocabulary sort as `vocab`, behind all others; the last pass makes kNoToken of it
@@ -213,9 +212,12 @@ __device__ __forceinline__ uint32_t sort_key(const SortPass &p, int i) {
     return p.tokens ? min(key_of(p.tokens[i], p.vocab), (uint32_t)p.vocab) : p.keys[i];
 }
 
+// BITS: that a digit has at most
+template <int BITS>
 __global__ __launch_bounds__(kSortThreads) void digit_count_kernel(SortPass p) {
+    constexpr int kDigits = 1 << BITS;
     __shared__ uint32_t s_count[kDigits];
-    s_count[threadIdx.x] = 0;
+    for (int d = threadIdx.x; d < kDigits; d += kSortThreads) s_count[d] = 0;
     __syncthreads();
     const int first = (int)blockIdx.x * kSortTile + (int)threadIdx.x;
     uint32_t key[kSortRounds];
@@ -225,11 +227,14 @@ __global__ __launch_bounds__(kSortThreads) void digit_count_kernel(SortPass p) {
     for (int r = 0; r < kSortRounds; ++r)
         if (first + r * kSortThreads < p.n) atomicAdd(&s_count[key[r] >> p.shift & ((1u << p.bits) - 1)], 1u);
     __syncthreads();
-    p.counts[(size_t)blockIdx.x * kDigits + threadIdx.x] = s_count[threadIdx.x];
+    for (int d = threadIdx.x; d < kDigits; d += kSortThreads) p.counts[(size_t)blockIdx.x * kDigits + d] = s_count[d];
 }
 
+template <int BITS>
 __global__ __launch_bounds__(kSortThreads) void digit_move_kernel(SortPass p) {
-    constexpr int kWaves = kSortThreads / 64;
+    constexpr int kWaves = kSortThreads / 64, kDigits = 1 << BITS, kEach = kDigits / kSortThreads, kAhead = 16 / kEach;
+    static_assert(kEach == 1 || kEach == 4, "digits of a thread, side by side");
+    typedef std::conditional_t<kEach == 1, uint32_t, raw16> Counts;
     __shared__ uint32_t s_at[kWaves][kDigits];       // counts of a wavefront's keys, then the place of its next one
     __shared__ uint32_t s_sum[kWaves];
     const int tile = (int)blockIdx.x, wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63;
@@ -242,27 +247,33 @@ __global__ __launch_bounds__(kSortThreads) void digit_move_kernel(SortPass p) {
         key[r] = sort_key(p, at);
         place[r] = p.tokens ? at : p.places[at];
     }
-    // a digit a thread: how many there are, and in the tiles before
-    uint32_t all = 0, before = 0;
-    const uint32_t *counts = p.counts + threadIdx.x;
-    for (int t = 0; t < p.tiles; t += 16) {
-        uint32_t c[16];
+    // of each of the thread's digits: how many there are, and in the tiles before
+    Counts all = {}, before = {};
+    const Counts *counts = (const Counts *)p.counts + threadIdx.x;
+    for (int t = 0; t < p.tiles; t += kAhead) {
+        Counts c[kAhead];
 #pragma unroll
-        for (int u = 0; u < 16; ++u) c[u] = counts[(size_t)min(t + u, p.tiles - 1) * kDigits];
+        for (int u = 0; u < kAhead; ++u) c[u] = counts[(size_t)min(t + u, p.tiles - 1) * kSortThreads];
 #pragma unroll
-        for (int u = 0; u < 16; ++u) {
-            all += t + u < p.tiles ? c[u] : 0;
-            before += t + u < tile ? c[u] : 0;
+        for (int u = 0; u < kAhead; ++u) {
+            all += c[u] * (uint32_t)(t + u < p.tiles);
+            before += c[u] * (uint32_t)(t + u < tile);
         }
     }
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) s_at[w][threadIdx.x] = 0;
+    const auto of = [](const Counts &c, int q) __attribute__((always_inline)) -> uint32_t {
+        if constexpr (kEach == 1) return c;
+        else return c[q];
+    };
+    for (int i = threadIdx.x; i < kWaves * kDigits; i += kSortThreads) (&s_at[0][0])[i] = 0;
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kSortRounds; ++r)
         if (first + r * 64 < p.n) atomicAdd(&s_at[wave][key[r] >> p.shift & ((1u << p.bits) - 1)], 1u);
     // keys of smaller digits
-    uint32_t sum = all;
+    uint32_t own = 0;
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) own += of(all, q);
+    uint32_t sum = own;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
         const uint32_t y = __shfl_up(sum, off, 64);
@@ -270,13 +281,19 @@ __global__ __launch_bounds__(kSortThreads) void digit_move_kernel(SortPass p) {
     }
     if (lane == 63) s_sum[wave] = sum;
     __syncthreads();
-    uint32_t at = sum - all + before;
-    for (int w = 0; w < wave; ++w) at += s_sum[w];
+    uint32_t base = sum - own;
+    for (int w = 0; w < wave; ++w) base += s_sum[w];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        const uint32_t c = s_at[w][threadIdx.x];
-        s_at[w][threadIdx.x] = at;
-        at += c;
+    for (int q = 0; q < kEach; ++q) {
+        uint32_t at = base + of(before, q);
+        base += of(all, q);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            uint32_t &to = s_at[w][threadIdx.x * kEach + q];
+            const uint32_t c = to;
+            to = at;
+            at += c;
+        }
     }
     __syncthreads();
     // 64 keys after the other: those of a digit among them in order, by comparing digits bit by bit.  (Counted so as well, instead of by atomics, the
@@ -306,7 +323,11 @@ int launch_sort(const EmbedGradArgs &a, hipStream_t stream) {
         SR_HIP(hipGetLastError());
         return SR_OK;
     }
-    const int bits = 32 - __builtin_clz((unsigned)a.vocab), passes = ceil_div(bits, kMostDigitBits), each = ceil_div(bits, passes);
+    // digits of nine bits, and of eleven where those save a pass: a vocabulary below 2048 takes one, of 2^18 to 2^22 two (9000 tokens below 1024: 19.5 us
+    // with the rest of the call, in two passes 24.6)
+    const int bits = 32 - __builtin_clz((unsigned)a.vocab);
+    const bool eleven = ceil_div(bits, kMostDigitBits) < ceil_div(bits, 9);
+    const int passes = ceil_div(bits, eleven ? kMostDigitBits : 9), each = ceil_div(bits, passes);
     SortPass p{a.tokens, nullptr, nullptr, nullptr, nullptr, a.counts, a.n, ceil_div(a.n, kSortTile), a.vocab, 0, each, 0};
     for (int k = 0; k < passes; ++k) {
         const bool end = (passes - 1 - k) % 2 == 0;              // the last pass leaves the list where it is read
@@ -314,9 +335,11 @@ int launch_sort(const EmbedGradArgs &a, hipStream_t stream) {
         p.to_places = end ? a.places : a.other_places;
         p.shift = k * each;
         p.last = k + 1 == passes;
-        digit_count_kernel<<<dim3(p.tiles), dim3(kSortThreads), 0, stream>>>(p);
+        if (eleven) digit_count_kernel<11><<<dim3(p.tiles), dim3(kSortThreads), 0, stream>>>(p);
+        else digit_count_kernel<9><<<dim3(p.tiles), dim3(kSortThreads), 0, stream>>>(p);
         SR_HIP(hipGetLastError());
-        digit_move_kernel<<<dim3(p.tiles), dim3(kSortThreads), 0, stream>>>(p);
+        if (eleven) digit_move_kernel<11><<<dim3(p.tiles), dim3(kSortThreads), 0, stream>>>(p);
+        else digit_move_kernel<9><<<dim3(p.tiles), dim3(kSortThreads), 0, stream>>>(p);
         SR_HIP(hipGetLastError());
         p.tokens = nullptr;
         p.keys = p.to_keys;

@@ -82,14 +82,14 @@ inline EmbedGradPlan embed_grad_plan(int n, int width, bool single, int table_by
 
 // Where things lie in the workspace, in bytes: sorted tokens and their places, the same between passes of the sort, digit counts of every tile, and
 // two rows of partial sums for every span
-constexpr int kMostDigitBits = 9, kDigits = 1 << kMostDigitBits, kSortTile = 2048;
+constexpr int kMostDigitBits = 11, kSortTile = 2048;
 struct EmbedGradRoom {
     size_t places, other_sorted, other_places, counts, parts, end;
 };
 inline EmbedGradRoom embed_grad_room(int n, int width, const EmbedGradPlan &p) {
     const size_t list = 4 * (size_t)n;
     EmbedGradRoom r{list, 2 * list, 3 * list, 4 * list, 0, 0};
-    r.parts = r.counts + (size_t)4 * kDigits * ceil_div(n, kSortTile);
+    r.parts = r.counts + ((size_t)4 << kMostDigitBits) * ceil_div(n, kSortTile);
     r.end = r.parts + (size_t)8 * width * p.spans;
     return r;
 }
