@@ -476,11 +476,27 @@ def _rows(where, what, t, shape):
     return _pack_rows(t.data_ptr(), ld, kind, 0)
 
 
+_MOST = 2 ** 31 - 1                  # what an int of the C boundary holds: ctypes passes the low 32 bits of more, without a word
+
+
+def _beyond(where, what, n):
+    raise SrError(SR_E_LIMIT, f"{where}: {what}: 2**31 - 1 at most, got {n}")
+
+
 def _matrix(where, what, t):
     size = t.shape
     if len(size) != 2:
         raise SrError(SR_E_ARG, f"{where}: {what}: two dimensions expected, got {tuple(size)}")
+    if size[0] > _MOST or size[1] > _MOST:
+        _beyond(where, what, tuple(size))
     return size
+
+
+def _token_count(where, tokens):
+    n = tokens.numel()
+    if n > _MOST:
+        _beyond(where, "tokens", n)
+    return n
 
 
 def _vector(where, what, t, n, last=0):
@@ -508,7 +524,7 @@ def _launch_on(where, stream, device, *others):
 def sr_embed(table, tokens, out, *, scale=1.0, stream=None):
     """out[i] = scale * table[tokens[i]], zeros where the token lies outside the table.  table: [vocab, width] of float32, bfloat16 or
     float16; tokens int32 [n]; out: [n, width] of the table's type or float32."""
-    n = tokens.numel()
+    n = _token_count("sr_embed", tokens)
     vocab, width = size = _matrix("sr_embed", "table", table)
     rows, to = _rows("sr_embed", "table", table, size), _rows("sr_embed", "out", out, (n, width))
     ids = _of_type(tokens, "i4", n, "sr_embed: tokens")
@@ -522,7 +538,7 @@ def sr_embed_grad(d_out, tokens, d_table, workspace, *, scale=1.0, accumulate=Fa
     """d_table[v] = scale * sum of d_out[i] over tokens[i] = v, in a fixed order; accumulate: added to what d_table holds, whose other rows are
     not touched.  d_out: [n, width] of float32, bfloat16 or float16; d_table: [vocab, width] of the same type or float32;
     workspace: device bytes, embed_grad_workspace(n, width) of them."""
-    n = tokens.numel()
+    n = _token_count("sr_embed_grad", tokens)
     vocab, width = size = _matrix("sr_embed_grad", "d_table", d_table)
     rows, to = _rows("sr_embed_grad", "d_out", d_out, (n, width)), _rows("sr_embed_grad", "d_table", d_table, size)
     ids = _of_type(tokens, "i4", n, "sr_embed_grad: tokens")

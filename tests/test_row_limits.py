@@ -1,0 +1,72 @@
+"""The row operators at the ends of what their arguments can say, without a GPU: stand-ins of tensors whose addresses are never read."""
+import pytest
+import torch
+
+import paper_2605_05802_amd as sr
+
+MANY = 1 << 32                         # its low 32 bits are 0: no rows
+
+
+class Stub:
+    """What the binding asks a tensor for."""
+    is_cuda = True
+    nbytes = 1 << 40
+
+    def __init__(self, *shape, dtype=torch.float32):
+        self.shape, self.dtype = torch.Size(shape), dtype
+
+    def numel(self):
+        return self.shape.numel()
+
+    def stride(self, d=None):
+        s = [1]
+        for n in self.shape[:0:-1]:
+            s.insert(0, s[0] * n)
+        return tuple(s) if d is None else s[d]
+
+    def dim(self):
+        return len(self.shape)
+
+    def data_ptr(self):
+        return 4096 * (1 + id(self) % 997)
+
+    def is_contiguous(self):
+        return True
+
+    def get_device(self):
+        return 0
+
+
+@pytest.fixture
+def on_any_device(monkeypatch):
+    monkeypatch.setattr(sr, "_launch_on", lambda *a: 0)
+
+
+def f(*shape, dtype=torch.float32):
+    return Stub(*shape, dtype=dtype)
+
+
+def i4(n):
+    return Stub(n, dtype=torch.int32)
+
+
+WS = Stub(1 << 20, dtype=torch.uint8)
+BEYOND = {
+    "embed, tokens": lambda: sr.sr_embed(f(10, 1), i4(MANY), f(MANY, 1)),
+    "embed, vocabulary": lambda: sr.sr_embed(f(MANY + 10, 1), i4(0), f(0, 1)),
+    "embed, just beyond": lambda: sr.sr_embed(f(10, 1), i4(1 << 31), f(1 << 31, 1)),
+    "embed_grad, tokens": lambda: sr.sr_embed_grad(f(MANY, 1), i4(MANY), f(10, 1), WS, accumulate=True),
+    "embed_grad, vocabulary": lambda: sr.sr_embed_grad(f(0, 1), i4(0), f(MANY + 10, 1), WS, accumulate=True),
+    "dropout, rows": lambda: sr.sr_dropout(f(MANY, 1), f(MANY, 1), sr.Dropout(0.1, 1)),
+    "dropout, columns": lambda: sr.sr_dropout(f(0, MANY + 4), f(0, MANY + 4), sr.Dropout(0.1, 1)),
+    "add_norm, rows": lambda: sr.sr_add_norm(f(MANY, 1), f(1), f(MANY, 1)),
+    "add_norm_grad, rows": lambda: sr.sr_add_norm_grad(f(MANY, 1), f(MANY, 1), f(MANY), f(1), None, d_x=f(MANY, 1)),
+}
+
+
+@pytest.mark.parametrize("call", BEYOND)
+def test_sizes_that_32_bits_do_not_hold_are_refused(on_any_device, call):
+    """Not taken modulo 2^32: 2^32 + 5 rows are no call of five."""
+    with pytest.raises(sr.SrError, match=r"2\*\*31 - 1") as e:
+        BEYOND[call]()
+    assert e.value.status == sr.SR_E_LIMIT
