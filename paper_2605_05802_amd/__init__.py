@@ -196,6 +196,26 @@ def _check(status: int, where: str):
         raise SrError(status, where)
 
 
+_MOST = 2 ** 31 - 1                  # what an int of the C boundary holds: ctypes passes the low 32 bits of more, without a word
+
+
+def _beyond(where, what, n):
+    raise SrError(SR_E_LIMIT, f"{where}: {what}: 2**31 - 1 at most, got {n}")
+
+
+def _int(where, what, n):
+    if n > _MOST:
+        _beyond(where, what, n)
+    return n
+
+
+def _actions(where, actions):
+    """(n_groups, G, stride)"""
+    if max(actions.shape) > _MOST:
+        _beyond(where, "actions", tuple(actions.shape))
+    return actions.shape
+
+
 def _ptr(t):
     """Device (or host) address of a torch tensor / numpy array / None."""
     if t is None:
@@ -218,7 +238,7 @@ def _stream(stream):
 
 def sr_gate_batch(actions, prefix_lens, threshold: float, sums=None, retire=None, stream=None):
     """actions: device int32 [n_groups, G, stride]; sums int32 / retire uint8: device [n_lens, n_groups]."""
-    n_groups, G, stride = actions.shape
+    n_groups, G, stride = _actions("sr_gate_batch", actions)
     lens = (ctypes.c_int * len(prefix_lens))(*prefix_lens)
     _check(lib().sr_gate_batch(_ptr(actions), n_groups, G, stride, lens, len(prefix_lens), threshold,
                                _ptr(sums), _ptr(retire), _stream(stream)), "sr_gate_batch")
@@ -226,7 +246,7 @@ def sr_gate_batch(actions, prefix_lens, threshold: float, sums=None, retire=None
 
 def sr_gate_batch_antidiag(actions, prefix_lens, threshold: float, sums=None, retire=None, stream=None):
     """sr_gate_batch by the anti-diagonal decomposition (same arguments, same results)."""
-    n_groups, G, stride = actions.shape
+    n_groups, G, stride = _actions("sr_gate_batch_antidiag", actions)
     lens = (ctypes.c_int * len(prefix_lens))(*prefix_lens)
     _check(lib().sr_gate_batch_antidiag(_ptr(actions), n_groups, G, stride, lens, len(prefix_lens), threshold,
                                         _ptr(sums), _ptr(retire), _stream(stream)), "sr_gate_batch_antidiag")
@@ -241,7 +261,7 @@ SIGNALS_FIELDS = (("d_K", "f8"), ("lev_scaled", "i8"), ("bigram_jaccard", "f8"),
 def sr_signals_batch(actions, prefix_lens, d_L: float, tau_H: float, out, obs=None, end_step=None, stream=None):
     """actions, obs: device int32 [n_groups, G, stride]; end_step: device int32 [n_groups, G];
     out: device uint8 [n_lens, n_groups, SIGNALS_BYTES] receiving sr_signals_t records."""
-    n_groups, G, stride = actions.shape
+    n_groups, G, stride = _actions("sr_signals_batch", actions)
     lens = (ctypes.c_int * len(prefix_lens))(*prefix_lens)
     _check(lib().sr_signals_batch(_ptr(actions), _ptr(obs), _ptr(end_step), n_groups, G, stride, lens,
                                   len(prefix_lens), d_L, tau_H, _ptr(out), _stream(stream)), "sr_signals_batch")
@@ -250,14 +270,14 @@ def sr_signals_batch(actions, prefix_lens, d_L: float, tau_H: float, out, obs=No
 def sr_grpo_loss(logprob, rewards, G: int, eps: float, advantages, group_scratch, loss, stream=None):
     """logprob: device float64 [n_groups*G]; rewards: device float32, same; advantages: device float32 or None;
     group_scratch: device float64 [n_groups]; loss: device float64 [1]."""
-    n_groups = logprob.numel() // G
+    n_groups = _int("sr_grpo_loss", "groups", logprob.numel() // G)
     _check(lib().sr_grpo_loss(_ptr(logprob), _ptr(rewards), n_groups, G, eps, _ptr(advantages), _ptr(group_scratch),
                               _ptr(loss), _stream(stream)), "sr_grpo_loss")
 
 
 def sr_grpo_loss_static(logprob, rewards, G: int, eps: float, advantages, loss, stream=None):
     """sr_grpo_loss without a workspace argument (the library's fixed device array holds the group shares)."""
-    n_groups = logprob.numel() // G
+    n_groups = _int("sr_grpo_loss_static", "groups", logprob.numel() // G)
     _check(lib().sr_grpo_loss_static(_ptr(logprob), _ptr(rewards), n_groups, G, eps, _ptr(advantages), _ptr(loss),
                                      _stream(stream)), "sr_grpo_loss_static")
 
@@ -306,13 +326,13 @@ def _token_rows(where, logits, targets, seq_start, mask, grad, token_logprob, gr
     dtype = _dtypes().get(logits.dtype)
     if dtype is None or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise SrError(SR_E_ARG, f"{where}: logits: [rows, vocab] of float32, bfloat16 or float16 with adjacent columns expected")
-    n, vocab = logits.shape
+    n, vocab = _int(where, "rows", logits.shape[0]), _int(where, "vocabulary", logits.shape[1])
     ld_grad, to = 0, None
     if grad is not None:
         if grad.shape != logits.shape or grad.dtype is not logits.dtype or (vocab > 1 and grad.stride(1) != 1):
             raise SrError(SR_E_ARG, f"{where}: grad: shape and type of the logits, with adjacent columns, expected")
         ld_grad, to = grad.stride(0) if n > 1 else vocab, grad.data_ptr()
-    n_seq = seq_start.numel() - 1
+    n_seq = _int(where, "sequences", seq_start.numel() - 1)
     return TokenRows(logits.data_ptr(), to, logits.stride(0) if n > 1 else vocab, ld_grad, _of_type(targets, "i4", n, "targets"),
                      _of_type(mask, "u1", n, "mask"), _of_type(seq_start, "i4", n_seq + 1, "seq_start"),
                      _of_type(token_logprob, "f4", n, "token_logprob"), dtype, n, vocab, n_seq, grad_scale, 0), n, n_seq
@@ -476,13 +496,6 @@ def _rows(where, what, t, shape):
     return _pack_rows(t.data_ptr(), ld, kind, 0)
 
 
-_MOST = 2 ** 31 - 1                  # what an int of the C boundary holds: ctypes passes the low 32 bits of more, without a word
-
-
-def _beyond(where, what, n):
-    raise SrError(SR_E_LIMIT, f"{where}: {what}: 2**31 - 1 at most, got {n}")
-
-
 def _matrix(where, what, t):
     size = t.shape
     if len(size) != 2:
@@ -490,13 +503,6 @@ def _matrix(where, what, t):
     if size[0] > _MOST or size[1] > _MOST:
         _beyond(where, what, tuple(size))
     return size
-
-
-def _token_count(where, tokens):
-    n = tokens.numel()
-    if n > _MOST:
-        _beyond(where, "tokens", n)
-    return n
 
 
 def _vector(where, what, t, n, last=0):
@@ -524,7 +530,7 @@ def _launch_on(where, stream, device, *others):
 def sr_embed(table, tokens, out, *, scale=1.0, stream=None):
     """out[i] = scale * table[tokens[i]], zeros where the token lies outside the table.  table: [vocab, width] of float32, bfloat16 or
     float16; tokens int32 [n]; out: [n, width] of the table's type or float32."""
-    n = _token_count("sr_embed", tokens)
+    n = _int("sr_embed", "tokens", tokens.numel())
     vocab, width = size = _matrix("sr_embed", "table", table)
     rows, to = _rows("sr_embed", "table", table, size), _rows("sr_embed", "out", out, (n, width))
     ids = _of_type(tokens, "i4", n, "sr_embed: tokens")
@@ -538,7 +544,7 @@ def sr_embed_grad(d_out, tokens, d_table, workspace, *, scale=1.0, accumulate=Fa
     """d_table[v] = scale * sum of d_out[i] over tokens[i] = v, in a fixed order; accumulate: added to what d_table holds, whose other rows are
     not touched.  d_out: [n, width] of float32, bfloat16 or float16; d_table: [vocab, width] of the same type or float32;
     workspace: device bytes, embed_grad_workspace(n, width) of them."""
-    n = _token_count("sr_embed_grad", tokens)
+    n = _int("sr_embed_grad", "tokens", tokens.numel())
     vocab, width = size = _matrix("sr_embed_grad", "d_table", d_table)
     rows, to = _rows("sr_embed_grad", "d_out", d_out, (n, width)), _rows("sr_embed_grad", "d_table", d_table, size)
     ids = _of_type(tokens, "i4", n, "sr_embed_grad: tokens")
@@ -708,11 +714,11 @@ class Context:
         _check(lib().sr_load_weights(self._h, ctypes.byref(w), _stream(stream)), "sr_load_weights")
 
     def sr_prefill_chunk(self, tokens, shared_per_group: bool, stream=None):
-        _check(lib().sr_prefill_chunk(self._h, _ptr(tokens), tokens.shape[-1], int(shared_per_group),
+        _check(lib().sr_prefill_chunk(self._h, _ptr(tokens), _int("sr_prefill_chunk", "tokens", tokens.shape[-1]), int(shared_per_group),
                                       _stream(stream)), "sr_prefill_chunk")
 
     def sr_score_chunk(self, tokens, action_mask=None, out_token_logprob=None, stream=None):
-        _check(lib().sr_score_chunk(self._h, _ptr(tokens), _ptr(action_mask), tokens.shape[-1],
+        _check(lib().sr_score_chunk(self._h, _ptr(tokens), _ptr(action_mask), _int("sr_score_chunk", "tokens", tokens.shape[-1]),
                                     _ptr(out_token_logprob), _stream(stream)), "sr_score_chunk")
 
     def sr_get_logprob(self, dst, stream=None):

@@ -70,3 +70,50 @@ def test_sizes_that_32_bits_do_not_hold_are_refused(on_any_device, call):
     with pytest.raises(sr.SrError, match=r"2\*\*31 - 1") as e:
         BEYOND[call]()
     assert e.value.status == sr.SR_E_LIMIT
+
+
+@pytest.fixture
+def without_a_stream(monkeypatch):
+    monkeypatch.setattr(sr, "_stream", lambda stream: 0)
+
+
+f8 = lambda n: Stub(n, dtype=torch.float64)
+BEYOND_BEFORE = {                      # the entry points of the update step and of the gate
+    "grpo_loss, groups": lambda: sr.sr_grpo_loss(f8(MANY * 2), f(MANY * 2), 2, 1e-6, f(MANY * 2), f8(MANY), f8(1)),
+    "grpo_loss_static, groups": lambda: sr.sr_grpo_loss_static(f8(MANY * 2), f(MANY * 2), 2, 1e-6, f(MANY * 2), f8(1)),
+    "policy_loss, rows": lambda: sr.sr_policy_loss(f(MANY, 2), i4(MANY), i4(2), f(MANY), f(1), f(4), WS),
+    "policy_loss, vocabulary": lambda: sr.sr_policy_loss(f(1, MANY + 2), i4(1), i4(2), f(1), f(1), f(4), WS),
+    "policy_loss, sequences": lambda: sr.sr_policy_loss(f(1, 2), i4(1), i4(MANY + 2), f(1), f(MANY + 1), f(4), WS),
+    "preference_loss, rows": lambda: sr.sr_preference_loss(f(MANY, 2), i4(MANY), i4(3), f(4), WS),
+    "gate_batch, groups": lambda: sr.sr_gate_batch(Stub(MANY + 1, 2, 1, dtype=torch.int32), [1], 0.5, i4(MANY + 1)),
+    "gate_batch, stride": lambda: sr.sr_gate_batch(Stub(1, 2, MANY + 1, dtype=torch.int32), [1], 0.5, i4(1)),
+    "gate_batch_antidiag, groups": lambda: sr.sr_gate_batch_antidiag(Stub(MANY + 1, 2, 1, dtype=torch.int32), [1], 0.5, i4(MANY + 1)),
+    "signals_batch, groups": lambda: sr.sr_signals_batch(Stub(MANY + 1, 2, 1, dtype=torch.int32), [1], 0.5, 0.0, f(1)),
+}
+
+
+class NothingCalled:
+    def __getattr__(self, name):
+        if name == "sr_strerror":
+            return sr._lib.sr_strerror
+        return lambda *a: sr.SR_OK     # what it was given has gone through ints already, or would have
+
+
+@pytest.mark.parametrize("call", BEYOND_BEFORE)
+def test_sizes_that_32_bits_do_not_hold_are_refused_by_the_losses_and_the_gate(without_a_stream, monkeypatch, call):
+    sr.lib()
+    monkeypatch.setattr(sr, "lib", NothingCalled)
+    with pytest.raises(sr.SrError, match=r"2\*\*31 - 1") as e:
+        BEYOND_BEFORE[call]()
+    assert e.value.status == sr.SR_E_LIMIT
+
+
+def test_chunks_that_32_bits_do_not_hold_are_refused(without_a_stream, monkeypatch):
+    sr.lib()
+    monkeypatch.setattr(sr, "lib", NothingCalled)
+    c = sr.Context.__new__(sr.Context)
+    c._h = 0
+    tokens = Stub(1, MANY + 3, dtype=torch.int32)
+    for call in (lambda: c.sr_prefill_chunk(tokens, False), lambda: c.sr_score_chunk(tokens)):
+        with pytest.raises(sr.SrError, match=r"2\*\*31 - 1"):
+            call()
