@@ -309,8 +309,10 @@ __global__ __launch_bounds__(kSortThreads) void digit_move_kernel(SortPass p) {
         }
         const int rank = __popcll(same & (((uint64_t)1 << lane) - 1));
         const uint32_t to = s_at[wave][digit] + rank;
+        wave_sync();                                 // all lanes have their place, and the first of a digit moves it on for the next round
+        if (here && rank == 0) s_at[wave][digit] = to + __popcll(same);
+        wave_sync();
         if (here) {
-            if (rank == 0) s_at[wave][digit] = to + __popcll(same);
             p.to_keys[to] = p.last && key[r] == (uint32_t)p.vocab ? kNoToken : key[r];
             p.to_places[to] = place[r];
         }

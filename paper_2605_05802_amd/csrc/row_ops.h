@@ -84,6 +84,14 @@ __device__ __forceinline__ void store_span(T *row, const Span &s, const float *x
     }
 }
 
+// What lanes of this wavefront wrote to LDS before is there for its other lanes behind it.  The hardware keeps a wavefront's LDS accesses in
+// order and needs nothing for that; the compiler, which sees one lane, has to be told.  All lanes come here.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Over the lanes of a row: 16 or 32 of them or the wavefront
 template <int LANES, typename F>
 __device__ __forceinline__ float reduce_lanes(float x, F &&f) {

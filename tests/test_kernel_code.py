@@ -42,3 +42,21 @@ def test_shared_blocks_are_read_before_they_are_overwritten(attention_asm, kerne
     for head in heads:
         last = re.findall(r"s_waitcnt[^\n]*", head)[-1]
         assert "lgkmcnt(0)" in last and "vmcnt" in last
+
+
+@pytest.fixture(scope="module")
+def embed_asm(tmp_path_factory):
+    out = tmp_path_factory.mktemp("asm") / "embed.s"
+    r = subprocess.run([HIPCC] + FLAGS + ["--cuda-device-only", "-S", os.path.join(CSRC, "embed.hip"), "-o", str(out)],
+                       capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, r.stderr
+    return out.read_text()
+
+
+@pytest.mark.parametrize("kernel", ["digit_move_kernelILi9E", "digit_move_kernelILi11E"])
+def test_places_that_lanes_hand_to_each_other_are_ordered(embed_asm, kernel):
+    """The sort's rounds of 64 keys hand the place of a digit's next key on through LDS, from the lane that has the digit's first key to the lanes of the
+    next round.  Every load and every store of it lies between wave barriers, which the compiler moves neither over."""
+    body = re.search(r"^_ZN\S*" + kernel + r"\S*:[^\n]*\n(.*?)^\.Lfunc_end", embed_asm, re.S | re.M).group(1)
+    rounds = re.findall(r"ds_read_b32|ds_write_b32|wave barrier", body.split("s_barrier")[-1])
+    assert rounds == ["ds_read_b32", "wave barrier", "ds_write_b32", "wave barrier"] * 4
