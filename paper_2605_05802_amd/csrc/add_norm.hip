@@ -24,7 +24,7 @@ struct NormRowArgs {
     int64_t ld_x, ld_residual, ld_total, ld_out;
     float *rstd, *scales;
     int rows, width;
-    int has_x, gain_single;          // x: read in any case, of the residual's rows where there is none
+    int has_x, gain_single;          // x: read in any case, the gain where there is none
     int e5m2, block_lanes, blocks;   // lanes of a block, 0: the row; blocks of a row
     float eps;
     MaskArgs mask;
@@ -221,8 +221,9 @@ int add_norm(const sr_norm_rows *x, hipStream_t stream) {
     const RowShape shape = norm_shape(x->width, single);
     if ((int64_t)x->rows * shape.threads > UINT32_MAX - 255) return SR_E_LIMIT;
     a.has_x = x->x.data != nullptr;
-    a.x = a.has_x ? x->x.data : x->residual.data;
-    a.ld_x = a.has_x ? x->x.ld : x->residual.ld;
+    const BranchRows branch = branch_rows(x->x.data, x->x.ld, x->gain);
+    a.x = branch.data;
+    a.ld_x = branch.ld;
     if (!a.has_x) a.mask.drop = 0;
     a.residual = x->residual.data;
     a.ld_residual = x->residual.ld;

@@ -34,6 +34,15 @@ inline RowShape norm_shape(int width, bool single) {
     return s;
 }
 
+// A norm without a branch loads its rows' worth of one all the same and leaves it out (the kernel has one form): the gain, again and again, which it
+// reads anyway.  The residual's rows would do where the types are equal; elements of 16 bits beside a residual in single precision lie
+// elsewhere in it, between its rows too.  (16384 rows of 3584 bf16 beside fp32, nothing stored but the norm: 66 us, by way of the residual 71.)
+struct BranchRows {
+    const void *data;
+    int64_t ld;
+};
+inline BranchRows branch_rows(const void *x, int64_t ld, const void *gain) { return x ? BranchRows{x, ld} : BranchRows{gain, 0}; }
+
 // Rows of the partial sums of a gain's gradient: workgroups (wavefronts, for rows that are not) that take rows in turn.  Workgroups: 1024
 // threads to a compute unit, two at least, while each has two rows under way (16384 rows of 3584 bf16 beside fp32 186 us, with 2048 threads 191;
 // 30000 of 1031 83 and 91).  Wavefronts: as many as fit (60000 rows of 256 bf16 beside fp32 52 us, with half of them
