@@ -456,14 +456,16 @@ int sr_embed_grad(const sr_rows *d_out, const int32_t *tokens, int n, float scal
 
 /*
  * Dropout.  Its mask is a function of numbers and is never stored: element (row r, column c) of a batch of `width` columns is dropped iff
- *     (bits >> 16 (c % 4)) % 2^16 < round(65536 p),   bits = word (first_row + r) * ceil(width / 4) + c / 4
+ *     (bits >> 16 (c % 4)) % 2^16 < D,   bits = word (first_row + r) * ceil(width / 4) + c / 4
+ *     D = min(65535, round(65536 p))
  * of the SplitMix64 stream keyed (seed, mask + *step): the same mask forward and backward, whatever the types, strides and the operator,
- * and whatever part of the rows a call is given (first_row).  What is kept is multiplied by 65536 / (65536 - round(65536 p)), the
- * reciprocal of the share that these bits keep; what is dropped is 0, also where the input is not finite.
+ * and whatever part of the rows a call is given (first_row).  What is kept is multiplied by 65536 / (65536 - D), the reciprocal of the
+ * share that these bits keep; what is dropped is 0, also where the input is not finite.  So p below 2^-17 drops nothing, and however near
+ * p is to 1, one element in 65536 is kept.
  * `step` (device, may be NULL) is read when the kernel runs, so that a replayed graph draws another mask at every step.
  */
 typedef struct {
-    float p;                   /* 0 <= p < 1 */
+    float p;                   /* 0 <= p < 1; D / 65536 of it counts */
     uint32_t reserved;
     uint64_t seed;
     uint64_t mask;             /* which mask of that seed: a layer's number, for example */

@@ -557,6 +557,7 @@ def sr_embed_grad(d_out, tokens, d_table, workspace, *, scale=1.0, accumulate=Fa
 
 class Dropout:
     """Which mask: p, a seed, the number of a mask of that seed (a layer's, for example), and the number of the batch's first row.
+    p counts in steps of 2^-16, up to 65535 of them.
     step: device int64 [1], added to `mask` when the kernel runs, for graphs that are replayed; kept alive by this object."""
 
     __slots__ = ("c", "address", "step")

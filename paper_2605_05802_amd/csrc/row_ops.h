@@ -106,7 +106,7 @@ __device__ __forceinline__ float reduce_lanes(float x, F &&f) {
 // dropout
 // ---------------------------------------------------------------------------------------------
 // Element (row, column) of a mask has the 16 bits (column % 4) of word (row * ceil(width / 4) + column / 4) of a SplitMix64 stream, and
-// goes if they are below `drop` = round(65536 p).  16 bits make four elements of a word, whose two 64-bit products are what a mask costs;
+// goes if they are below `drop` = min(65535, round(65536 p)).  16 bits make four elements of a word, whose two 64-bit products are what a mask costs;
 // the kept ones are multiplied by 65536 / (65536 - drop), the reciprocal of the share that these bits keep.
 struct MaskArgs {
     uint64_t seed, which, first_row;
