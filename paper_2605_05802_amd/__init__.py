@@ -611,7 +611,11 @@ def sr_add_norm(residual, gain, out, *, x=None, total=None, rstd=None, scales=No
     if dropout is not None:
         mask, step = dropout.address, dropout.step
     handle = _launch_on(where, stream, residual.get_device(), gain, out, x, total, rstd, scales, step)
-    status = (_row_calls.get(where) or _row_call(where))(a + r + t + o + _pack_norm(g, sums, s, mask, kind, n, width, scale_block, eps, 0), handle)
+    try:
+        rest = _pack_norm(g, sums, s, mask, kind, n, width, scale_block, eps, 0)
+    except struct.error:
+        raise SrError(SR_E_ARG, f"{where}: scale_block {scale_block!r} or eps {eps!r}") from None
+    status = (_row_calls.get(where) or _row_call(where))(a + r + t + o + rest, handle)
     if status:
         _check(status, where)
 

@@ -117,3 +117,10 @@ def test_chunks_that_32_bits_do_not_hold_are_refused(without_a_stream, monkeypat
     for call in (lambda: c.sr_prefill_chunk(tokens, False), lambda: c.sr_score_chunk(tokens)):
         with pytest.raises(sr.SrError, match=r"2\*\*31 - 1"):
             call()
+
+
+@pytest.mark.parametrize("options", [dict(eps=None), dict(eps="1e-6"), dict(scale_block=1 << 40), dict(scale_block=-(1 << 40)), dict(scale_block=32.5)])
+def test_numbers_that_the_norm_s_structure_does_not_hold_are_refused(on_any_device, options):
+    with pytest.raises(sr.SrError, match="eps|scale") as e:
+        sr.sr_add_norm(f(4, 64), f(64), f(4, 64), **options)
+    assert e.value.status == sr.SR_E_ARG
