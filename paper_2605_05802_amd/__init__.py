@@ -574,16 +574,22 @@ class Dropout:
         self.address = ctypes.addressof(self.c)
 
 
+def _mask_of(where, dropout):
+    """(address of its sr_mask, its step or None)"""
+    if not isinstance(dropout, Dropout):
+        raise SrError(SR_E_ARG, f"{where}: dropout: a Dropout expected")
+    return dropout.address, dropout.step
+
+
 def sr_dropout(x, out, dropout: Dropout, *, residual=None, stream=None):
     """out = dropout(x), or residual + dropout(x).  x: [rows, width] of float32, bfloat16 or float16; residual: the same type or float32; out: of
     the residual's type, or x's; may be x or the residual itself.  The backward pass is the same call on the gradient."""
-    if not isinstance(dropout, Dropout):
-        raise SrError(SR_E_ARG, "sr_dropout: dropout: a Dropout expected")
+    mask, step = _mask_of("sr_dropout", dropout)
     n, width = size = _matrix("sr_dropout", "x", x)
     rows, to = _rows("sr_dropout", "x", x, size), _rows("sr_dropout", "out", out, size)
     add = None if residual is None else _rows("sr_dropout", "residual", residual, size)
-    handle = _launch_on("sr_dropout", stream, x.get_device(), out, residual, dropout.step)
-    status = (_row_calls.get("sr_dropout") or _row_call("sr_dropout"))(rows, add, to, n, width, dropout.address, handle)
+    handle = _launch_on("sr_dropout", stream, x.get_device(), out, residual, step)
+    status = (_row_calls.get("sr_dropout") or _row_call("sr_dropout"))(rows, add, to, n, width, mask, handle)
     if status:
         _check(status, "sr_dropout")
 
@@ -609,7 +615,7 @@ def sr_add_norm(residual, gain, out, *, x=None, total=None, rstd=None, scales=No
     if scales is not None:
         s = _vector(where, "scales", scales, n if scale_block == 0 else n * (-(-width // scale_block)) if scale_block > 0 else -1)[0]
     if dropout is not None:
-        mask, step = dropout.address, dropout.step
+        mask, step = _mask_of(where, dropout)
     handle = _launch_on(where, stream, residual.get_device(), gain, out, x, total, rstd, scales, step)
     try:
         rest = _pack_norm(g, sums, s, mask, kind, n, width, scale_block, eps, 0)
@@ -633,7 +639,7 @@ def sr_add_norm_grad(d_out, total, rstd, gain, workspace, *, d_total=None, d_res
     if workspace is not None:
         ws, room = _workspace(where, workspace)
     if dropout is not None:
-        mask, step = dropout.address, dropout.step
+        mask, step = _mask_of(where, dropout)
     args = (_rows(where, "d_out", d_out, size) + _rows(where, "total", total, size) + _rows(where, "d_total", d_total, size) +
             _rows(where, "d_residual", d_residual, size) + _rows(where, "d_x", d_x, size) +
             _pack_norm_grad(_vector(where, "rstd", rstd, n)[0], g, to, mask, kind, to_kind, n, width, bool(accumulate), 0))

@@ -124,3 +124,11 @@ def test_numbers_that_the_norm_s_structure_does_not_hold_are_refused(on_any_devi
     with pytest.raises(sr.SrError, match="eps|scale") as e:
         sr.sr_add_norm(f(4, 64), f(64), f(4, 64), **options)
     assert e.value.status == sr.SR_E_ARG
+
+
+@pytest.mark.parametrize("call", [lambda d: sr.sr_add_norm(f(4, 64), f(64), f(4, 64), dropout=d),
+                                  lambda d: sr.sr_add_norm_grad(f(4, 64), f(4, 64), f(4), f(64), None, d_x=f(4, 64), dropout=d)])
+@pytest.mark.parametrize("dropout", [0.1, True, "0.1", (0.1, 7)])
+def test_the_norms_take_a_dropout_for_a_mask_and_nothing_else(on_any_device, call, dropout):
+    with pytest.raises(sr.SrError, match="a Dropout expected"):
+        call(dropout)
