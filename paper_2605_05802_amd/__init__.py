@@ -453,16 +453,23 @@ class _RowTypes(dict):
     """torch's element types of rows -> sr_dtype; None for others.  Filled when it is first asked, which saves every later question a call."""
 
     def __missing__(self, dtype):
-        global _torch_c
+        global _current_device, _current_handle
         if not self:
             import torch
             _dtypes()
-            _torch_c = torch._C
+            _current_device, _current_handle = _device_calls(torch._C)
             self.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3, torch.float8_e5m2: 4})
         return self.get(dtype)
 
 
-_row_types, _torch_c = _RowTypes(), None
+def _device_calls(torch_c):
+    """The current device, and the handle of a device's current stream: as numbers where torch has functions for these (see _stream), else by its public ones."""
+    import torch
+    return (getattr(torch_c, "_cuda_getDevice", torch.cuda.current_device),
+            getattr(torch_c, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream))
+
+
+_row_types, _current_device, _current_handle = _RowTypes(), None, None
 _row_calls = {}
 
 
@@ -522,9 +529,9 @@ def _launch_on(where, stream, device, *others):
             device = -1
     if device < 0:
         raise SrError(SR_E_ARG, f"{where}: device tensors expected, all of one device")
-    if device != _torch_c._cuda_getDevice():
+    if device != _current_device():
         raise SrError(SR_E_ARG, f"{where}: tensors of the current device expected")
-    return _torch_c._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
+    return _current_handle(device) if stream is None else _stream(stream)
 
 
 def sr_embed(table, tokens, out, *, scale=1.0, stream=None):

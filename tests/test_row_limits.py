@@ -132,3 +132,26 @@ def test_numbers_that_the_norm_s_structure_does_not_hold_are_refused(on_any_devi
 def test_the_norms_take_a_dropout_for_a_mask_and_nothing_else(on_any_device, call, dropout):
     with pytest.raises(sr.SrError, match="a Dropout expected"):
         call(dropout)
+
+
+def test_a_torch_without_its_private_functions(monkeypatch):
+    """The current device and the stream's handle by way of torch's public functions, as in the other entry points."""
+    device, handle = sr._device_calls(object())
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device: type("Stream", (), {"cuda_stream": 4000 + device}))
+    assert device is torch.cuda.current_device and handle(3) == 4003
+
+
+@pytest.mark.gpu
+def test_calls_by_way_of_public_functions(monkeypatch):
+    table, tokens = torch.randn(9, 16, device="cuda"), torch.tensor([3, -1, 8], dtype=torch.int32, device="cuda")
+    out = [torch.empty(3, 16, device="cuda") for _ in range(2)]
+    sr.sr_embed(table, tokens, out[0])
+    device, handle = sr._device_calls(object())
+    monkeypatch.setattr(sr, "_current_device", device)
+    monkeypatch.setattr(sr, "_current_handle", handle)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        sr.sr_embed(table, tokens, out[1])
+    side.synchronize()
+    assert torch.equal(out[0], out[1])
