@@ -450,7 +450,10 @@ int sr_embed(const sr_rows *table, int vocab, int width, const int32_t *tokens, 
  * may overlap (different streams) need one each.
  * SR_E_ARG as above; SR_E_LIMIT: n > 2^20 (a larger batch goes in parts that accumulate), width > 2^20, too many rows for a launch.
  */
-#define SR_EMBED_GRAD_WORKSPACE(n, width) (65536 + (size_t)32 * (size_t)(n) + ((size_t)(n) / 8 + 64) * 4 * (size_t)(width))
+#define SR_EMBED_GRAD_SUMS(n, width) ((size_t)(n) / 8 * 4 * (size_t)(width))
+#define SR_EMBED_GRAD_WORKSPACE(n, width) \
+    (65536 + (size_t)32 * (size_t)(n) + (size_t)256 * (size_t)(width) + \
+     (SR_EMBED_GRAD_SUMS(n, width) < (size_t)1 << 22 ? SR_EMBED_GRAD_SUMS(n, width) : (size_t)1 << 22))
 int sr_embed_grad(const sr_rows *d_out, const int32_t *tokens, int n, float scale, const sr_rows *d_table, int vocab, int width,
                   int accumulate, void *workspace, size_t workspace_bytes, void *stream);
 
@@ -531,7 +534,11 @@ typedef struct {
     const sr_mask *dropout;    /* HOST, NULL: none */
     int32_t gain_dtype, d_gain_dtype, rows, width, accumulate, reserved;
 } sr_norm_grad_rows;
-#define SR_NORM_GRAD_WORKSPACE(rows, width) ((size_t)((rows) < 2048 ? (rows) : 2048) * 4 * (size_t)(width) + 256)
+#define SR_NORM_GRAD_MOST(width) \
+    ((width) <= 1024 ? (size_t)8192 * (size_t)(width) : (width) <= 4096 ? (size_t)1 << 23 : (size_t)2048 * (size_t)(width))
+#define SR_NORM_GRAD_WORKSPACE(rows, width) \
+    (256 + ((size_t)4 * (size_t)(rows) * (size_t)(width) < SR_NORM_GRAD_MOST(width) ? (size_t)4 * (size_t)(rows) * (size_t)(width) \
+                                                                                    : SR_NORM_GRAD_MOST(width)))
 int sr_add_norm_grad(const sr_norm_grad_rows *rows, void *workspace, size_t workspace_bytes, void *stream);
 
 /*

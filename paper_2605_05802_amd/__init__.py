@@ -441,12 +441,12 @@ def sr_clip_grad_norm(tensors, max_norm: float, norm, workspace, *, scale=1.0, s
 
 def embed_grad_workspace(n: int, width: int) -> int:
     """Bytes of workspace for sr_embed_grad (SR_EMBED_GRAD_WORKSPACE)."""
-    return 65536 + 32 * n + (n // 8 + 64) * 4 * width
+    return 65536 + 32 * n + 256 * width + min(n // 8 * 4 * width, 1 << 22)
 
 
 def norm_grad_workspace(rows: int, width: int) -> int:
     """Bytes of workspace for sr_add_norm_grad (SR_NORM_GRAD_WORKSPACE)."""
-    return min(rows, 2048) * 4 * width + 256
+    return 256 + min(4 * rows * width, 8192 * width if width <= 1024 else 1 << 23 if width <= 4096 else 2048 * width)
 
 
 class _RowTypes(dict):

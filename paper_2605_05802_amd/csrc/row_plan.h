@@ -47,6 +47,7 @@ inline BranchRows branch_rows(const void *x, int64_t ld, const void *gain) { ret
 // threads to a compute unit, two at least, while each has two rows under way (16384 rows of 3584 bf16 beside fp32 186 us, with 2048 threads 191;
 // 30000 of 1031 83 and 91).  Wavefronts: as many as fit (60000 rows of 256 bf16 beside fp32 52 us, with half of them
 // 58, with a quarter 96).
+// However many rows there are, the sums take 8 MB at most, or 512 rows of more than 4096 columns: a workgroup's 1024 / threads come to 8192 / width.
 constexpr int kMostNormParts = 2048;
 inline int norm_grad_parts(int rows, const RowShape &s) {
     const int each = 1024 / (s.lanes ? 64 : s.threads), some = rows < 4 * kMostNormParts ? rows : 4 * kMostNormParts;
@@ -90,7 +91,8 @@ inline EmbedGradPlan embed_grad_plan(int n, int width, bool single, int table_by
 }
 
 // Where things lie in the workspace, in bytes: sorted tokens and their places, the same between passes of the sort, digit counts of every tile, and
-// two rows of partial sums for every span
+// two rows of partial sums for every span.  These are 4 MB and two rows at most: chunks grow with the list, so that there are no more than 1024 / slices spans and
+// one, of slices that are 512 columns at most.
 constexpr int kMostDigitBits = 11, kSortTile = 2048;
 struct EmbedGradRoom {
     size_t places, other_sorted, other_places, counts, parts, end;
