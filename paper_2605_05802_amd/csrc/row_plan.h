@@ -20,8 +20,9 @@ struct RowShape {
 constexpr int kMostNormWidth = 16384, kMostDropWidth = 1 << 30, kMostEmbedWidth = 1 << 20;
 
 // As few vectors a thread as 1024 threads allow, but two of four columns from 512 threads on.  (Gradients: 4096 rows of 3584 bf16 beside fp32 51.4 us, one
-// each 52.8; two of eight columns, or one each with the next row's beside them, spill registers: 4096 rows of 4100 bf16 44 us in one each and 71 in two,
-// 1500 of 16384 67 with two and 199 in four.)
+// each 52.8; 4096 rows of 4100 bf16 44 us in one each and 71 in two, 1500 of 16384 69 in two and 199 in four.  Registers of the gradient's kernels: one vector of
+// four columns 64, two 104, one of eight 90, two of eight 121, without the next row's beside them, with which 23 would spill; four of four, beyond 8192 columns
+// beside fp32, 128, and 8 spilled.)
 inline RowShape norm_shape(int width, bool single) {
     RowShape s{row_vec(width, single), 1, 0, 0};
     const int n = ceil_div(width, s.per_vec);
